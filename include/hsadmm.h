@@ -22,6 +22,9 @@
  * pattern stops changing after a few iterations), which changes no result and makes a step whose selection comes
  * out as predicted touch every element once; and it forms the intra-node residual norms on the way.
  * hsadmm_stopping_test (host) is the break test of Algorithm 1's Phase 5.
+ * Around the outer iteration: hsadmm_gradient_norms and hsadmm_adamw train the replicas between two steps (Phase 1, Eq. (7)
+ * with AdamW; optimizer states in 32 or 8 bits), and hsadmm_compact_mx / hsadmm_expand_mx write the packed buffer in 8 or 4
+ * bits a value and read the nodes' buffers back.
  *
  * Data layout.  A layer is the row-major fp32 array W[c_out][c_in][khw]
  * (Section 2, first paragraph; khw = K_H*K_W, 1 for linear layers).  A
@@ -743,6 +746,165 @@ int hsadmm_step(const hsadmm_plan_t* plan, const hsadmm_step_args_t* args);
 int hsadmm_selection_from_mask(const hsadmm_plan_t* plan, const uint8_t* mask, int32_t* sel,
                                void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * Types of the gradients (and of the working copy of the weights) of the two calls below: fp32, bfloat16, IEEE half.
+ * An arena of a 16-bit type has the layout of the fp32 arenas, 2 bytes an element, and is aligned to 8 bytes.
+ */
+#define HSADMM_TYPE_F32   0
+#define HSADMM_TYPE_BF16  1
+#define HSADMM_TYPE_F16   2
+
+/*
+ * Norms of the replicas' gradients over all layers, and what clips them:
+ *     norm[r]  = sqrt(sum over the layers of G_r^2), accumulated in fp64
+ *     scale[r] = min(1, max_norm / norm[r]);  NaN where norm[r] is not finite
+ * (arena padding is not read).  `scale` is what hsadmm_adamw takes as grad_scale: it multiplies the gradient by it, and
+ * leaves a replica whose scale is not finite as it is, so a step whose gradient overflowed is skipped without the host.
+ *   G         HOST array of R DEVICE pointers, gradient arenas of grad_type
+ *   max_norm  > 0; infinity: no clipping (scale is 1, or NaN)
+ *   norm      device, R doubles, may be NULL;  scale  device, R floats, may be NULL (not both)
+ * The order of the additions depends on the plan and R alone (results are reproducible run to run).
+ * Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
+ */
+int hsadmm_gradient_norms(const hsadmm_plan_t* plan, const void* const* G, int32_t R, int32_t grad_type, double max_norm,
+                          double* norm, float* scale, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * The scalars of an AdamW step (decoupled weight decay) that change from step to step:
+ *     decay = 1 - lr weight_decay,  step_size = lr / (1 - beta_1^t),  root = 1 / sqrt(1 - beta_2^t)
+ * formed in fp64 and rounded once; noise as given.  HOST function; out is HOST memory.  step (t) >= 1 counts the updates
+ * including this one.
+ * Errors: INVALID_ARGUMENT (nothing is written): lr or weight_decay negative or not finite, a beta outside [0, 1), step < 1.
+ */
+typedef struct {
+    float decay;
+    float step_size;
+    float root;
+    uint32_t noise;    /* 8-bit states: a number that differs from step to step (any sequence, e.g. a counter's hash) */
+} hsadmm_adamw_coef_t;
+
+int hsadmm_adamw_coefficients(double lr, double beta_one, double beta_two, double weight_decay, int64_t step,
+                              uint32_t noise, hsadmm_adamw_coef_t* out);
+
+/*
+ * State blocks of a plan: with 8-bit states every 256 consecutive elements of a layer, counted from its first element, share
+ * a scale (a layer's last block may be shorter).  *blocks: all layers' blocks, in table order = the length of the scale arrays.
+ */
+int hsadmm_plan_state_blocks(const hsadmm_plan_t* plan, int64_t* blocks);
+
+/*
+ * One AdamW step of every layer of R replicas (Algorithm 1, Phase 1: the local problem of Eq. (7), with AdamW in the place of
+ * the paper's SGD).  Per replica r and element, in fp32 (every operation rounded by itself, except that the reciprocal in the
+ * last line is within one unit in the last place and the multiplications after it are fused with the subtraction):
+ *     g = scale_r G;  with Z, U, rho:  g = g + rho_l ((W - Z) + U)             the proximal term of Eq. (7)
+ *     m = beta_1 m + (1 - beta_1) g;   v = beta_2 v + (1 - beta_2) g^2
+ *     W = W decay - step_size m / (sqrt(v) root + eps);  W_low = W rounded to the gradients' type
+ * Fill a zeroed hsadmm_adamw_args_t; a NULL field means "not wanted" / "not given".  Arena padding is neither read nor written.
+ *
+ *   struct_bytes     sizeof(hsadmm_adamw_args_t) as the caller was compiled (INVALID_ARGUMENT if it differs)
+ *   R                replicas, 1 <= R <= HSADMM_MAX_REPLICAS.  The fields W .. W_low are HOST arrays of R DEVICE pointers
+ *   grad_type        HSADMM_TYPE_* of G and W_low
+ *   state_bits       32 or 8
+ *   W                in/out, full-layout arenas, 16-byte aligned
+ *   G                in, gradient arenas
+ *   M, V             in/out, the first and second moments.  32: fp32 arenas, 16-byte aligned, zeros before the first step.
+ *                    8: arenas of one byte an element, 4-byte aligned: m and the root of v as e4m3 codes in units of their
+ *                    block's scale (zeros, with scales of zero, before the first step)
+ *   M_scale, V_scale in/out, 8 bits only (NULL otherwise): arrays of hsadmm_plan_state_blocks floats
+ *   W_low            out, optional, 16-bit grad_type only: arenas that receive the rounded weights (the working copy of
+ *                    mixed-precision training)
+ *   Z, U, rho        in, all three or none: the node's consensus z_i and the replica-mean scaled dual (full-layout arenas,
+ *                    16-byte aligned), and L floats, the layers' rho_1; read once for all replicas
+ *   grad_scale       in, optional, R floats (hsadmm_gradient_norms); a replica whose factor is not finite is left untouched
+ *   coef             in, optional, DEVICE: takes the place of lr, weight_decay, step and noise (hsadmm_adamw_coefficients).
+ *                    Read by the kernel when it runs, so a captured graph follows the buffer's contents from replay to replay.
+ *   lr, beta_one, beta_two, eps, weight_decay, step, noise   as in hsadmm_adamw_coefficients; eps >= 2^-126
+ *
+ * 8-bit states.  A block's scale is its largest |m| (root) / 448, after the update; the update itself uses the unrounded
+ * moments.  Codes are rounded stochastically, so a moment that moves by less than a code a step still moves on average (to
+ * nearest, beta_2 = 0.999 would hold a root for good): y becomes floor(y / step + u) step on e4m3's grid, u in [0, 1) in steps of
+ * 2^-20 from the upper 20 bits of a mix of noise, r and the element's place (the same u for m and root; results are a
+ * function of the arguments alone).  A root that is not zero keeps at least the smallest code: a zero would divide the next
+ * update by eps alone.  A block whose largest magnitude is below 2^-100 is held as zero; one with a value that is not
+ * finite reads back as not finite everywhere.
+ *
+ * The arenas written (W, M, V, the scales, W_low) must not overlap each other or any input (INVALID_ARGUMENT); inputs may
+ * overlap (replicas may share one gradient).
+ * Errors: INVALID_ARGUMENT, UNSUPPORTED (R, state_bits, grad_type), HIP.
+ */
+typedef struct {
+    size_t struct_bytes;
+    int32_t R;
+    int32_t grad_type;
+    int32_t state_bits;
+    uint32_t noise;
+    float* const* W;
+    const void* const* G;
+    void* const* M;
+    void* const* V;
+    float* const* M_scale;
+    float* const* V_scale;
+    void* const* W_low;
+    const float* Z;
+    const float* U;
+    const float* rho;
+    const float* grad_scale;
+    const hsadmm_adamw_coef_t* coef;
+    double lr;
+    double beta_one;
+    double beta_two;
+    double eps;
+    double weight_decay;
+    int64_t step;
+    void* hip_stream;
+} hsadmm_adamw_args_t;
+
+int hsadmm_adamw(const hsadmm_plan_t* plan, const hsadmm_adamw_args_t* args);
+
+/*
+ * Formats of a quantised packed buffer: blocks of 32 consecutive packed positions share a scale 2^(byte - 127) (byte 255: the
+ * block is NaN).  FP8: one byte a value, e4m3 (largest 448).  FP4: two values a byte, e2m1 (largest 6), the first in the low
+ * half.  Buffers: packed_capacity_elems bytes of codes (FP4: half), 16-byte aligned, and packed_capacity_elems / 32 scale bytes.
+ */
+#define HSADMM_MX_FP8   0
+#define HSADMM_MX_FP4   1
+
+/*
+ * Tensor shrinkage into a quantised buffer (Section 4.4.1, Eq. (15); the pre-transmission buffer of Algorithm 1, Phase 4): the
+ * values hsadmm_compact (src1 NULL) or hsadmm_compact_sum packs, at the same places, in the codes of `format`, quantised as
+ * they are packed.  A block's scale is the least 2^e, e >= -127, with which its largest magnitude does not exceed the format's
+ * largest value; codes are the nearest values that are finite in fp32, ties to even.  A block with a value that is not finite
+ * becomes NaN.
+ * The plan's pack_align_elems must be a multiple of 32 (UNSUPPORTED otherwise), so that no block holds two layers; the
+ * places of a layer's last block after its last value hold code 0.  Alignment padding beyond that block is not written.
+ *   src0, src1  device, full-layout arenas (read only), 16-byte aligned; src1 may be NULL
+ *   mask        as in hsadmm_compact (NULL: the index mappings held in this workspace)
+ *   codes, scales   device, out
+ *   layer_off, kept_idx, workspace  as in hsadmm_compact (layer_off counts elements)
+ * Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
+ */
+int hsadmm_compact_mx(const hsadmm_plan_t* plan, const float* src0, const float* src1, const uint8_t* mask, int32_t format,
+                      uint8_t* codes, uint8_t* scales, int64_t* layer_off, int32_t* kept_idx,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Global consensus and recovery from the quantised buffers of M nodes in one pass (Eq. (11); Section 4.4.3; Algorithm 1,
+ * Phase 4 behind an all-gather of the nodes' buffers): with d_i the values node i's codes stand for,
+ *     dst = ((d_0 + d_1) + ... + d_{M-1}) * fl32(1/M)  on kept positions (fp32, node order), +0 on all others of every layer,
+ * what hsadmm_average and hsadmm_expand give for the buffers' values; with Zi and Vd also the inter-node dual update
+ * Vd <- Vd + (Zi - dst) of Eq. (13), as hsadmm_expand_dual.  M = 1 reads a single buffer back.
+ *   codes, scales  HOST arrays of M DEVICE pointers (1 <= M <= HSADMM_MAX_MASKS), buffers of `format` written under this mask;
+ *                  codes 16-byte aligned
+ *   mask           as in hsadmm_expand (NULL: the index mappings held in this workspace)
+ *   dst            device, out, full-layout arena, 16-byte aligned
+ *   Zi, Vd         both or none (INVALID_ARGUMENT), 16-byte aligned; dst, Zi and Vd must not overlap (INVALID_ARGUMENT)
+ * The plan's pack_align_elems must be a multiple of 32 (UNSUPPORTED otherwise).
+ * Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
+ */
+int hsadmm_expand_mx(const hsadmm_plan_t* plan, const uint8_t* const* codes, const uint8_t* const* scales, int32_t M,
+                     int32_t format, const uint8_t* mask, float* dst, const float* Zi, float* Vd,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Static string for an error code (never NULL). */
 const char* hsadmm_strerror(int code);
 
@@ -769,7 +931,7 @@ int hsadmm_version(void);
  * profile taken elsewhere can be matched to the plan it is quoted for.
  * Errors: INVALID_ARGUMENT, HOST_MEMORY, HIP.
  */
-#define HSADMM_KERNEL_COUNT 29
+#define HSADMM_KERNEL_COUNT 34
 int hsadmm_kernel_timing_enable(hsadmm_plan_t* plan, int enable);
 int hsadmm_kernel_timing_read(hsadmm_plan_t* plan, double* total_ms, int64_t* launches);
 int hsadmm_kernel_grid(const hsadmm_plan_t* plan, int kernel_id);

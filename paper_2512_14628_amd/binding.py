@@ -19,6 +19,8 @@ INCLUDE_DIR = os.path.join(_ROOT, "include")
 LIB_PATH = os.environ.get("HSADMM_LIB") or os.path.join(_HERE, "libhsadmm.so")
 
 MODE_NONE, MODE_FILTER, MODE_CHANNEL, MODE_BOTH = 0, 1, 2, 3
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+MX_FP8, MX_FP4 = 0, 1
 MAX_REPLICAS = 16
 
 HIPCC_FLAGS = [
@@ -38,8 +40,10 @@ EXPORTS = ("hsadmm_plan_create", "hsadmm_plan_destroy", "hsadmm_plan_sizes", "hs
            "hsadmm_retrain_project", "hsadmm_retrain_expand",
            "hsadmm_adapt_penalties", "hsadmm_scale_layers", "hsadmm_project_compact_static",
            "hsadmm_step", "hsadmm_selection_from_mask", "hsadmm_kernel_grid", "hsadmm_plan_estimates",
-           "hsadmm_layer_sqnorms", "hsadmm_stopping_test", "hsadmm_plan_create_nested")
-KERNEL_COUNT = 29
+           "hsadmm_layer_sqnorms", "hsadmm_stopping_test", "hsadmm_plan_create_nested",
+           "hsadmm_gradient_norms", "hsadmm_adamw_coefficients", "hsadmm_plan_state_blocks", "hsadmm_adamw",
+           "hsadmm_compact_mx", "hsadmm_expand_mx")
+KERNEL_COUNT = 34
 
 
 class HsadmmError(RuntimeError):
@@ -78,6 +82,31 @@ _STEP_FIELDS = (
 
 class _StepArgs(ctypes.Structure):
     _fields_ = [(name, ctype) for name, ctype, _ in _STEP_FIELDS]
+
+
+class _AdamwCoef(ctypes.Structure):
+    _fields_ = [("decay", ctypes.c_float), ("step_size", ctypes.c_float), ("root", ctypes.c_float),
+                ("noise", ctypes.c_uint32)]
+
+
+# hsadmm_adamw_args_t, field by field, in declaration order, as _STEP_FIELDS.
+#   "each": HOST array of one device buffer per replica (a sequence, or None), "int" / "float": a scalar
+_ADAMW_FIELDS = (
+    ("struct_bytes", ctypes.c_size_t, "sizeof"),
+    ("R", ctypes.c_int32, "replica_count"), ("grad_type", ctypes.c_int32, "int"),
+    ("state_bits", ctypes.c_int32, "int"), ("noise", ctypes.c_uint32, "int"),
+    ("W", ctypes.POINTER(_vp), "each"), ("G", ctypes.POINTER(_vp), "each"), ("M", ctypes.POINTER(_vp), "each"),
+    ("V", ctypes.POINTER(_vp), "each"), ("M_scale", ctypes.POINTER(_vp), "each"),
+    ("V_scale", ctypes.POINTER(_vp), "each"), ("W_low", ctypes.POINTER(_vp), "each"),
+    ("Z", _vp, "dev"), ("U", _vp, "dev"), ("rho", _vp, "dev"), ("grad_scale", _vp, "dev"), ("coef", _vp, "dev"),
+    ("lr", ctypes.c_double, "float"), ("beta_one", ctypes.c_double, "float"), ("beta_two", ctypes.c_double, "float"),
+    ("eps", ctypes.c_double, "float"), ("weight_decay", ctypes.c_double, "float"), ("step", ctypes.c_int64, "int"),
+    ("hip_stream", _vp, "stream"),
+)
+
+
+class _AdamwArgs(ctypes.Structure):
+    _fields_ = [(name, ctype) for name, ctype, _ in _ADAMW_FIELDS]
 
 
 _lib = None
@@ -199,6 +228,21 @@ def load_library():
                                          dp, dp, dp, dp, ctypes.c_double,
                                          ctypes.c_double, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
     lib.hsadmm_stopping_test.restype = ctypes.c_int
+    lib.hsadmm_gradient_norms.argtypes = [vp, ctypes.POINTER(vp), ctypes.c_int32, ctypes.c_int32, ctypes.c_double, vp, vp,
+                                          vp, ctypes.c_size_t, vp]
+    lib.hsadmm_gradient_norms.restype = ctypes.c_int
+    lib.hsadmm_adamw_coefficients.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                              ctypes.c_int64, ctypes.c_uint32, ctypes.POINTER(_AdamwCoef)]
+    lib.hsadmm_adamw_coefficients.restype = ctypes.c_int
+    lib.hsadmm_plan_state_blocks.argtypes = [vp, ctypes.POINTER(ctypes.c_int64)]
+    lib.hsadmm_plan_state_blocks.restype = ctypes.c_int
+    lib.hsadmm_adamw.argtypes = [vp, ctypes.POINTER(_AdamwArgs)]
+    lib.hsadmm_adamw.restype = ctypes.c_int
+    lib.hsadmm_compact_mx.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.hsadmm_compact_mx.restype = ctypes.c_int
+    lib.hsadmm_expand_mx.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.c_int32, ctypes.c_int32, vp, vp,
+                                     vp, vp, vp, ctypes.c_size_t, vp]
+    lib.hsadmm_expand_mx.restype = ctypes.c_int
     lib.hsadmm_kernel_grid.argtypes = [vp, ctypes.c_int]
     lib.hsadmm_kernel_grid.restype = ctypes.c_int
     lib.hsadmm_plan_estimates.argtypes = [vp]
@@ -709,4 +753,108 @@ def hsadmm_expand_dual(plan: Plan, packed, mask, dst, Zi, Vd, workspace, stream=
                                 wb, _stream(stream))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_expand_dual")
+    return rc
+
+
+def _each(buffers):
+    """HOST array of the device addresses of one buffer per replica or node; None -> NULL."""
+    if buffers is None:
+        return None
+    return (ctypes.c_void_p * max(len(buffers), 1))(*[_ptr(b) for b in buffers])
+
+
+def hsadmm_gradient_norms(plan: Plan, G: Sequence, max_norm: float, norm, scale, workspace, grad_type: int = TYPE_F32,
+                          stream=None, workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    """Norms of the replicas' gradients and the factors that clip them (NaN: not finite); either output may be None."""
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    rc = load_library().hsadmm_gradient_norms(plan.handle, _each(G), len(G), int(grad_type), float(max_norm), _ptr(norm),
+                                              _ptr(scale), _ptr(workspace), wb, _stream(stream))
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_gradient_norms")
+    return rc
+
+
+def hsadmm_adamw_coefficients(lr: float, beta_one: float, beta_two: float, weight_decay: float, step: int,
+                              noise: int = 0):
+    """(decay, step_size, root, noise) of an AdamW step; as bytes on the device (three floats, one uint32) they are
+    hsadmm_adamw's `coef`."""
+    out = _AdamwCoef()
+    rc = load_library().hsadmm_adamw_coefficients(float(lr), float(beta_one), float(beta_two), float(weight_decay),
+                                                  int(step), int(noise) & 0xFFFFFFFF, ctypes.byref(out))
+    if rc != 0:
+        raise HsadmmError(rc, "hsadmm_adamw_coefficients")
+    return out.decay, out.step_size, out.root, out.noise
+
+
+def hsadmm_plan_state_blocks(plan: Plan) -> int:
+    """Length of the scale arrays of 8-bit optimizer states."""
+    n = ctypes.c_int64()
+    rc = load_library().hsadmm_plan_state_blocks(plan.handle, ctypes.byref(n))
+    if rc != 0:
+        raise HsadmmError(rc, "hsadmm_plan_state_blocks")
+    return n.value
+
+
+def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence, stream=None, check: bool = True,
+                 **fields) -> int:
+    """One AdamW step of every layer of every replica.  W, G, M, V: one buffer per replica; keyword arguments are the
+    other fields of hsadmm_adamw_args_t (grad_type, state_bits, M_scale, V_scale, W_low, Z, U, rho, grad_scale, coef, lr,
+    beta_one, ...).  Not given: grad_type TYPE_F32, state_bits 32, beta_one 0.9, beta_two 0.999, eps 1e-8, step 1; buffers
+    stay NULL, other numbers 0."""
+    lib = load_library()
+    known = {name for name, _, how in _ADAMW_FIELDS if how in ("dev", "each", "int", "float")} - {"W", "G", "M", "V"}
+    unknown = set(fields) - known
+    if unknown:
+        raise TypeError("hsadmm_adamw has no field(s) %s" % ", ".join(sorted(unknown)))
+    for name in ("G", "M", "V", "M_scale", "V_scale", "W_low"):
+        buffers = {"G": G, "M": M, "V": V}.get(name, fields.get(name))
+        if buffers is not None and len(buffers) != len(W):
+            raise ValueError("hsadmm_adamw: %d buffers in %s, %d replicas" % (len(buffers), name, len(W)))
+    values = {"state_bits": 32, "beta_one": 0.9, "beta_two": 0.999, "eps": 1e-8, "step": 1, **fields,
+              "W": W, "G": G, "M": M, "V": V}
+    args = _AdamwArgs()
+    for name, _, how in _ADAMW_FIELDS:
+        if how == "sizeof":
+            value = ctypes.sizeof(_AdamwArgs)
+        elif how == "replica_count":
+            value = len(W)
+        elif how == "each":
+            value = _each(values.get(name))
+        elif how == "dev":
+            value = _ptr(values.get(name))
+        elif how == "int":
+            value = int(values.get(name, 0))
+        elif how == "float":
+            value = float(values.get(name, 0.0))
+        else:
+            value = _stream(stream)
+        setattr(args, name, value)
+    rc = lib.hsadmm_adamw(plan.handle, ctypes.byref(args))
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_adamw")
+    return rc
+
+
+def hsadmm_compact_mx(plan: Plan, src0, src1, mask, format: int, codes, scales, layer_off, kept_idx, workspace, stream=None,
+                      workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    """hsadmm_compact (src1 None) or hsadmm_compact_sum into codes of MX_FP8 or MX_FP4 and a scale byte per 32 of them."""
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    rc = load_library().hsadmm_compact_mx(plan.handle, _ptr(src0), _ptr(src1), _ptr(mask), int(format), _ptr(codes),
+                                          _ptr(scales), _ptr(layer_off), _ptr(kept_idx), _ptr(workspace), wb,
+                                          _stream(stream))
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_compact_mx")
+    return rc
+
+
+def hsadmm_expand_mx(plan: Plan, codes: Sequence, scales: Sequence, format: int, mask, dst, Zi, Vd, workspace, stream=None,
+                     workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    """The mean of the nodes' quantised buffers, scattered to full layout; with Zi and Vd also Vd <- Vd + (Zi - dst)."""
+    if len(codes) != len(scales):
+        raise ValueError("hsadmm_expand_mx: %d buffers of codes, %d of scales" % (len(codes), len(scales)))
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    rc = load_library().hsadmm_expand_mx(plan.handle, _each(codes), _each(scales), len(codes), int(format), _ptr(mask),
+                                         _ptr(dst), _ptr(Zi), _ptr(Vd), _ptr(workspace), wb, _stream(stream))
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_expand_mx")
     return rc

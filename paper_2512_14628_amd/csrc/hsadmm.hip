@@ -80,6 +80,8 @@
 #include "kernels_held.hpp"
 #include "kernels_residuals.hpp"
 #include "kernels_compact.hpp"
+#include "kernels_training.hpp"
+#include "kernels_mx.hpp"
 
 namespace {
 
@@ -108,7 +110,7 @@ struct WsLayout {
     size_t key, colpart, pos, cnt, layer_off, kept_idx, respart, work, rowres, pred, est_cnt, est_keys, est_thr, est_thr_tag, nest, total;
 };
 
-enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kKernelCount };
+enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kKernelCount };
 static_assert(kKernelCount == HSADMM_KERNEL_COUNT, "kernel id table");
 constexpr size_t kTimingPairs = 8192;
 constexpr size_t kRepairGrid = 2048;       // workgroups of the repair pass under a prediction: 8 per compute unit
@@ -144,6 +146,8 @@ struct hsadmm_plan {
     std::vector<WorkItem> items_chan;   // channel_final: the row items of the CHANNEL layers (a subset of items_rows)
     std::vector<WorkItem> items_both;   // composite_colsums: tiles of the layers under both constraints
     std::vector<int32_t> both_layers;   // their indices
+    std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, gather_mx, scatter_mx: every layer cut without regard to rows
+    int64_t state_blocks = 0;           // blocks that share a scale in 8-bit optimizer states
     int32_t n_segments = 0;             // scan segments (one per layer, two per BOTH layer)
     int32_t pack_align = 1;
     int64_t arena_elems = 0;
@@ -166,6 +170,7 @@ struct hsadmm_plan {
     WorkItem* d_items_chan = nullptr;
     WorkItem* d_items_both = nullptr;
     int32_t* d_both_layers = nullptr;
+    FlatItem* d_items_flat = nullptr;
     uint16_t* d_group_layer = nullptr;   // groups_total: scan segment of every group (bit 15: unconstrained layer)
     float* d_coef = nullptr;             // 2L: a_l, b_l of Eq. (9), set by hsadmm_plan_set_node_weights (default 1, 0)
     void* static_ws = nullptr;           // device address of `scratch` on the plan's device
@@ -409,6 +414,8 @@ int lay_out(hsadmm_plan* p, const hsadmm_layer_t* layers, const hsadmm_nest_t* n
         items->clear();
     p->dev_layers.clear();
     p->both_layers.clear();
+    p->items_flat.clear();
+    p->state_blocks = 0;
     int64_t gb = 0, cp = 0, cap = 0, poff = 0, nest_bytes = 0;
     int32_t seg = 0, kstart = 0;
     group_layer.clear();
@@ -478,6 +485,11 @@ int lay_out(hsadmm_plan* p, const hsadmm_layer_t* layers, const hsadmm_nest_t* n
         if (x.mode == HSADMM_MODE_NONE) add_row_items(p->items_none, l, d, x.mode, fine);
         if (!has_colsums) add_row_items(p->items_plain, l, d, x.mode, fine);
         d.rows_items = (int32_t)p->items_rows.size() - d.rows_item0;
+        const int64_t n_layer = (int64_t)x.c_out * d.row_len;
+        for (int64_t o = 0; o < n_layer; o += kFlatElems)
+            p->items_flat.push_back(FlatItem{x.elem_off + o, p->state_blocks + o / kStateBlock,
+                                             (int32_t)std::min<int64_t>(kFlatElems, n_layer - o), l});
+        p->state_blocks += (n_layer + kStateBlock - 1) / kStateBlock;
         if (x.mode == HSADMM_MODE_CHANNEL) {
             add_tile_items(p->items_proj, l, d, kChanRows, wide_strips);
             add_row_items(p->items_chan, l, d, x.mode, fine);
@@ -694,6 +706,40 @@ unsigned long long held_number() noexcept
     return 0xFFF4000000000000ull | ((start + 4 * calls.fetch_add(1, std::memory_order_relaxed)) & 0x3FFFFFFFFFFFCull);
 }
 
+// The stretches of memory a call reads and writes: true if one that is written overlaps another.
+struct Stretches {
+    struct One { uintptr_t from, to; bool written; };
+    One all[8 * HSADMM_MAX_REPLICAS + 8];
+    int n = 0;
+    void add(const void* at, size_t bytes, bool written)
+    {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(at);
+        all[n++] = One{from, from + bytes, written};
+    }
+    bool clash()
+    {
+        std::sort(all, all + n, [](const One& a, const One& b) { return a.from < b.from; });
+        uintptr_t any = 0, written = 0;          // where the ones seen so far end
+        for (int i = 0; i < n; ++i) {
+            if (all[i].from < written || (all[i].written && all[i].from < any)) return true;
+            any = std::max(any, all[i].to);
+            if (all[i].written) written = std::max(written, all[i].to);
+        }
+        return false;
+    }
+};
+
+template <int T, bool S8>
+hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool prox, bool low, hipStream_t s)
+{
+    const auto go = [&](auto kernel) {
+        return launch(p, kAdamw, kernel, (unsigned)p->items_flat.size(), kBlock, s, (const FlatItem*)p->d_items_flat, a, R);
+    };
+    if constexpr (T != HSADMM_TYPE_F32)
+        if (low) return prox ? go(adamw_kernel<T, S8, true, true>) : go(adamw_kernel<T, S8, false, true>);
+    return prox ? go(adamw_kernel<T, S8, true, false>) : go(adamw_kernel<T, S8, false, false>);
+}
+
 bool stream_is_captured(hipStream_t s)
 {
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
@@ -854,6 +900,7 @@ int hsadmm_plan_create_nested(const hsadmm_layer_t* layers, const hsadmm_nest_t*
     upload(p->items_chan, &p->d_items_chan);
     upload(p->items_both, &p->d_items_both);
     upload(p->both_layers, &p->d_both_layers);
+    upload(p->items_flat, &p->d_items_flat);
     upload(group_layer, &p->d_group_layer);
     upload(chunk_layer, &p->d_chunk_layer);
     upload(coef, &p->d_coef);
@@ -884,6 +931,7 @@ void hsadmm_plan_destroy(hsadmm_plan_t* p)
     if (p->d_items_chan) (void)hipFree(p->d_items_chan);
     if (p->d_items_both) (void)hipFree(p->d_items_both);
     if (p->d_both_layers) (void)hipFree(p->d_both_layers);
+    if (p->d_items_flat) (void)hipFree(p->d_items_flat);
     if (p->d_group_layer) (void)hipFree(p->d_group_layer);
     if (p->d_chunk_layer) (void)hipFree(p->d_chunk_layer);
     if (p->d_coef) (void)hipFree(p->d_coef);
@@ -1941,6 +1989,209 @@ int hsadmm_retrain_expand(const hsadmm_plan_t* p, const float* packed, const uin
                        residuals, true);
 }
 
+// ------------------------------------------------------------------ local training (Algorithm 1, Phase 1)
+
+// Workgroups of the sums of squares over all replicas: eight per compute unit.
+constexpr int64_t kGradGrid = 2048;
+
+int hsadmm_gradient_norms(const hsadmm_plan_t* p, const void* const* G, int32_t R, int32_t grad_type, double max_norm,
+                          double* norm, float* scale, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    if (!p || !G || (!norm && !scale) || !workspace || R < 1 || !(max_norm > 0.0)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (R > HSADMM_MAX_REPLICAS || grad_type < HSADMM_TYPE_F32 || grad_type > HSADMM_TYPE_F16) return HSADMM_ERR_UNSUPPORTED;
+    if ((norm && !is_aligned(norm, 8)) || (scale && !is_aligned(scale, 4)) || !is_aligned(workspace, 256))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    GradArgs a{};
+    for (int r = 0; r < R; ++r) {
+        if (!G[r] || !is_aligned(G[r], grad_type == HSADMM_TYPE_F32 ? 16 : 8)) return HSADMM_ERR_INVALID_ARGUMENT;
+        a.G[r] = G[r];
+    }
+    if (workspace_bytes < p->ws.total) return HSADMM_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    // a partial sum per workgroup, in the place of the residual sums' partials (four doubles a row item, 32 at least)
+    const int64_t room = (int64_t)((p->ws.work - p->ws.respart) / sizeof(double));
+    const int n_items = (int)p->items_flat.size();
+    const int P = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)n_items, kGradGrid / R, room / R}));
+    double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + p->ws.respart);
+    const auto sums = [&](auto kernel) {
+        return launch(p, kGradSq, kernel, (unsigned)(P * R), kBlock, s, (const FlatItem*)p->d_items_flat, n_items, a, P, part);
+    };
+    hipError_t e = grad_type == HSADMM_TYPE_F32 ? sums(gradient_sqsums<HSADMM_TYPE_F32>)
+                 : grad_type == HSADMM_TYPE_BF16 ? sums(gradient_sqsums<HSADMM_TYPE_BF16>)
+                                                 : sums(gradient_sqsums<HSADMM_TYPE_F16>);
+    if (e != hipSuccess) return HSADMM_ERR_HIP;
+    e = launch(p, kGradFinish, gradient_norm_finish, (unsigned)R, kBlock, s, (const double*)part, P, max_norm, norm, scale);
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}
+
+int hsadmm_adamw_coefficients(double lr, double beta_one, double beta_two, double weight_decay, int64_t step,
+                              uint32_t noise, hsadmm_adamw_coef_t* out)
+{
+    const auto size = [](double x) { return x >= 0.0 && x <= 1e300; };      // (a NaN fails its comparison)
+    if (!out || !size(lr) || !size(weight_decay) || !(beta_one >= 0.0 && beta_one < 1.0) ||
+        !(beta_two >= 0.0 && beta_two < 1.0) || step < 1)
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    out->decay = (float)(1.0 - lr * weight_decay);
+    out->step_size = (float)(lr / (1.0 - std::pow(beta_one, (double)step)));
+    out->root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta_two, (double)step)));
+    out->noise = noise;
+    return HSADMM_OK;
+}
+
+int hsadmm_plan_state_blocks(const hsadmm_plan_t* p, int64_t* blocks)
+{
+    if (!p || !blocks) return HSADMM_ERR_INVALID_ARGUMENT;
+    *blocks = p->state_blocks;
+    return HSADMM_OK;
+}
+
+int hsadmm_adamw(const hsadmm_plan_t* p, const hsadmm_adamw_args_t* x)
+{
+    if (!p || !x || x->struct_bytes != sizeof(hsadmm_adamw_args_t)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!x->W || !x->G || !x->M || !x->V || x->R < 1) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (x->R > HSADMM_MAX_REPLICAS || x->grad_type < HSADMM_TYPE_F32 || x->grad_type > HSADMM_TYPE_F16 ||
+        (x->state_bits != 32 && x->state_bits != 8))
+        return HSADMM_ERR_UNSUPPORTED;
+    const bool eight = x->state_bits == 8, wide = x->grad_type == HSADMM_TYPE_F32;
+    const bool prox = x->Z || x->U || x->rho;
+    if (eight != (x->M_scale != nullptr) || eight != (x->V_scale != nullptr)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (x->W_low && wide) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (prox && (!x->Z || !x->U || !x->rho || !is_aligned(x->Z, 16) || !is_aligned(x->U, 16) || !is_aligned(x->rho, 4)))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if ((x->grad_scale && !is_aligned(x->grad_scale, 4)) || (x->coef && !is_aligned(x->coef, 4)))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    AdamwArgs a{};
+    // (with coef on the device its own values decide; the betas are checked all the same)
+    if (hsadmm_adamw_coefficients(x->coef ? 0.0 : x->lr, x->beta_one, x->beta_two, x->coef ? 0.0 : x->weight_decay,
+                                  x->coef ? 1 : x->step, x->noise, &a.coef) != HSADMM_OK)
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!(x->eps >= 0x1p-126 && x->eps <= 1e30)) return HSADMM_ERR_INVALID_ARGUMENT;
+    const size_t n = (size_t)p->arena_elems, blocks = (size_t)p->state_blocks;
+    Stretches used;
+    for (int r = 0; r < x->R; ++r) {
+        a.W[r] = x->W[r]; a.G[r] = x->G[r]; a.M[r] = x->M[r]; a.V[r] = x->V[r];
+        if (!a.W[r] || !a.G[r] || !a.M[r] || !a.V[r] || !is_aligned(a.W[r], 16) || !is_aligned(a.G[r], wide ? 16 : 8) ||
+            !is_aligned(a.M[r], eight ? 4 : 16) || !is_aligned(a.V[r], eight ? 4 : 16))
+            return HSADMM_ERR_INVALID_ARGUMENT;
+        used.add(a.W[r], 4 * n, true);
+        used.add(a.G[r], wide ? 4 * n : 2 * n, false);
+        used.add(a.M[r], eight ? n : 4 * n, true);
+        used.add(a.V[r], eight ? n : 4 * n, true);
+        if (eight) {
+            a.Ms[r] = x->M_scale[r]; a.Vs[r] = x->V_scale[r];
+            if (!a.Ms[r] || !a.Vs[r] || !is_aligned(a.Ms[r], 4) || !is_aligned(a.Vs[r], 4)) return HSADMM_ERR_INVALID_ARGUMENT;
+            used.add(a.Ms[r], 4 * blocks, true);
+            used.add(a.Vs[r], 4 * blocks, true);
+        }
+        if (x->W_low) {
+            a.Wl[r] = x->W_low[r];
+            if (!a.Wl[r] || !is_aligned(a.Wl[r], 8)) return HSADMM_ERR_INVALID_ARGUMENT;
+            used.add(a.Wl[r], 2 * n, true);
+        }
+    }
+    if (prox) {
+        used.add(x->Z, 4 * n, false);
+        used.add(x->U, 4 * n, false);
+        used.add(x->rho, 4 * p->layers.size(), false);
+    }
+    if (x->grad_scale) used.add(x->grad_scale, 4 * (size_t)x->R, false);
+    if (x->coef) used.add(x->coef, sizeof(hsadmm_adamw_coef_t), false);
+    if (used.clash()) return HSADMM_ERR_INVALID_ARGUMENT;
+    a.Z = x->Z; a.U = x->U; a.rho = x->rho;
+    a.grad_scale = x->grad_scale;
+    a.coef_dev = x->coef;
+    a.beta1 = (float)x->beta_one; a.one_minus_beta1 = (float)(1.0 - x->beta_one);
+    a.beta2 = (float)x->beta_two; a.one_minus_beta2 = (float)(1.0 - x->beta_two);
+    a.eps = (float)x->eps;
+    hipStream_t s = static_cast<hipStream_t>(x->hip_stream);
+    const auto typed = [&](auto t) {
+        constexpr int T = decltype(t)::value;
+        return eight ? launch_adamw<T, true>(p, a, x->R, prox, x->W_low != nullptr, s)
+                     : launch_adamw<T, false>(p, a, x->R, prox, x->W_low != nullptr, s);
+    };
+    const hipError_t e = wide ? typed(std::integral_constant<int, HSADMM_TYPE_F32>{})
+                       : x->grad_type == HSADMM_TYPE_BF16 ? typed(std::integral_constant<int, HSADMM_TYPE_BF16>{})
+                                                          : typed(std::integral_constant<int, HSADMM_TYPE_F16>{});
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}
+
+// ------------------------------------------------------------------ quantised packed buffers
+
+static MxMaps mx_maps(const hsadmm_plan* p, const char* ws)
+{
+    MxMaps m;
+    m.pos = reinterpret_cast<const int32_t*>(ws + p->ws.pos);
+    m.cnt = reinterpret_cast<const int32_t*>(ws + p->ws.cnt);
+    m.kept_idx = reinterpret_cast<const int32_t*>(ws + p->ws.kept_idx);
+    m.layer_off = reinterpret_cast<const int64_t*>(ws + p->ws.layer_off);
+    m.n_layers = (int)p->layers.size();
+    return m;
+}
+
+int hsadmm_compact_mx(const hsadmm_plan_t* p, const float* src0, const float* src1, const uint8_t* mask, int32_t format,
+                      uint8_t* codes, uint8_t* scales, int64_t* layer_off, int32_t* kept_idx, void* workspace,
+                      size_t workspace_bytes, void* hip_stream)
+{
+    if (!p || !src0 || !codes || !scales || !layer_off || !kept_idx || !workspace) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if ((format != HSADMM_MX_FP8 && format != HSADMM_MX_FP4) || p->pack_align % kMxBlock != 0) return HSADMM_ERR_UNSUPPORTED;
+    if (!is_aligned(src0, 16) || (src1 && !is_aligned(src1, 16)) || !is_aligned(codes, 16) || !is_aligned(layer_off, 8) ||
+        !is_aligned(kept_idx, 4) || !is_aligned(workspace, 256))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if (workspace_bytes < p->ws.total) return HSADMM_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    char* ws = static_cast<char*>(workspace);
+    if (mask) {
+        const int rc = run_scan(p, mask, ws, s);
+        if (rc != HSADMM_OK) return rc;
+    }
+    const auto go = [&](auto kernel) {
+        return launch(p, kGatherMx, kernel, (unsigned)p->items_flat.size(), kBlock, s, (const FlatItem*)p->d_items_flat,
+                      (const DevLayer*)p->d_layers, src0, src1, mx_maps(p, ws), codes, scales, CopyOut{layer_off, kept_idx});
+    };
+    const hipError_t e = format == HSADMM_MX_FP8 ? (src1 ? go(gather_mx<HSADMM_MX_FP8, true>) : go(gather_mx<HSADMM_MX_FP8, false>))
+                                                 : (src1 ? go(gather_mx<HSADMM_MX_FP4, true>) : go(gather_mx<HSADMM_MX_FP4, false>));
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}
+
+int hsadmm_expand_mx(const hsadmm_plan_t* p, const uint8_t* const* codes, const uint8_t* const* scales, int32_t M,
+                     int32_t format, const uint8_t* mask, float* dst, const float* Zi, float* Vd, void* workspace,
+                     size_t workspace_bytes, void* hip_stream)
+{
+    if (!p || !codes || !scales || !dst || !workspace || M < 1 || (Zi != nullptr) != (Vd != nullptr))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (M > HSADMM_MAX_MASKS || (format != HSADMM_MX_FP8 && format != HSADMM_MX_FP4) || p->pack_align % kMxBlock != 0)
+        return HSADMM_ERR_UNSUPPORTED;
+    if (!is_aligned(dst, 16) || !is_aligned(workspace, 256) || (Zi && (!is_aligned(Zi, 16) || !is_aligned(Vd, 16))))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if (Zi && (spans_overlap(dst, Zi, p->arena_elems) || spans_overlap(dst, Vd, p->arena_elems) ||
+               spans_overlap(Zi, Vd, p->arena_elems)))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    MxBuffers b{};
+    for (int i = 0; i < M; ++i) {
+        if (!codes[i] || !scales[i] || !is_aligned(codes[i], 16)) return HSADMM_ERR_INVALID_ARGUMENT;
+        b.codes[i] = codes[i];
+        b.scales[i] = scales[i];
+    }
+    if (workspace_bytes < p->ws.total) return HSADMM_ERR_WORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    char* ws = static_cast<char*>(workspace);
+    if (mask) {
+        const int rc = run_scan(p, mask, ws, s);
+        if (rc != HSADMM_OK) return rc;
+    }
+    const auto go = [&](auto kernel) {
+        return launch(p, kScatterMx, kernel, (unsigned)p->items_flat.size(), kBlock, s, (const FlatItem*)p->d_items_flat,
+                      (const DevLayer*)p->d_layers, b, (int)M, 1.0f / (float)M, mx_maps(p, ws), dst, Zi, Vd);
+    };
+    const hipError_t e = format == HSADMM_MX_FP8 ? (Zi ? go(scatter_mx<HSADMM_MX_FP8, true>) : go(scatter_mx<HSADMM_MX_FP8, false>))
+                                                 : (Zi ? go(scatter_mx<HSADMM_MX_FP4, true>) : go(scatter_mx<HSADMM_MX_FP4, false>));
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}
+
 const char* hsadmm_strerror(int code)
 {
     switch (code) {
@@ -2033,6 +2284,11 @@ const char* hsadmm_kernel_name(int kernel_id)
         case kSqnormPart: return "sqnorm_partials";
         case kResPick: return "residual_pick";
         case kWHintedRepair: return "weighted_hinted_repair";
+        case kGradSq: return "gradient_sqsums";
+        case kGradFinish: return "gradient_norm_finish";
+        case kAdamw: return "adamw";
+        case kGatherMx: return "gather_mx";
+        case kScatterMx: return "scatter_mx";
         default: return "";
     }
 }

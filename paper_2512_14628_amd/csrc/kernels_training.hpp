@@ -1,0 +1,340 @@
+// hsadmm_gradient_norms / hsadmm_adamw: the replicas' own training step between two steps of the consensus (Algorithm 1,
+// Phase 1; Eq. (7) with AdamW), all layers of all replicas in one launch.
+// Part of the single translation unit built from hsadmm.hip (included there, in order).
+#ifndef KERNELS_TRAINING_HPP
+#define KERNELS_TRAINING_HPP
+#include "hsadmm_device.hpp"
+#include "kernels_select.hpp"
+
+namespace {
+
+// ------------------------------------------------------------------ flat items
+
+// kFlatElems consecutive elements of one layer (fewer at its end): the unit of work of the kernels that do not care about
+// groups.  A thread of the workgroup owns kFlatQuads fours of adjacent elements, kBlock fours apart, so a wave's access is
+// contiguous and a wave's 64 fours are one state block.
+constexpr int kStateBlock = 256;
+constexpr int kFlatElems = 2048;
+constexpr int kFlatQuads = kFlatElems / (4 * kBlock);
+static_assert(kStateBlock == 4 * kWave, "a wave's fours are one state block");
+
+struct FlatItem {
+    int64_t base;      // arena element of the item's first element (a multiple of 4)
+    int64_t block0;    // state block of the item's first element
+    int32_t n;         // elements
+    int32_t layer;
+};
+static_assert(sizeof(FlatItem) == 24, "FlatItem layout");
+
+typedef __bf16 v4bf __attribute__((ext_vector_type(4)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+
+template <int T> struct ElemOf { typedef float type; typedef v4f vec; };
+template <> struct ElemOf<HSADMM_TYPE_BF16> { typedef __bf16 type; typedef v4bf vec; };
+template <> struct ElemOf<HSADMM_TYPE_F16> { typedef _Float16 type; typedef v4h vec; };
+
+// Four elements of type T at p as fp32, the first nv of them (1 to 4; the others are 0).
+template <int T>
+__device__ __forceinline__ v4f load4(const typename ElemOf<T>::type* p, int nv)
+{
+    if (nv == 4)
+        return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const typename ElemOf<T>::vec*>(p)), v4f);
+    v4f v = {0.f, 0.f, 0.f, 0.f};
+    if (nv > 0) v.x = (float)p[0];
+    if (nv > 1) v.y = (float)p[1];
+    if (nv > 2) v.z = (float)p[2];
+    return v;
+}
+
+// The first nv of four values to p, rounded to nearest.
+template <int T>
+__device__ __forceinline__ void store4(typename ElemOf<T>::type* p, const v4f& v, int nv)
+{
+    typedef typename ElemOf<T>::type E;
+    if (nv == 4) {
+        __builtin_nontemporal_store(__builtin_convertvector(v, typename ElemOf<T>::vec),
+                                    reinterpret_cast<typename ElemOf<T>::vec*>(p));
+        return;
+    }
+    if (nv > 0) p[0] = (E)v.x;
+    if (nv > 1) p[1] = (E)v.y;
+    if (nv > 2) p[2] = (E)v.z;
+}
+
+// ------------------------------------------------------------------ gradient norms
+
+struct GradArgs { const void* G[HSADMM_MAX_REPLICAS]; };
+
+// Sums of squares in fp64 (the square of an fp32 value is exact there): workgroup p of a replica's P takes the flat items
+// p, p + P, ...; the order of the additions depends on the plan and the number of replicas only.
+template <int T>
+__global__ __launch_bounds__(kBlock) void gradient_sqsums(const FlatItem* __restrict__ items, int n_items, GradArgs a, int P,
+                                                          double* __restrict__ part)
+{
+    __shared__ double red[kWaves];
+    const int r = blockIdx.x / P, p = blockIdx.x - r * P;
+    const typename ElemOf<T>::type* G = static_cast<const typename ElemOf<T>::type*>(a.G[r]);
+    double s0 = 0.0, s1 = 0.0, s2 = 0.0, s3 = 0.0;
+    for (int i = p; i < n_items; i += P) {
+        const FlatItem it = items[i];
+        v4f g[kFlatQuads];
+#pragma unroll
+        for (int k = 0; k < kFlatQuads; ++k) {
+            const int q = 4 * (threadIdx.x + k * kBlock);
+            g[k] = load4<T>(G + it.base + q, min(4, it.n - q));
+        }
+#pragma unroll
+        for (int k = 0; k < kFlatQuads; ++k) {
+            s0 = fma((double)g[k].x, (double)g[k].x, s0);
+            s1 = fma((double)g[k].y, (double)g[k].y, s1);
+            s2 = fma((double)g[k].z, (double)g[k].z, s2);
+            s3 = fma((double)g[k].w, (double)g[k].w, s3);
+        }
+    }
+    const double s = wave_xor_sum((s0 + s1) + (s2 + s3), kWave);
+    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = red[0];
+        for (int w = 1; w < kWaves; ++w) t += red[w];
+        part[blockIdx.x] = t;
+    }
+}
+
+// One workgroup per replica: norm = sqrt(sum), scale = min(1, max_norm / norm), NaN where the norm is not finite.
+__global__ __launch_bounds__(kBlock) void gradient_norm_finish(const double* __restrict__ part, int P, double max_norm,
+                                                               double* __restrict__ norm, float* __restrict__ scale)
+{
+    __shared__ double red[kWaves];
+    double s = 0.0;
+    for (int i = threadIdx.x; i < P; i += kBlock) s += part[(int64_t)blockIdx.x * P + i];
+    s = wave_xor_sum(s, kWave);
+    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        double t = red[0];
+        for (int w = 1; w < kWaves; ++w) t += red[w];
+        t = sqrt(t);
+        if (norm) norm[blockIdx.x] = t;
+        if (scale) {
+            const bool finite = t <= 1.7976931348623157e308;          // (a NaN fails the comparison)
+            scale[blockIdx.x] = !finite ? __builtin_nanf("") : t > max_norm ? (float)(max_norm / t) : 1.0f;
+        }
+    }
+}
+
+// ------------------------------------------------------------------ AdamW
+
+struct AdamwArgs {
+    float* W[HSADMM_MAX_REPLICAS];
+    const void* G[HSADMM_MAX_REPLICAS];
+    void* M[HSADMM_MAX_REPLICAS];          // fp32, or e4m3 codes with the scales Ms
+    void* V[HSADMM_MAX_REPLICAS];          // fp32 second moments, or codes of their roots with the scales Vs
+    float* Ms[HSADMM_MAX_REPLICAS];
+    float* Vs[HSADMM_MAX_REPLICAS];
+    void* Wl[HSADMM_MAX_REPLICAS];         // LOW: the weights rounded to the gradients' type
+    const float* Z;                        // PROX: z_i, the replica-mean dual, rho_1 per layer
+    const float* U;
+    const float* rho;
+    const float* grad_scale;               // may be null
+    const hsadmm_adamw_coef_t* coef_dev;   // may be null: coef
+    hsadmm_adamw_coef_t coef;
+    float beta1, one_minus_beta1, beta2, one_minus_beta2, eps;
+};
+
+// Largest of the wave's values, in every lane: four exchanges inside the rows of 16 lanes, then the four rows.
+__device__ __forceinline__ unsigned int wave_umax(unsigned int x)
+{
+    x = max(x, row_exchange<kDppXor1>(x));
+    x = max(x, row_exchange<kDppXor2>(x));
+    x = max(x, row_exchange<kDppHalfMirror>(x));
+    x = max(x, row_exchange<kDppMirror>(x));
+    return max(max(lane_value(x, 0), lane_value(x, 16)), max(lane_value(x, 32), lane_value(x, 48)));
+}
+
+// The four values of a lane's four, from codes and the block's scale.
+__device__ __forceinline__ v4f decode4(unsigned int codes, float scale)
+{
+    const v2f lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes, true);
+    const v4f v = {lo.x, lo.y, hi.x, hi.y};
+    return v * scale;
+}
+
+// Rounding numbers of a four: 32 bits each, of which the conversion uses the upper 20.  One mix per four (two
+// multiplications by odd numbers, two shifts), then a multiplication by an odd number of each element's own: neighbours'
+// numbers need not be independent of each other, an element's numbers of different steps do.
+constexpr unsigned int kMix1 = 0x6A09E667u, kMix2 = 0xBB67AE85u, kMix3 = 0x3C6EF373u;
+__device__ __forceinline__ unsigned int mix_four(unsigned int x)
+{
+    x *= kMix1;
+    x = (x ^ (x >> 16)) * kMix2;
+    return x ^ (x >> 15);
+}
+
+// Codes of four values y (already in units of the scale): rounded stochastically to e4m3, |y| <= 448.
+__device__ __forceinline__ unsigned int encode4(const v4f& y, unsigned int mix)
+{
+    int c = 0;
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(y.x, (int)mix, c, 0);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(y.y, (int)(mix * kMix1), c, 1);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(y.z, (int)(mix * kMix2), c, 2);
+    c = __builtin_amdgcn_cvt_sr_fp8_f32(y.w, (int)(mix * kMix3), c, 3);
+    return (unsigned int)c;
+}
+
+__device__ __forceinline__ unsigned int load_codes(const uint8_t* p, int nv)
+{
+    if (nv == 4) return __builtin_nontemporal_load(reinterpret_cast<const unsigned int*>(p));
+    unsigned int c = 0;
+    for (int i = 0; i < 3; ++i)
+        if (i < nv) c |= (unsigned int)p[i] << (8 * i);
+    return c;
+}
+
+__device__ __forceinline__ void store_codes(uint8_t* p, unsigned int c, int nv)
+{
+    if (nv == 4) { __builtin_nontemporal_store(c, reinterpret_cast<unsigned int*>(p)); return; }
+    for (int i = 0; i < 3; ++i)
+        if (i < nv) p[i] = (uint8_t)(c >> (8 * i));
+}
+
+// A block whose largest magnitude is below this is held as zero: its reciprocal would leave fp32's normal range.
+constexpr float kStateFloor = 0x1p-100f;
+
+// A block's scale (largest magnitude / 448) and what brings its values into units of it.  `top`: the bits of the largest
+// magnitude; the bits of a NaN or an infinity are larger than any number's, so such a block's scale is not finite.
+__device__ __forceinline__ float block_scale(unsigned int top, float& to_units)
+{
+    const float t = __uint_as_float(top);
+    const bool none = t < kStateFloor;
+    const float r = __builtin_amdgcn_rcpf(t);
+    to_units = none ? 0.f : __builtin_fmaf(__builtin_fmaf(-t, r, 1.0f), r, r) * 448.0f;
+    return none ? 0.f : t * (1.0f / 448.0f);
+}
+
+__device__ __forceinline__ unsigned int top_bits(const v4f& v)
+{
+    const unsigned int m = 0x7fffffffu;
+    return max(max(__float_as_uint(v.x) & m, __float_as_uint(v.y) & m), max(__float_as_uint(v.z) & m, __float_as_uint(v.w) & m));
+}
+
+// The root of x >= 0 to nearest, but for about one value in a million that lies next to the middle of two: the machine's
+// reciprocal root and one correction of x times it.  (Codes are cut from the root and the moments: a result that differs by
+// one unit in the last place from the operation's own rounding moves a code in every millionth case, this one hardly ever.)
+__device__ __forceinline__ float root_of(float x)
+{
+    const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f));
+    const float s = x * y;
+    return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+}
+
+// Formulas: see hsadmm_adamw in the header.  Moments are formed in fp32, every operation rounded by itself; the weights' last
+// two operations are fused and the reciprocal before them is the machine's own, within one unit in the last place.
+template <int T, bool S8, bool PROX, bool LOW, bool FULL>
+__device__ __forceinline__ void adamw_item(const FlatItem& it, const AdamwArgs& a, int R)
+{
+    typedef typename ElemOf<T>::type E;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x & (kWave - 1);
+    const hsadmm_adamw_coef_t co = a.coef_dev ? *a.coef_dev : a.coef;
+    int nv[kFlatQuads];
+    int64_t at[kFlatQuads];
+    v4f z[kFlatQuads], u[kFlatQuads];
+#pragma unroll
+    for (int k = 0; k < kFlatQuads; ++k) {
+        const int q = 4 * (threadIdx.x + k * kBlock);
+        nv[k] = FULL ? 4 : min(4, it.n - q);
+        at[k] = it.base + q;
+        if (PROX) { z[k] = load4<HSADMM_TYPE_F32>(a.Z + at[k], nv[k]); u[k] = load4<HSADMM_TYPE_F32>(a.U + at[k], nv[k]); }
+    }
+    const float rho = PROX ? a.rho[it.layer] : 0.f;
+    for (int r = 0; r < R; ++r) {
+        const float s = a.grad_scale ? a.grad_scale[r] : 1.0f;
+        if (!(__builtin_fabsf(s) < __builtin_inff())) continue;      // a gradient that is not finite: no step
+        float* W = a.W[r];
+        const E* G = static_cast<const E*>(a.G[r]);
+        v4f w[kFlatQuads], g[kFlatQuads], m[kFlatQuads], v[kFlatQuads];
+        unsigned int mc[kFlatQuads], vc[kFlatQuads];
+        float ms[kFlatQuads], vs[kFlatQuads];
+#pragma unroll
+        for (int k = 0; k < kFlatQuads; ++k) {
+            w[k] = load4<HSADMM_TYPE_F32>(W + at[k], nv[k]);
+            g[k] = load4<T>(G + at[k], nv[k]);
+            if (S8) {
+                const bool on = FULL || it.n > (wave + k * kWaves) * kStateBlock;
+                const int64_t b = it.block0 + wave + k * kWaves;
+                mc[k] = load_codes(static_cast<const uint8_t*>(a.M[r]) + at[k], nv[k]);
+                vc[k] = load_codes(static_cast<const uint8_t*>(a.V[r]) + at[k], nv[k]);
+                ms[k] = on ? a.Ms[r][b] : 0.f;
+                vs[k] = on ? a.Vs[r][b] : 0.f;
+            } else {
+                m[k] = load4<HSADMM_TYPE_F32>(static_cast<const float*>(a.M[r]) + at[k], nv[k]);
+                v[k] = load4<HSADMM_TYPE_F32>(static_cast<const float*>(a.V[r]) + at[k], nv[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kFlatQuads; ++k) {
+            if (S8) {
+                m[k] = decode4(mc[k], ms[k]);
+                const v4f q = decode4(vc[k], vs[k]);
+                v[k] = q * q;
+            }
+            v4f rt;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float gi = g[k][i] * s;
+                if (PROX) gi = gi + rho * ((w[k][i] - z[k][i]) + u[k][i]);
+                m[k][i] = a.beta1 * m[k][i] + a.one_minus_beta1 * gi;
+                v[k][i] = a.beta2 * v[k][i] + a.one_minus_beta2 * (gi * gi);
+                rt[i] = root_of(v[k][i]);
+                const float t = m[k][i] * __builtin_amdgcn_rcpf(__builtin_fmaf(rt[i], co.root, a.eps));
+                w[k][i] = __builtin_fmaf(-co.step_size, t, w[k][i] * co.decay);
+            }
+            store4<HSADMM_TYPE_F32>(W + at[k], w[k], nv[k]);
+            if (LOW) store4<T>(static_cast<E*>(a.Wl[r]) + at[k], w[k], nv[k]);
+            if (!S8) {
+                store4<HSADMM_TYPE_F32>(static_cast<float*>(a.M[r]) + at[k], m[k], nv[k]);
+                store4<HSADMM_TYPE_F32>(static_cast<float*>(a.V[r]) + at[k], v[k], nv[k]);
+            } else {
+                if (!FULL) {
+                    // (values past the end of the layer count for nothing)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i >= nv[k]) m[k][i] = rt[i] = 0.f;
+                }
+                const unsigned int mt = wave_umax(top_bits(m[k])), vt = wave_umax(top_bits(rt));
+                float mu, vu;
+                const float mscale = block_scale(mt, mu), vscale = block_scale(vt, vu);
+                const int64_t four = at[k] >> 2;
+                const unsigned int mix = mix_four((unsigned int)four + (unsigned int)(four >> 32) * kMix3 + co.noise +
+                                                  (unsigned int)r * kMix3);
+                v4f ym = m[k] * mu, yv = rt * vu;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    ym[i] = __builtin_amdgcn_fmed3f(ym[i], -448.0f, 448.0f);
+                    // a root that is not zero keeps a code that is not: a zero would divide by eps alone
+                    yv[i] = yv[i] > 0.f ? __builtin_amdgcn_fmed3f(yv[i], 0x1p-9f, 448.0f) : 0.f;
+                }
+                store_codes(static_cast<uint8_t*>(a.M[r]) + at[k], encode4(ym, mix), nv[k]);
+                store_codes(static_cast<uint8_t*>(a.V[r]) + at[k], encode4(yv, mix), nv[k]);
+                const int64_t b = it.block0 + wave + k * kWaves;
+                if (lane == 0 && (FULL || it.n > (wave + k * kWaves) * kStateBlock)) {
+                    a.Ms[r][b] = mscale;
+                    a.Vs[r][b] = vscale;
+                }
+            }
+        }
+    }
+}
+
+template <int T, bool S8, bool PROX, bool LOW>
+__global__ __launch_bounds__(kBlock) void adamw_kernel(const FlatItem* __restrict__ items, AdamwArgs a, int R)
+{
+    const FlatItem it = items[blockIdx.x];
+    if (it.n == kFlatElems) adamw_item<T, S8, PROX, LOW, true>(it, a, R);
+    else adamw_item<T, S8, PROX, LOW, false>(it, a, R);
+}
+
+}  // namespace
+#endif

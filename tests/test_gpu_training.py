@@ -1,0 +1,554 @@
+"""hsadmm_gradient_norms and hsadmm_adamw against the same formulas in 64 bits (numpy, written here from the header's text).
+
+Tolerances.  Every fp32 operation of the update rounds by at most e = 2^-24 relative to its result (a fused multiply-add
+once), the root and the reciprocal by 2^-23 = 2 e at most, a constant that was rounded to fp32 by e.  `reference` below adds
+these up along the formulas, per element; a factor of 1.01 covers the terms of second order."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_14628_amd as pkg
+import workloads as wk
+from tests.ref_e4m3 import E4M3, grid_step, rounding_numbers, round_down_on_grid
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+TYPES = {pkg.TYPE_F32: torch.float32, pkg.TYPE_BF16: torch.bfloat16, pkg.TYPE_F16: torch.float16}
+# layers of one to a few thousand elements: single elements, ends inside a four, inside a state block, inside an item
+SHAPES = [(1, 1, 1), (1, 2, 1), (3, 1, 1), (5, 51, 1), (16, 16, 1), (1, 257, 1), (23, 89, 1), (32, 64, 1), (3, 683, 1),
+          (31, 15, 9), (64, 33, 9), (2, 4097, 1)]
+DEV = "cuda:0"
+
+
+def workload(shapes=SHAPES, R=1, seed=0):
+    wl = wk.custom_workload([(co, ci, khw, wk.MODE_FILTER, max(1, co // 2)) for co, ci, khw in shapes], R=R, seed=seed)
+    wl.n_arena += -wl.n_arena % 64                            # (replicas are rows of one tensor: each row aligned)
+    return wl
+
+
+def inside(wl):
+    m = np.zeros(wl.n_arena, bool)
+    for l in wl.layers:
+        m[l.elem_off:l.elem_off + l.n] = True
+    return m
+
+
+def per_layer(wl, values):
+    out = np.zeros(wl.n_arena)
+    for l, v in zip(wl.layers, values):
+        out[l.elem_off:l.elem_off + l.n] = v
+    return out
+
+
+def dev(x, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+    return t if dtype is None else t.to(dtype)
+
+
+def host(t):
+    return t.detach().cpu().float().double().numpy() if t.dtype != torch.float64 else t.cpu().numpy()
+
+
+class Run:
+    """Random inputs of a training step, on the device and as float64 on the host.  Arena padding holds NaN."""
+
+    def __init__(self, wl, R, grad_type, seed=0, prox=True, spread=1.0):
+        rng = np.random.default_rng(seed)
+        n, self.wl, self.R, self.on = wl.n_arena, wl, R, inside(wl)
+        nan = ~self.on
+
+        def arena(x, dtype=torch.float32):
+            x = np.array(x, np.float32)
+            x[..., nan] = np.nan
+            return dev(x, dtype)
+
+        scale = per_layer(wl, 10.0 ** rng.uniform(-2, 0, len(wl.layers)) * spread)
+        self.G = arena(rng.standard_normal((R, n)) * scale * 0.1, TYPES[grad_type])
+        self.W = arena(rng.standard_normal((R, n)) * 0.1)
+        self.M = arena(rng.standard_normal((R, n)) * scale * 0.03)
+        self.V = arena((rng.standard_normal((R, n)) * scale * 0.1) ** 2)
+        self.Z = arena(rng.standard_normal(n) * 0.1) if prox else None
+        self.U = arena(rng.standard_normal(n) * 0.01) if prox else None
+        self.rho = dev(rng.uniform(1e-3, 1.0, len(wl.layers)).astype(np.float32)) if prox else None
+        self.scale = dev(rng.uniform(0.3, 1.0, R).astype(np.float32))
+        self.hyper = dict(lr=3e-3, beta_one=0.9, beta_two=0.99, eps=1e-8, weight_decay=0.02, step=7)
+        self.grad_type = grad_type
+        self.low = None
+
+    def fields(self):
+        f = dict(grad_type=self.grad_type, grad_scale=self.scale, **self.hyper)
+        if self.Z is not None:
+            f.update(Z=self.Z, U=self.U, rho=self.rho)
+        return f
+
+    def reference(self, M=None, V=None):
+        """W, M, V after the step in float64, the roots, and a bound on the fp32 error of each."""
+        h, on = self.hyper, self.on
+        W, G = host(self.W)[:, on], host(self.G)[:, on]
+        m = host(self.M)[:, on] if M is None else M[:, on]
+        v = host(self.V)[:, on] if V is None else V[:, on]
+        s = host(self.scale)[:, None]
+        g = s * G
+        eg = E * np.abs(g)
+        if self.Z is not None:
+            rho = per_layer(self.wl, host(self.rho))[on]
+            d = W - host(self.Z)[on]
+            p = d + host(self.U)[on]
+            ep = E * (np.abs(d) + np.abs(p))
+            g = g + rho * p
+            eg = eg + rho * ep + E * rho * np.abs(p) + E * np.abs(g)
+        b1, b2 = h["beta_one"], h["beta_two"]
+        m2 = b1 * m + (1 - b1) * g
+        em = (1 - b1) * eg + E * (2 * b1 * np.abs(m) + 2 * (1 - b1) * np.abs(g) + np.abs(m2))
+        v2 = b2 * v + (1 - b2) * g * g
+        ev = (1 - b2) * 2 * np.abs(g) * eg + E * (2 * b2 * v + 3 * (1 - b2) * g * g + v2)
+        r = np.sqrt(v2)
+        er = np.where(r > 0, ev / np.maximum(r, 1e-300), 0) + 2 * E * r         # (halved for small ev; doubled to be sure)
+        root = 1 / math.sqrt(1 - b2 ** h["step"])
+        den = r * root + h["eps"]
+        eden = er * root + E * r * root + E * h["eps"] + E * den
+        t = m2 / den
+        et = em / den + np.abs(t) * (eden / den + 3 * E)
+        a, decay = h["lr"] / (1 - b1 ** h["step"]), 1 - h["lr"] * h["weight_decay"]
+        W2 = W * decay - a * t
+        eW = 2 * E * np.abs(W * decay) + a * (et + E * np.abs(t)) + E * np.abs(W2)
+        return dict(W=W2, M=m2, V=v2, r=r), dict(W=1.01 * eW, M=1.01 * em, V=1.01 * ev, r=1.01 * er)
+
+
+def check_close(name, got, want, tol, floor=2.0 ** -126):
+    bad = np.abs(got - want) > tol + floor
+    assert not bad.any(), (name, int(bad.sum()), float(np.max(np.abs(got - want) / (tol + floor))))
+
+
+def padding_untouched(run, before):
+    """Arena padding keeps its bits."""
+    for name, old in before.items():
+        new = getattr(run, name)
+        a = old[..., ~torch.from_numpy(run.on).to(DEV)].contiguous().view(torch.uint8)
+        b = new[..., ~torch.from_numpy(run.on).to(DEV)].contiguous().view(torch.uint8)
+        assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("prox", [False, True])
+@pytest.mark.parametrize("grad_type", [pkg.TYPE_F32, pkg.TYPE_BF16, pkg.TYPE_F16])
+@pytest.mark.parametrize("R", [1, 3, 16])
+def test_update_with_32_bit_states(R, grad_type, prox):
+    wl = workload()
+    run = Run(wl, R, grad_type, seed=R + 10 * grad_type, prox=prox)
+    plan = pkg.Plan(wl.table())
+    low = None if grad_type == pkg.TYPE_F32 else torch.full_like(run.G, 7.0)
+    run.low = low
+    want, tol = run.reference()
+    before = {k: getattr(run, k).clone() for k in ("W", "M", "V") + (("low",) if low is not None else ())}
+    pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V),
+                     W_low=None if low is None else list(low), **run.fields())
+    for name in ("W", "M", "V"):
+        check_close(name, host(getattr(run, name))[:, run.on], want[name], tol[name])
+    padding_untouched(run, before)
+    if low is not None:
+        on = torch.from_numpy(run.on).to(DEV)
+        assert torch.equal(low[:, on].view(torch.int16), run.W[:, on].to(low.dtype).view(torch.int16))
+    plan.close()
+
+
+def eight(run, plan, seed, fresh=False):
+    """8-bit states for a run: codes [R, n] and scales [R, blocks], random or zero; what they stand for as float64."""
+    R, n, nb = run.R, run.wl.n_arena, pkg.hsadmm_plan_state_blocks(plan)
+    rng = np.random.default_rng(seed)
+    block = np.full(n, -1)
+    at = 0
+    for l in run.wl.layers:
+        block[l.elem_off:l.elem_off + l.n] = at + np.arange(l.n) // 256
+        at += -(-l.n // 256)
+    assert at == nb
+    mc = np.zeros((R, n), np.uint8) if fresh else rng.integers(0, 127, (R, n)).astype(np.uint8) | (
+        rng.integers(0, 2, (R, n)) << 7).astype(np.uint8)
+    vc = np.zeros((R, n), np.uint8) if fresh else rng.integers(0, 127, (R, n)).astype(np.uint8)
+    ms = np.zeros((R, nb), np.float32) if fresh else (10.0 ** rng.uniform(-7, -3, (R, nb))).astype(np.float32)
+    vs = np.zeros((R, nb), np.float32) if fresh else (10.0 ** rng.uniform(-6, -3, (R, nb))).astype(np.float32)
+    run.M, run.V, run.Ms, run.Vs = dev(mc), dev(vc), dev(ms), dev(vs)
+    run.block = block
+    return E4M3[mc] * ms[:, block], (E4M3[vc] * vs[:, block].astype(np.float64)) ** 2
+
+
+def check_codes(name, run, codes, scales, exact, tol, u, keep_alive):
+    """Codes and scales of float64 values `exact` (known to `tol`): the scale from the block's largest, every code one that
+    the rounding formula gives for some value within the tolerance."""
+    on, R = run.on, run.R
+    nb = scales.shape[1]
+    codes, scales = codes.cpu().numpy()[:, on], host(scales)
+    blk = run.block[on]
+    for r in range(R):
+        top = np.zeros(nb)
+        np.maximum.at(top, blk, np.abs(exact[r]))
+        top_tol = np.zeros(nb)
+        np.maximum.at(top_tol, blk, tol[r])
+        check_close(name + " scale", scales[r], top / 448, (top_tol + 3 * E * top) / 448)
+        # y = |x| * (448 / top): the quotient and the product round, the reciprocal by 2 E
+        rel = tol[r] / np.maximum(np.abs(exact[r]), 1e-300) + top_tol[blk] / np.maximum(top[blk], 1e-300) + 5 * E
+        y = np.abs(exact[r]) * np.where(top[blk] > 0, 448 / np.maximum(top[blk], 1e-300), 0)
+        got = np.abs(E4M3[codes[r]])
+        lo = round_down_on_grid(np.minimum(y * (1 - rel), 448), u[r][on])
+        hi = round_down_on_grid(np.minimum(y * (1 + rel), 448), u[r][on])
+        if keep_alive:
+            lo, hi = (np.where(y > 0, np.maximum(q, 2.0 ** -9), q) for q in (lo, hi))
+        bad = (got != lo) & (got != hi)
+        assert not bad.any(), (name, r, int(bad.sum()), y[bad][:4], got[bad][:4], lo[bad][:4])
+        assert (lo == hi).mean() > 0.9                       # (few codes are in doubt)
+        sign = (codes[r] >> 7) != 0
+        assert np.array_equal(sign[got > 0], (exact[r] < 0)[got > 0]), name
+
+
+@pytest.mark.parametrize("fresh", [False, True])
+@pytest.mark.parametrize("R,grad_type,prox", [(1, pkg.TYPE_F32, False), (3, pkg.TYPE_BF16, True), (16, pkg.TYPE_F16, True),
+                                              (2, pkg.TYPE_F32, True)])
+def test_update_with_8_bit_states(R, grad_type, prox, fresh):
+    wl = workload()
+    run = Run(wl, R, grad_type, seed=5 * R + grad_type, prox=prox)
+    plan = pkg.Plan(wl.table())
+    M, V = eight(run, plan, seed=R, fresh=fresh)
+    low = None if grad_type == pkg.TYPE_F32 else torch.full_like(run.G, 7.0)
+    # (a decoded moment rounds once, the square of a root twice: in the terms `reference` counts with these factors)
+    want, tol = run.reference(M, V)
+    h = run.hyper
+    em = tol["M"] + 1.01 * E * h["beta_one"] * np.abs(M[:, run.on])
+    ev = tol["V"] + 1.01 * 3 * E * h["beta_two"] * V[:, run.on]
+    er = np.where(want["r"] > 0, ev / np.maximum(want["r"], 1e-300), 0) + 2 * E * want["r"]
+    before = {k: getattr(run, k).clone() for k in ("W", "M", "V")}
+    noise = 0xDEADBEEF
+    pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), state_bits=8, M_scale=list(run.Ms),
+                     V_scale=list(run.Vs), W_low=None if low is None else list(low), noise=noise, **run.fields())
+    a = h["lr"] / (1 - h["beta_one"] ** h["step"])
+    den = want["r"] / math.sqrt(1 - h["beta_two"] ** h["step"]) + h["eps"]
+    more = a / den * (em - tol["M"]) + a * np.abs(want["M"]) / den * (3 * E * 2)
+    check_close("W", host(run.W)[:, run.on], want["W"], tol["W"] + 1.01 * more)
+    u = rounding_numbers(wl.n_arena, R, noise)
+    check_codes("M", run, run.M, run.Ms, want["M"], em, u, False)
+    check_codes("V", run, run.V, run.Vs, want["r"], er, u, True)
+    padding_untouched(run, before)
+    if low is not None:
+        on = torch.from_numpy(run.on).to(DEV)
+        assert torch.equal(low[:, on].view(torch.int16), run.W[:, on].to(low.dtype).view(torch.int16))
+    plan.close()
+
+
+def test_the_same_call_gives_the_same_bits_and_other_noise_other_codes():
+    wl = workload()
+    results = []
+    for noise in (5, 5, 6):
+        run = Run(wl, 2, pkg.TYPE_F32, seed=1)
+        plan = pkg.Plan(wl.table())
+        eight(run, plan, seed=1)
+        pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), state_bits=8, M_scale=list(run.Ms),
+                         V_scale=list(run.Vs), noise=noise, **run.fields())
+        results.append([t.cpu().numpy().view(np.uint8).copy() for t in (run.W, run.M, run.V, run.Ms, run.Vs)])
+        plan.close()
+    assert all(np.array_equal(x, y) for x, y in zip(results[0], results[1]))
+    for i in (0, 3, 4):                                       # weights and scales do not depend on the noise
+        assert np.array_equal(results[0][i], results[2][i])
+    assert (results[0][1] != results[2][1]).mean() > 0.1
+
+
+def test_roots_decay_on_average_though_a_step_is_far_below_a_code():
+    """Without a gradient a root shrinks by sqrt(beta_2) a step, one part in 2000 where a code is one in 8 to 16: to nearest
+    it would not move.  The expectation is exact; an element's own standard deviation after 600 steps is below 0.35 (a step's
+    variance is at most (r / 8)^2 p, p = 0.0005 * 16), the mean over 65536 of them below 0.0014; 1 % is allowed."""
+    wl = workload([(64, 1024, 1)])
+    plan = pkg.Plan(wl.table())
+    n, nb = wl.n_arena, pkg.hsadmm_plan_state_blocks(plan)
+    rng = np.random.default_rng(0)
+    code = rng.integers(40, 120, n).astype(np.uint8)
+    V, Vs = dev(code), dev(np.ones(nb, np.float32))
+    M, Ms = torch.zeros_like(V), torch.zeros_like(Vs)
+    W, G = torch.zeros(n, device=DEV), torch.zeros(n, device=DEV)
+    for t in range(600):
+        pkg.hsadmm_adamw(plan, [W], [G], [M], [V], state_bits=8, M_scale=[Ms], V_scale=[Vs], lr=1e-3, step=t + 1,
+                         noise=(t * 0x9E3779B9) & 0xFFFFFFFF)
+    got = E4M3[V.cpu().numpy()] * np.repeat(host(Vs), 256)[:n]
+    ratio = got.sum() / E4M3[code].sum()
+    assert abs(ratio / 0.999 ** 300 - 1) < 0.01, ratio
+    assert (got > 0).all() and float(W.abs().max()) == 0.0
+    plan.close()
+
+
+def test_zero_states_stay_zero_and_roots_that_are_not_zero_stay_alive():
+    wl = workload([(1, 300, 1)])
+    plan = pkg.Plan(wl.table())
+    g = np.zeros(wl.n_arena, np.float32)
+    g[0], g[1] = 1.0, 1e-9                                    # the second is 2^-30 of the block's largest
+    W, G = torch.zeros(wl.n_arena, device=DEV), dev(g)
+    M, V = (torch.zeros(wl.n_arena, dtype=torch.uint8, device=DEV) for _ in range(2))
+    Ms, Vs = (torch.zeros(2, device=DEV) for _ in range(2))
+    pkg.hsadmm_adamw(plan, [W], [G], [M], [V], state_bits=8, M_scale=[Ms], V_scale=[Vs], lr=1e-3, noise=3)
+    v = V.cpu().numpy()
+    assert v[0] == 126 and v[1] == 1 and not v[2:].any()
+    assert float(Vs[1]) == 0.0 and float(Ms[1]) == 0.0         # the second block saw nothing
+    assert not np.isnan(host(W)).any()
+    plan.close()
+
+
+def test_a_block_with_a_value_that_is_not_finite_shows_it():
+    wl = workload([(4, 256, 1)])
+    plan = pkg.Plan(wl.table())
+    for bad in (float("nan"), float("inf")):
+        run = Run(wl, 1, pkg.TYPE_F32, seed=3, prox=False)
+        eight(run, plan, seed=3)
+        run.G[0, 300] = bad
+        pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), state_bits=8, M_scale=list(run.Ms),
+                         V_scale=list(run.Vs), **run.fields())
+        ms, vs = host(run.Ms)[0], host(run.Vs)[0]
+        assert not np.isfinite(ms[1]) and not np.isfinite(vs[1])
+        assert np.isfinite(ms[[0, 2, 3]]).all() and np.isfinite(vs[[0, 2, 3]]).all()
+    plan.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_replica_whose_scale_is_not_finite_is_left_as_it_is(bits):
+    wl = workload()
+    plan = pkg.Plan(wl.table())
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        run = Run(wl, 3, pkg.TYPE_BF16, seed=2)
+        if bits == 8:
+            eight(run, plan, seed=2)
+        run.scale[1] = bad
+        run.G[1] = float("nan")
+        low = torch.full_like(run.G, 7.0)
+        names = ["W", "M", "V"] + (["Ms", "Vs"] if bits == 8 else [])
+        before = {k: getattr(run, k).clone() for k in names}
+        more = dict(M_scale=list(run.Ms), V_scale=list(run.Vs)) if bits == 8 else {}
+        pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), W_low=list(low), state_bits=bits,
+                         **more, **run.fields())
+        for k in names:
+            a, b = before[k], getattr(run, k)
+            assert torch.equal(a[1].view(torch.uint8), b[1].view(torch.uint8)), k
+            assert not torch.equal(a[0].view(torch.uint8), b[0].view(torch.uint8)), k
+            assert not torch.equal(a[2].view(torch.uint8), b[2].view(torch.uint8)), k
+        assert (low[1] == 7.0).all()
+    plan.close()
+
+
+def test_the_pull_is_the_gradient_of_the_proximal_term_by_differences():
+    """With beta_1 = 0 and no loss gradient the first moment is the gradient of rho/2 |W - Z + U|^2; against central
+    differences in 64 bits (exact for a square) of the term as it is written."""
+    wl = workload([(5, 51, 1)])
+    run = Run(wl, 1, pkg.TYPE_F32, seed=4)
+    run.G.zero_()
+    run.hyper["beta_one"] = 0.0
+    plan = pkg.Plan(wl.table())
+    W, Z, U, rho = host(run.W)[0][run.on], host(run.Z)[run.on], host(run.U)[run.on], float(run.rho[0])
+    term = lambda w: 0.5 * rho * (w - Z + U) ** 2                       # noqa: E731  (a sum of these: a term per element)
+    step = 0.5
+    diff = (term(W + step) - term(W - step)) / (2 * step)
+    pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), **run.fields())
+    # two roundings of the difference and the sum, three of the products; 1e-13 for the differences
+    tol = 5 * E * rho * (np.abs(W - Z) + np.abs(W - Z + U)) + 1e-13
+    check_close("pull", host(run.M)[0][run.on], diff, tol)
+    plan.close()
+
+
+def test_coefficients_on_the_device_follow_a_captured_graph():
+    """A graph of norms and update, replayed with the coefficients changed in between, against eager calls; eager work on
+    the same buffers' copies lies between the replays."""
+    wl = workload(R=2)
+    a, b = Run(wl, 2, pkg.TYPE_BF16, seed=8), Run(wl, 2, pkg.TYPE_BF16, seed=8)
+    plan = pkg.Plan(wl.table())
+    for run in (a, b):
+        eight(run, plan, seed=8)
+        run.ws = torch.zeros(plan.workspace_bytes, dtype=torch.uint8, device=DEV)
+    coef = torch.zeros(4, device=DEV)
+
+    def put(t):
+        d, s, r, noise = pkg.hsadmm_adamw_coefficients(1e-3 * t, 0.9, 0.99, 0.02, t, 77 * t)
+        values = np.array([d, s, r, 0], np.float32)
+        values.view(np.uint32)[3] = noise
+        coef.copy_(dev(values))
+
+    def step(run, **how):
+        pkg.hsadmm_gradient_norms(plan, list(run.G), 0.5, None, run.scale, run.ws, grad_type=pkg.TYPE_BF16)
+        pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), state_bits=8, M_scale=list(run.Ms),
+                         V_scale=list(run.Vs), grad_type=pkg.TYPE_BF16, grad_scale=run.scale, Z=run.Z, U=run.U, rho=run.rho,
+                         beta_two=0.99, **how)
+
+    put(1)
+    stream = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        step(a, coef=coef)
+    for t in range(1, 5):
+        put(t)
+        torch.cuda.synchronize()
+        graph.replay()
+        step(b, lr=1e-3 * t, weight_decay=0.02, step=t, noise=77 * t)
+        torch.cuda.synchronize()
+        for k in ("W", "M", "V", "Ms", "Vs"):
+            assert torch.equal(getattr(a, k).view(torch.uint8), getattr(b, k).view(torch.uint8)), (t, k)
+        assert torch.equal(a.scale, b.scale)
+    plan.close()
+
+
+def test_replicas_may_share_a_gradient_and_a_step_runs_on_any_stream():
+    wl = workload()
+    a, b = Run(wl, 2, pkg.TYPE_F32, seed=6), Run(wl, 2, pkg.TYPE_F32, seed=6)
+    plan = pkg.Plan(wl.table())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    pkg.hsadmm_adamw(plan, list(a.W), [a.G[0], a.G[0]], list(a.M), list(a.V), stream=side, **a.fields())
+    side.synchronize()
+    b.G[1] = b.G[0]
+    pkg.hsadmm_adamw(plan, list(b.W), list(b.G), list(b.M), list(b.V), **b.fields())
+    torch.cuda.synchronize()
+    for k in ("W", "M", "V"):
+        assert torch.equal(getattr(a, k).view(torch.uint8), getattr(b, k).view(torch.uint8))
+    plan.close()
+
+
+def test_layers_beyond_four_gibi_elements_of_an_arena():
+    """Offsets that pass 32 bits, in elements: the first and the last layer of a table whose arena is mostly padding."""
+    far = 2 ** 32 + 8192
+    t = {"elem_off": np.array([0, far], np.int64), "c_out": np.array([3, 5], np.int32),
+         "c_in": np.array([100, 777], np.int32), "khw": np.array([1, 1], np.int32), "mode": np.array([1, 1], np.int32),
+         "k": np.array([1, 2], np.int32)}
+    plan = pkg.Plan(t)
+    small = workload([(3, 100, 1), (5, 777, 1)])
+    ref = Run(small, 1, pkg.TYPE_BF16, seed=9, prox=False)
+    small_plan = pkg.Plan(small.table())
+    eight(ref, small_plan, seed=9)
+    ln = far + 5 * 777
+    big = {"W": torch.empty(ln, device=DEV), "G": torch.empty(ln, dtype=torch.bfloat16, device=DEV),
+           "M": torch.empty(ln, dtype=torch.uint8, device=DEV), "V": torch.empty(ln, dtype=torch.uint8, device=DEV)}
+    spans = [(0, 0, 300), (far, small.layers[1].elem_off, 5 * 777)]
+    for k, x in big.items():
+        for o, so, n in spans:
+            x[o:o + n] = getattr(ref, k)[0][so:so + n]
+    Ms, Vs = ref.Ms[0].clone(), ref.Vs[0].clone()
+    f = ref.fields()
+    want, tol = ref.reference(*[x for x in (E4M3[ref.M.cpu().numpy()] * host(ref.Ms)[:, ref.block],
+                                            (E4M3[ref.V.cpu().numpy()] * host(ref.Vs)[:, ref.block]) ** 2)])
+    pkg.hsadmm_adamw(plan, [big["W"]], [big["G"]], [big["M"]], [big["V"]], state_bits=8, M_scale=[Ms], V_scale=[Vs], noise=4,
+                     **f)
+    pkg.hsadmm_adamw(small_plan, list(ref.W), list(ref.G), list(ref.M), list(ref.V), state_bits=8, M_scale=list(ref.Ms),
+                     V_scale=list(ref.Vs), noise=4, **f)
+    for o, so, n in spans:
+        assert torch.equal(big["W"][o:o + n], ref.W[0][so:so + n])          # (codes differ: they depend on the place)
+    assert torch.equal(Ms, ref.Ms[0]) and torch.equal(Vs, ref.Vs[0])
+    u = rounding_numbers(5 * 777 + 16, 1, 4, first=far)[0][:5 * 777]
+    exact = want["M"][0][300:]
+    blk = ref.block[ref.on][300:]
+    y = np.abs(exact) / host(Ms)[blk]
+    got = np.abs(E4M3[big["M"][far:far + 5 * 777].cpu().numpy()])
+    assert (got == round_down_on_grid(np.minimum(y, 448), u)).mean() > 0.99
+    norm = torch.zeros(1, dtype=torch.float64, device=DEV)
+    ws = torch.zeros(plan.workspace_bytes, dtype=torch.uint8, device=DEV)
+    pkg.hsadmm_gradient_norms(plan, [big["G"]], 1.0, norm, None, ws, grad_type=pkg.TYPE_BF16)
+    g = host(ref.G)[0][ref.on]
+    assert abs(float(norm) / math.sqrt(float((g * g).sum())) - 1) < 1e-12
+    plan.close()
+    small_plan.close()
+
+
+# ------------------------------------------------------------------ norms
+
+@pytest.mark.parametrize("grad_type", [pkg.TYPE_F32, pkg.TYPE_BF16, pkg.TYPE_F16])
+@pytest.mark.parametrize("R", [1, 3, 16])
+@pytest.mark.parametrize("shapes", [SHAPES, [(1, 1, 1)], [(600, 700, 9)]])
+def test_gradient_norms(R, grad_type, shapes):
+    """Sums of squares in fp64 of values whose squares are exact: n * 2^-53 relative at most."""
+    wl = workload(shapes)
+    run = Run(wl, R, grad_type, seed=R, prox=False)
+    plan = pkg.Plan(wl.table())
+    ws = torch.zeros(plan.workspace_bytes, dtype=torch.uint8, device=DEV)
+    norm = torch.full((R + 1,), -1.0, dtype=torch.float64, device=DEV)
+    scale = torch.full((R + 1,), -1.0, device=DEV)
+    g = host(run.G)[:, run.on]
+    want = np.sqrt((g * g).sum(1))
+    limit = float(np.sort(want)[R // 2])                       # some above it, some below
+    pkg.hsadmm_gradient_norms(plan, list(run.G), limit, norm, scale, ws, grad_type=grad_type)
+    got = host(norm)
+    assert np.all(np.abs(got[:R] / want - 1) < wl.n_total * 2.0 ** -52) and got[R] == -1
+    f = host(scale)
+    assert np.all(np.abs(f[:R] - np.minimum(1, limit / want)) <= 1.01 * E) and f[R] == -1
+    pkg.hsadmm_gradient_norms(plan, list(run.G), float("inf"), None, scale, ws, grad_type=grad_type)
+    assert np.all(host(scale)[:R] == 1)
+    plan.close()
+
+
+def test_gradient_norms_of_nothing_and_of_values_that_are_not_finite():
+    wl = workload()
+    plan = pkg.Plan(wl.table())
+    ws = torch.zeros(plan.workspace_bytes, dtype=torch.uint8, device=DEV)
+    norm, scale = torch.zeros(4, dtype=torch.float64, device=DEV), torch.zeros(4, device=DEV)
+    G = torch.zeros(4, wl.n_arena, device=DEV)
+    last = wl.layers[-1]
+    G[1, last.elem_off + last.n - 1] = float("nan")
+    G[2, 0] = float("-inf")
+    G[3, 4] = 3e38                                             # its square is beyond fp32, not beyond fp64
+    pkg.hsadmm_gradient_norms(plan, list(G), 2.0, norm, scale, ws)
+    n, f = host(norm), host(scale)
+    assert n[0] == 0 and f[0] == 1 and np.isnan(n[1]) and np.isnan(f[1]) and np.isinf(n[2]) and np.isnan(f[2])
+    assert abs(n[3] / float(np.float32(3e38)) - 1) < 1e-14 and abs(f[3] * n[3] / 2 - 1) < 1e-6
+    plan.close()
+
+
+# ------------------------------------------------------------------ refusals
+
+def test_update_refuses_what_it_cannot_do():
+    wl = workload()
+    run = Run(wl, 2, pkg.TYPE_F32, seed=1)
+    plan = pkg.Plan(wl.table())
+    before = [x.clone() for x in (run.W, run.M, run.V)]
+    base = dict(W=list(run.W), G=list(run.G), M=list(run.M), V=list(run.V), **run.fields())
+
+    def refused(code, **change):
+        a = {**base, **change}
+        a = {k: v for k, v in a.items() if v is not None}
+        assert pkg.hsadmm_adamw(plan, a.pop("W"), a.pop("G"), a.pop("M"), a.pop("V"), check=False, **a) == code, change
+
+    odd = torch.zeros(wl.n_arena + 8, device=DEV)[1:]
+    refused(-1, W=[run.W[0], odd])                             # misaligned
+    refused(-1, W=[run.W[0], run.W[0]])                        # two replicas, one arena
+    refused(-1, M=[run.M[0], run.V[1]])                        # a moment in another's place
+    refused(-1, G=[run.G[0], run.W[1]])                        # a gradient that is being written over
+    refused(-1, Z=run.W[0])
+    refused(-1, Z=None)
+    refused(-1, U=None)
+    refused(-1, rho=None)
+    refused(-1, M_scale=list(run.M))                           # scales without 8-bit states
+    refused(-1, state_bits=8)                                  # ... and the other way round
+    refused(-4, state_bits=16)
+    refused(-4, grad_type=3)
+    refused(-4, grad_type=-1)
+    refused(-1, W_low=list(torch.zeros_like(run.W)))           # fp32 gradients have no working copy
+    for name, bad in (("lr", -1.0), ("lr", float("nan")), ("beta_one", 1.0), ("beta_one", -0.1), ("beta_two", 1.0),
+                      ("eps", 0.0), ("eps", 1e-40), ("eps", float("inf")), ("weight_decay", -1.0), ("step", 0)):
+        refused(-1, **{name: bad})
+    many = [torch.zeros(1, device=DEV)] * 17
+    refused(-4, W=many, G=many, M=many, V=many)
+    assert pkg.hsadmm_adamw(plan, [], [], [], [], check=False) == -1
+    with pytest.raises(ValueError):
+        pkg.hsadmm_adamw(plan, list(run.W), [run.G[0]], list(run.M), list(run.V))
+    with pytest.raises(TypeError):
+        pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), momentum=1)
+    torch.cuda.synchronize()
+    for x, y in zip(before, (run.W, run.M, run.V)):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    plan.close()
+
+
+def test_norms_refuse_what_they_cannot_do():
+    wl = workload()
+    plan = pkg.Plan(wl.table())
+    G = torch.zeros(wl.n_arena + 8, device=DEV)
+    ws = torch.zeros(plan.workspace_bytes, dtype=torch.uint8, device=DEV)
+    norm, scale = torch.zeros(1, dtype=torch.float64, device=DEV), torch.zeros(1, device=DEV)
+    call = lambda G=[G], limit=1.0, norm=norm, scale=scale, ws=ws, **k: pkg.hsadmm_gradient_norms(  # noqa: E731
+        plan, G, limit, norm, scale, ws, check=False, **k)
+    assert call() == 0
+    assert call(limit=0.0) == -1 and call(limit=float("nan")) == -1 and call(limit=-1.0) == -1
+    assert call(norm=None, scale=None) == -1 and call(G=[]) == -1 and call(G=[G[1:]]) == -1 and call(G=[None]) == -1
+    assert call(grad_type=3) == -4 and call(G=[G] * 17) == -4
+    assert call(ws=ws[:256], workspace_bytes=256) == -2 and call(ws=ws[1:], workspace_bytes=plan.workspace_bytes) == -1
+    plan.close()
