@@ -147,6 +147,7 @@ struct hsadmm_plan {
     std::vector<WorkItem> items_both;   // composite_colsums: tiles of the layers under both constraints
     std::vector<int32_t> both_layers;   // their indices
     std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, gather_mx, scatter_mx: every layer cut without regard to rows
+    int64_t packed_elems = 0;           // what the plan's own selection packs
     int64_t state_blocks = 0;           // blocks that share a scale in 8-bit optimizer states
     int32_t n_segments = 0;             // scan segments (one per layer, two per BOTH layer)
     int32_t pack_align = 1;
@@ -516,6 +517,7 @@ int lay_out(hsadmm_plan* p, const hsadmm_layer_t* layers, const hsadmm_nest_t* n
     p->groups_total = gb;
     p->colpart_total = cp;
     p->packed_capacity = cap;
+    p->packed_elems = poff;
     size_t off = 0;
     p->ws.key = off;        off = align_up(off + sizeof(double) * (size_t)gb, 256);
     p->ws.colpart = off;    off = align_up(off + sizeof(double) * (size_t)(cp ? cp : 1), 256);
@@ -2119,6 +2121,13 @@ int hsadmm_adamw(const hsadmm_plan_t* p, const hsadmm_adamw_args_t* x)
 
 // ------------------------------------------------------------------ quantised packed buffers
 
+// Packed positions from which on a thread of the gather takes four fours instead of two: what the chip holds at once with two
+// (eight workgroups on each of 256 compute units).  With two / four, us: 1.0 M positions 7.2 / 8.1 (filters), 10.2 / 12.3
+// (channels), 4.0 M 13.0 / 14.0, 17.5 / 18.8, 6.1 M 17.3 / 15.0, 24.7 / 21.9, 11.4 M 27.6 / 24.7 (filters).
+constexpr int64_t kMxWide = 8 * 256 * 8 * kBlock;
+// (any number does: a workgroup goes on to further tiles)
+constexpr int64_t kMxGridMost = 1 << 22;
+
 static MxMaps mx_maps(const hsadmm_plan* p, const char* ws)
 {
     MxMaps m;
@@ -2147,12 +2156,17 @@ int hsadmm_compact_mx(const hsadmm_plan_t* p, const float* src0, const float* sr
         const int rc = run_scan(p, mask, ws, s);
         if (rc != HSADMM_OK) return rc;
     }
-    const auto go = [&](auto kernel) {
-        return launch(p, kGatherMx, kernel, (unsigned)p->items_flat.size(), kBlock, s, (const FlatItem*)p->d_items_flat,
-                      (const DevLayer*)p->d_layers, src0, src1, mx_maps(p, ws), codes, scales, CopyOut{layer_off, kept_idx});
+    const auto go = [&](auto q) {
+        constexpr int Q = decltype(q)::value;
+        const auto with = [&](auto kernel) {
+            const int64_t tiles = (p->packed_elems + 4 * Q * kBlock - 1) / (4 * Q * kBlock);
+            return launch(p, kGatherMx, kernel, (unsigned)std::max<int64_t>(1, std::min(tiles, kMxGridMost)), kBlock, s,
+                          (const DevLayer*)p->d_layers, src0, src1, mx_maps(p, ws), codes, scales, CopyOut{layer_off, kept_idx});
+        };
+        if (format == HSADMM_MX_FP8) return src1 ? with(gather_mx<HSADMM_MX_FP8, true, Q>) : with(gather_mx<HSADMM_MX_FP8, false, Q>);
+        return src1 ? with(gather_mx<HSADMM_MX_FP4, true, Q>) : with(gather_mx<HSADMM_MX_FP4, false, Q>);
     };
-    const hipError_t e = format == HSADMM_MX_FP8 ? (src1 ? go(gather_mx<HSADMM_MX_FP8, true>) : go(gather_mx<HSADMM_MX_FP8, false>))
-                                                 : (src1 ? go(gather_mx<HSADMM_MX_FP4, true>) : go(gather_mx<HSADMM_MX_FP4, false>));
+    const hipError_t e = p->packed_elems > kMxWide ? go(std::integral_constant<int, 4>{}) : go(std::integral_constant<int, 2>{});
     return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
 }
 
