@@ -292,11 +292,11 @@ __device__ __forceinline__ unsigned int block_umin(unsigned int x, unsigned int*
 // item, a thread fours of adjacent elements.  Fours of rows that are packed whole and in whole words come straight from the
 // buffers.  Other rows' elements (columns of a row, rows that start anywhere) have their places in one stretch of packed
 // positions: the workgroup finds where it starts and ends, decodes it in order into LDS, a code once, and picks from there.
-// (An element at a time out of the buffers / this way, us: ResNet-50, both constraints, four nodes in fp4 113.0 / 82.7; ResNet-18 of
-// width 45, filters, two nodes in fp8 9.7 / 9.2.)  Bound by HBM: ResNet-50, filters, eight nodes in fp8, with the dual update 502 MB
+// (An element at a time out of the buffers / this way, us: ResNet-50, both constraints, four nodes in fp4 113.0 / 82.7, with every
+// wave there is 77.8; ResNet-18 of width 45, filters, two nodes in fp8 9.7 / 8.9.)  Bound by HBM: ResNet-50, filters, eight nodes in fp8, with the dual update 502 MB
 // in 80.8 us, 6.2 TB/s.
 template <int FMT, bool DUAL>
-__global__ __launch_bounds__(kBlock) void scatter_mx(const FlatItem* __restrict__ items, const DevLayer* __restrict__ layers,
+__global__ __launch_bounds__(kBlock, 8) void scatter_mx(const FlatItem* __restrict__ items, const DevLayer* __restrict__ layers,
                                                      MxBuffers b, int M, float inv_M, MxMaps mp, float* __restrict__ dst,
                                                      const float* __restrict__ Zi, float* __restrict__ Vd)
 {
