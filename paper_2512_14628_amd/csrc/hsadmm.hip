@@ -735,7 +735,7 @@ template <int T, bool S8>
 hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool prox, bool low, hipStream_t s)
 {
     const auto go = [&](auto kernel) {
-        return launch(p, kAdamw, kernel, (unsigned)p->items_flat.size(), kBlock, s, (const FlatItem*)p->d_items_flat, a, R);
+        return launch(p, kAdamw, kernel, (unsigned)p->items_flat.size() * kFlatQuads, kBlock, s, (const FlatItem*)p->d_items_flat, a, R);
     };
     if constexpr (T != HSADMM_TYPE_F32)
         if (low) return prox ? go(adamw_kernel<T, S8, true, true>) : go(adamw_kernel<T, S8, false, true>);

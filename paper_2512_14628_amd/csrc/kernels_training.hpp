@@ -67,7 +67,9 @@ __device__ __forceinline__ void store4(typename ElemOf<T>::type* p, const v4f& v
 struct GradArgs { const void* G[HSADMM_MAX_REPLICAS]; };
 
 // Sums of squares in fp64 (the square of an fp32 value is exact there): workgroup p of a replica's P takes the flat items
-// p, p + P, ...; the order of the additions depends on the plan and the number of replicas only.
+// p, p + P, ...; the order of the additions depends on the plan and the number of replicas only.  Bound by HBM: ResNet-152, 8
+// replicas in bf16, 961 MB in 148 us (6.5 TB/s); ResNet-18, one in fp32, 10.7 us, of which 3 are gradient_norm_finish.  (Two to four
+// items in flight: 149 to 156 us and 10.7, and small networks lose a microsecond or two.)
 template <int T>
 __global__ __launch_bounds__(kBlock) void gradient_sqsums(const FlatItem* __restrict__ items, int n_items, GradArgs a, int P,
                                                           double* __restrict__ part)
@@ -79,10 +81,16 @@ __global__ __launch_bounds__(kBlock) void gradient_sqsums(const FlatItem* __rest
     for (int i = p; i < n_items; i += P) {
         const FlatItem it = items[i];
         v4f g[kFlatQuads];
+        // (whole items apart: a load whose length is looked at is converted, and so waited for, where it stands: 177 us above)
+        if (it.n == kFlatElems) {
 #pragma unroll
-        for (int k = 0; k < kFlatQuads; ++k) {
-            const int q = 4 * (threadIdx.x + k * kBlock);
-            g[k] = load4<T>(G + it.base + q, min(4, it.n - q));
+            for (int k = 0; k < kFlatQuads; ++k) g[k] = load4<T>(G + it.base + 4 * (threadIdx.x + k * kBlock), 4);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kFlatQuads; ++k) {
+                const int q = 4 * (threadIdx.x + k * kBlock);
+                g[k] = load4<T>(G + it.base + q, min(4, it.n - q));
+            }
         }
 #pragma unroll
         for (int k = 0; k < kFlatQuads; ++k) {
@@ -108,7 +116,16 @@ __global__ __launch_bounds__(kBlock) void gradient_norm_finish(const double* __r
 {
     __shared__ double red[kWaves];
     double s = 0.0;
-    for (int i = threadIdx.x; i < P; i += kBlock) s += part[(int64_t)blockIdx.x * P + i];
+    for (int i0 = 0; i0 < P; i0 += 8 * kBlock) {           // (eight loads in flight)
+        double x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = i0 + k * kBlock + (int)threadIdx.x;
+            x[k] = i < P ? part[(int64_t)blockIdx.x * P + i] : 0.0;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += x[k];
+    }
     s = wave_xor_sum(s, kWave);
     if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = s;
     __syncthreads();
@@ -231,109 +248,95 @@ __device__ __forceinline__ float root_of(float x)
 
 // Formulas: see hsadmm_adamw in the header.  Moments are formed in fp32, every operation rounded by itself; the weights' last
 // two operations are fused and the reciprocal before them is the machine's own, within one unit in the last place.
+// A workgroup takes 4 * kBlock elements, the `part`-th stretch of an item, of all replicas in turn, so z_i and u are read once.
+// (Two fours a thread: ResNet-50, 4 replicas, 32-bit states 549 us instead of 543, 8-bit states 333 / 322, four times wider 1061 / 1014.)
 template <int T, bool S8, bool PROX, bool LOW, bool FULL>
-__device__ __forceinline__ void adamw_item(const FlatItem& it, const AdamwArgs& a, int R)
+__device__ __forceinline__ void adamw_part(const FlatItem& it, int part, const AdamwArgs& a, int R)
 {
     typedef typename ElemOf<T>::type E;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int lane = threadIdx.x & (kWave - 1);
+    const int q = 4 * (part * kBlock + threadIdx.x);
+    const int nv = FULL ? 4 : min(4, it.n - q);
+    const int64_t at = it.base + q;
+    // the wave's state block, and whether the layer reaches that far
+    const int64_t block = it.block0 + part * kWaves + wave;
+    const bool on = FULL || it.n > (part * kWaves + wave) * kStateBlock;
     const hsadmm_adamw_coef_t co = a.coef_dev ? *a.coef_dev : a.coef;
-    int nv[kFlatQuads];
-    int64_t at[kFlatQuads];
-    v4f z[kFlatQuads], u[kFlatQuads];
-#pragma unroll
-    for (int k = 0; k < kFlatQuads; ++k) {
-        const int q = 4 * (threadIdx.x + k * kBlock);
-        nv[k] = FULL ? 4 : min(4, it.n - q);
-        at[k] = it.base + q;
-        if (PROX) { z[k] = load4<HSADMM_TYPE_F32>(a.Z + at[k], nv[k]); u[k] = load4<HSADMM_TYPE_F32>(a.U + at[k], nv[k]); }
-    }
+    v4f z, u;
+    if (PROX) { z = load4<HSADMM_TYPE_F32>(a.Z + at, nv); u = load4<HSADMM_TYPE_F32>(a.U + at, nv); }
     const float rho = PROX ? a.rho[it.layer] : 0.f;
     for (int r = 0; r < R; ++r) {
         const float s = a.grad_scale ? a.grad_scale[r] : 1.0f;
         if (!(__builtin_fabsf(s) < __builtin_inff())) continue;      // a gradient that is not finite: no step
-        float* W = a.W[r];
-        const E* G = static_cast<const E*>(a.G[r]);
-        v4f w[kFlatQuads], g[kFlatQuads], m[kFlatQuads], v[kFlatQuads];
-        unsigned int mc[kFlatQuads], vc[kFlatQuads];
-        float ms[kFlatQuads], vs[kFlatQuads];
-#pragma unroll
-        for (int k = 0; k < kFlatQuads; ++k) {
-            w[k] = load4<HSADMM_TYPE_F32>(W + at[k], nv[k]);
-            g[k] = load4<T>(G + at[k], nv[k]);
-            if (S8) {
-                const bool on = FULL || it.n > (wave + k * kWaves) * kStateBlock;
-                const int64_t b = it.block0 + wave + k * kWaves;
-                mc[k] = load_codes(static_cast<const uint8_t*>(a.M[r]) + at[k], nv[k]);
-                vc[k] = load_codes(static_cast<const uint8_t*>(a.V[r]) + at[k], nv[k]);
-                ms[k] = on ? a.Ms[r][b] : 0.f;
-                vs[k] = on ? a.Vs[r][b] : 0.f;
-            } else {
-                m[k] = load4<HSADMM_TYPE_F32>(static_cast<const float*>(a.M[r]) + at[k], nv[k]);
-                v[k] = load4<HSADMM_TYPE_F32>(static_cast<const float*>(a.V[r]) + at[k], nv[k]);
-            }
+        v4f w = load4<HSADMM_TYPE_F32>(a.W[r] + at, nv);
+        const v4f g = load4<T>(static_cast<const E*>(a.G[r]) + at, nv);
+        v4f m, v, rt;
+        if (S8) {
+            const unsigned int mc = load_codes(static_cast<const uint8_t*>(a.M[r]) + at, nv);
+            const unsigned int vc = load_codes(static_cast<const uint8_t*>(a.V[r]) + at, nv);
+            m = decode4(mc, on ? a.Ms[r][block] : 0.f);
+            const v4f root = decode4(vc, on ? a.Vs[r][block] : 0.f);
+            v = root * root;
+        } else {
+            m = load4<HSADMM_TYPE_F32>(static_cast<const float*>(a.M[r]) + at, nv);
+            v = load4<HSADMM_TYPE_F32>(static_cast<const float*>(a.V[r]) + at, nv);
         }
 #pragma unroll
-        for (int k = 0; k < kFlatQuads; ++k) {
-            if (S8) {
-                m[k] = decode4(mc[k], ms[k]);
-                const v4f q = decode4(vc[k], vs[k]);
-                v[k] = q * q;
-            }
-            v4f rt;
+        for (int i = 0; i < 4; ++i) {
+            float gi = g[i] * s;
+            if (PROX) gi = gi + rho * ((w[i] - z[i]) + u[i]);
+            m[i] = a.beta1 * m[i] + a.one_minus_beta1 * gi;
+            v[i] = a.beta2 * v[i] + a.one_minus_beta2 * (gi * gi);
+            rt[i] = root_of(v[i]);
+            const float t = m[i] * __builtin_amdgcn_rcpf(__builtin_fmaf(rt[i], co.root, a.eps));
+            w[i] = __builtin_fmaf(-co.step_size, t, w[i] * co.decay);
+        }
+        store4<HSADMM_TYPE_F32>(a.W[r] + at, w, nv);
+        if (LOW) store4<T>(static_cast<E*>(a.Wl[r]) + at, w, nv);
+        if (!S8) {
+            store4<HSADMM_TYPE_F32>(static_cast<float*>(a.M[r]) + at, m, nv);
+            store4<HSADMM_TYPE_F32>(static_cast<float*>(a.V[r]) + at, v, nv);
+            continue;
+        }
+        if (!FULL) {
+            // (values past the end of the layer count for nothing)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float gi = g[k][i] * s;
-                if (PROX) gi = gi + rho * ((w[k][i] - z[k][i]) + u[k][i]);
-                m[k][i] = a.beta1 * m[k][i] + a.one_minus_beta1 * gi;
-                v[k][i] = a.beta2 * v[k][i] + a.one_minus_beta2 * (gi * gi);
-                rt[i] = root_of(v[k][i]);
-                const float t = m[k][i] * __builtin_amdgcn_rcpf(__builtin_fmaf(rt[i], co.root, a.eps));
-                w[k][i] = __builtin_fmaf(-co.step_size, t, w[k][i] * co.decay);
-            }
-            store4<HSADMM_TYPE_F32>(W + at[k], w[k], nv[k]);
-            if (LOW) store4<T>(static_cast<E*>(a.Wl[r]) + at[k], w[k], nv[k]);
-            if (!S8) {
-                store4<HSADMM_TYPE_F32>(static_cast<float*>(a.M[r]) + at[k], m[k], nv[k]);
-                store4<HSADMM_TYPE_F32>(static_cast<float*>(a.V[r]) + at[k], v[k], nv[k]);
-            } else {
-                if (!FULL) {
-                    // (values past the end of the layer count for nothing)
+            for (int i = 0; i < 4; ++i)
+                if (i >= nv) m[i] = rt[i] = 0.f;
+        }
+        float mu, vu;
+        const float mscale = block_scale(wave_umax(top_bits(m)), mu), vscale = block_scale(wave_umax(top_bits(rt)), vu);
+        const int64_t four = at >> 2;
+        const unsigned int mix = mix_four((unsigned int)four + (unsigned int)(four >> 32) * kMix3 + co.noise + (unsigned int)r * kMix3);
+        v4f ym = m * mu, yv = rt * vu;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (i >= nv[k]) m[k][i] = rt[i] = 0.f;
-                }
-                const unsigned int mt = wave_umax(top_bits(m[k])), vt = wave_umax(top_bits(rt));
-                float mu, vu;
-                const float mscale = block_scale(mt, mu), vscale = block_scale(vt, vu);
-                const int64_t four = at[k] >> 2;
-                const unsigned int mix = mix_four((unsigned int)four + (unsigned int)(four >> 32) * kMix3 + co.noise +
-                                                  (unsigned int)r * kMix3);
-                v4f ym = m[k] * mu, yv = rt * vu;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    ym[i] = __builtin_amdgcn_fmed3f(ym[i], -448.0f, 448.0f);
-                    // a root that is not zero keeps a code that is not: a zero would divide by eps alone
-                    yv[i] = yv[i] > 0.f ? __builtin_amdgcn_fmed3f(yv[i], 0x1p-9f, 448.0f) : 0.f;
-                }
-                store_codes(static_cast<uint8_t*>(a.M[r]) + at[k], encode4(ym, mix), nv[k]);
-                store_codes(static_cast<uint8_t*>(a.V[r]) + at[k], encode4(yv, mix), nv[k]);
-                const int64_t b = it.block0 + wave + k * kWaves;
-                if (lane == 0 && (FULL || it.n > (wave + k * kWaves) * kStateBlock)) {
-                    a.Ms[r][b] = mscale;
-                    a.Vs[r][b] = vscale;
-                }
-            }
+        for (int i = 0; i < 4; ++i) {
+            ym[i] = __builtin_amdgcn_fmed3f(ym[i], -448.0f, 448.0f);
+            // a root that is not zero keeps a code that is not: a zero would divide by eps alone
+            yv[i] = yv[i] > 0.f ? __builtin_amdgcn_fmed3f(yv[i], 0x1p-9f, 448.0f) : 0.f;
+        }
+        store_codes(static_cast<uint8_t*>(a.M[r]) + at, encode4(ym, mix), nv);
+        store_codes(static_cast<uint8_t*>(a.V[r]) + at, encode4(yv, mix), nv);
+        if (on && (threadIdx.x & (kWave - 1)) == 0) {
+            a.Ms[r][block] = mscale;
+            a.Vs[r][block] = vscale;
         }
     }
 }
 
+// Waves per SIMD (see pass1_waves): with every wave its registers allow in flight, a kernel of many streams crowds the memory.
+// With 3, 4, 6, all 8, us: 32-bit states, ResNet-50, 4 replicas with the pull 523, 543, 560, 559 (5.85 TB/s at best), one replica in
+// bf16 147, 151, 155, 157, ResNet-18 alone 55.0, 53.4, 54.4, 54.5; 8-bit states with the pull, ResNet-50, 4 replicas 353, 318, 316,
+// 325 (5.83 TB/s), one 120, 110, 105, 102; without, four times wider 1517, 1275, 1065, 1001 (6.15 TB/s; more arithmetic per byte).
+constexpr int adamw_waves(bool S8, bool PROX) { return !S8 ? 3 : PROX ? 6 : kAllWaves; }
+
 template <int T, bool S8, bool PROX, bool LOW>
-__global__ __launch_bounds__(kBlock) void adamw_kernel(const FlatItem* __restrict__ items, AdamwArgs a, int R)
+__global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(1, adamw_waves(S8, PROX)))) void adamw_kernel(const FlatItem* __restrict__ items, AdamwArgs a, int R)
 {
-    const FlatItem it = items[blockIdx.x];
-    if (it.n == kFlatElems) adamw_item<T, S8, PROX, LOW, true>(it, a, R);
-    else adamw_item<T, S8, PROX, LOW, false>(it, a, R);
+    const FlatItem it = items[blockIdx.x / kFlatQuads];
+    const int part = blockIdx.x % kFlatQuads;
+    if (it.n - part * 4 * kBlock >= 4 * kBlock) adamw_part<T, S8, PROX, LOW, true>(it, part, a, R);
+    else if (it.n > part * 4 * kBlock) adamw_part<T, S8, PROX, LOW, false>(it, part, a, R);
 }
 
 }  // namespace
