@@ -89,24 +89,19 @@ class _AdamwCoef(ctypes.Structure):
                 ("noise", ctypes.c_uint32)]
 
 
-# hsadmm_adamw_args_t, field by field, in declaration order, as _STEP_FIELDS.
-#   "each": HOST array of one device buffer per replica (a sequence, or None), "int" / "float": a scalar
+# hsadmm_adamw_args_t, field by field, in declaration order.  W .. W_low are HOST arrays of device addresses.
 _ADAMW_FIELDS = (
-    ("struct_bytes", ctypes.c_size_t, "sizeof"),
-    ("R", ctypes.c_int32, "replica_count"), ("grad_type", ctypes.c_int32, "int"),
-    ("state_bits", ctypes.c_int32, "int"), ("noise", ctypes.c_uint32, "int"),
-    ("W", ctypes.POINTER(_vp), "each"), ("G", ctypes.POINTER(_vp), "each"), ("M", ctypes.POINTER(_vp), "each"),
-    ("V", ctypes.POINTER(_vp), "each"), ("M_scale", ctypes.POINTER(_vp), "each"),
-    ("V_scale", ctypes.POINTER(_vp), "each"), ("W_low", ctypes.POINTER(_vp), "each"),
-    ("Z", _vp, "dev"), ("U", _vp, "dev"), ("rho", _vp, "dev"), ("grad_scale", _vp, "dev"), ("coef", _vp, "dev"),
-    ("lr", ctypes.c_double, "float"), ("beta_one", ctypes.c_double, "float"), ("beta_two", ctypes.c_double, "float"),
-    ("eps", ctypes.c_double, "float"), ("weight_decay", ctypes.c_double, "float"), ("step", ctypes.c_int64, "int"),
-    ("hip_stream", _vp, "stream"),
+    ("struct_bytes", ctypes.c_size_t), ("R", ctypes.c_int32), ("grad_type", ctypes.c_int32),
+    ("state_bits", ctypes.c_int32), ("noise", ctypes.c_uint32),
+    ("W", _vp), ("G", _vp), ("M", _vp), ("V", _vp), ("M_scale", _vp), ("V_scale", _vp), ("W_low", _vp),
+    ("Z", _vp), ("U", _vp), ("rho", _vp), ("grad_scale", _vp), ("coef", _vp),
+    ("lr", ctypes.c_double), ("beta_one", ctypes.c_double), ("beta_two", ctypes.c_double),
+    ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("step", ctypes.c_int64), ("hip_stream", _vp),
 )
 
 
 class _AdamwArgs(ctypes.Structure):
-    _fields_ = [(name, ctype) for name, ctype, _ in _ADAMW_FIELDS]
+    _fields_ = list(_ADAMW_FIELDS)
 
 
 _lib = None
@@ -795,41 +790,31 @@ def hsadmm_plan_state_blocks(plan: Plan) -> int:
     return n.value
 
 
-def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence, stream=None, check: bool = True,
-                 **fields) -> int:
-    """One AdamW step of every layer of every replica.  W, G, M, V: one buffer per replica; keyword arguments are the
-    other fields of hsadmm_adamw_args_t (grad_type, state_bits, M_scale, V_scale, W_low, Z, U, rho, grad_scale, coef, lr,
-    beta_one, ...).  Not given: grad_type TYPE_F32, state_bits 32, beta_one 0.9, beta_two 0.999, eps 1e-8, step 1; buffers
-    stay NULL, other numbers 0."""
-    lib = load_library()
-    known = {name for name, _, how in _ADAMW_FIELDS if how in ("dev", "each", "int", "float")} - {"W", "G", "M", "V"}
-    unknown = set(fields) - known
-    if unknown:
-        raise TypeError("hsadmm_adamw has no field(s) %s" % ", ".join(sorted(unknown)))
-    for name in ("G", "M", "V", "M_scale", "V_scale", "W_low"):
-        buffers = {"G": G, "M": M, "V": V}.get(name, fields.get(name))
-        if buffers is not None and len(buffers) != len(W):
-            raise ValueError("hsadmm_adamw: %d buffers in %s, %d replicas" % (len(buffers), name, len(W)))
-    values = {"state_bits": 32, "beta_one": 0.9, "beta_two": 0.999, "eps": 1e-8, "step": 1, **fields,
-              "W": W, "G": G, "M": M, "V": V}
-    args = _AdamwArgs()
-    for name, _, how in _ADAMW_FIELDS:
-        if how == "sizeof":
-            value = ctypes.sizeof(_AdamwArgs)
-        elif how == "replica_count":
-            value = len(W)
-        elif how == "each":
-            value = _each(values.get(name))
-        elif how == "dev":
-            value = _ptr(values.get(name))
-        elif how == "int":
-            value = int(values.get(name, 0))
-        elif how == "float":
-            value = float(values.get(name, 0.0))
-        else:
-            value = _stream(stream)
-        setattr(args, name, value)
-    rc = lib.hsadmm_adamw(plan.handle, ctypes.byref(args))
+def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence, *, grad_type: int = TYPE_F32,
+                 state_bits: int = 32, M_scale: Optional[Sequence] = None, V_scale: Optional[Sequence] = None,
+                 W_low: Optional[Sequence] = None, Z=None, U=None, rho=None, grad_scale=None, coef=None, lr: float = 0.0,
+                 beta_one: float = 0.9, beta_two: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+                 step: int = 1, noise: int = 0, stream=None, check: bool = True) -> int:
+    """One AdamW step of every layer of every replica.  W, G, M, V (and M_scale, V_scale, W_low where they are given): one
+    buffer per replica; the other arguments are the fields of hsadmm_adamw_args_t."""
+    R = len(W)
+    at, places = [], []                     # one HOST array for all lists, and where each of them starts in it
+    for name, buffers in (("W", W), ("G", G), ("M", M), ("V", V), ("M_scale", M_scale), ("V_scale", V_scale),
+                          ("W_low", W_low)):
+        if buffers is None:
+            places.append(None)
+            continue
+        if len(buffers) != R:
+            raise ValueError("hsadmm_adamw: %d buffers in %s, %d replicas" % (len(buffers), name, R))
+        places.append(len(at))
+        at += [_ptr(b) for b in buffers]
+    array = (_vp * max(len(at), 1))(*at)
+    first = ctypes.addressof(array)
+    args = _AdamwArgs(ctypes.sizeof(_AdamwArgs), R, grad_type, state_bits, noise & 0xFFFFFFFF,
+                      *[None if p is None else first + ctypes.sizeof(_vp) * p for p in places],
+                      _ptr(Z), _ptr(U), _ptr(rho), _ptr(grad_scale), _ptr(coef), lr, beta_one, beta_two, eps, weight_decay,
+                      step, _stream(stream))
+    rc = load_library().hsadmm_adamw(plan.handle, ctypes.byref(args))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_adamw")
     return rc
