@@ -735,7 +735,7 @@ template <int T, bool S8>
 hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool prox, bool low, hipStream_t s)
 {
     const auto go = [&](auto kernel) {
-        return launch(p, kAdamw, kernel, (unsigned)p->items_flat.size() * kFlatQuads, kBlock, s, (const FlatItem*)p->d_items_flat, a, R);
+        return launch(p, kAdamw, kernel, (unsigned)p->items_flat.size() * (kFlatElems / (4 * kBlock)), kBlock, s, (const FlatItem*)p->d_items_flat, a, R);
     };
     if constexpr (T != HSADMM_TYPE_F32)
         if (low) return prox ? go(adamw_kernel<T, S8, true, true>) : go(adamw_kernel<T, S8, false, true>);
@@ -2014,7 +2014,7 @@ int hsadmm_gradient_norms(const hsadmm_plan_t* p, const void* const* G, int32_t 
     // a partial sum per workgroup, in the place of the residual sums' partials (four doubles a row item, 32 at least)
     const int64_t room = (int64_t)((p->ws.work - p->ws.respart) / sizeof(double));
     const int n_items = (int)p->items_flat.size();
-    const int P = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)n_items, kGradGrid / R, room / R}));
+    const int P = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)n_items * kParts, kGradGrid / R, room / R}));
     double* part = reinterpret_cast<double*>(static_cast<char*>(workspace) + p->ws.respart);
     const auto sums = [&](auto kernel) {
         return launch(p, kGradSq, kernel, (unsigned)(P * R), kBlock, s, (const FlatItem*)p->d_items_flat, n_items, a, P, part);
@@ -2198,7 +2198,7 @@ int hsadmm_expand_mx(const hsadmm_plan_t* p, const uint8_t* const* codes, const 
         if (rc != HSADMM_OK) return rc;
     }
     const auto go = [&](auto kernel) {
-        return launch(p, kScatterMx, kernel, (unsigned)p->items_flat.size(), kBlock, s, (const FlatItem*)p->d_items_flat,
+        return launch(p, kScatterMx, kernel, (unsigned)p->items_flat.size() * kParts, kBlock, s, (const FlatItem*)p->d_items_flat,
                       (const DevLayer*)p->d_layers, b, (int)M, 1.0f / (float)M, mx_maps(p, ws), dst, Zi, Vd);
     };
     const hipError_t e = format == HSADMM_MX_FP8 ? (Zi ? go(scatter_mx<HSADMM_MX_FP8, true>) : go(scatter_mx<HSADMM_MX_FP8, false>))

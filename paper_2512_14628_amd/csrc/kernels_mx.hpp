@@ -288,8 +288,8 @@ __device__ __forceinline__ unsigned int block_umin(unsigned int x, unsigned int*
     return min(min(red[0], red[1]), min(red[2], red[3]));
 }
 
-// dst <- the mean of M buffers on the kept elements, +0 elsewhere; DUAL: Vd <- Vd + (Zi - dst).  A workgroup takes a flat
-// item, a thread fours of adjacent elements.  Fours of rows that are packed whole and in whole words come straight from the
+// dst <- the mean of M buffers on the kept elements, +0 elsewhere; DUAL: Vd <- Vd + (Zi - dst).  A workgroup takes a part
+// of a flat item, a thread fours of adjacent elements.  Fours of rows that are packed whole and in whole words come straight from the
 // buffers.  Other rows' elements (columns of a row, rows that start anywhere) have their places in one stretch of packed
 // positions: the workgroup finds where it starts and ends, decodes it in order into LDS, a code once, and picks from there.
 // (An element at a time out of the buffers / this way, us: ResNet-50, both constraints, four nodes in fp4 113.0 / 82.7, with every
@@ -300,9 +300,13 @@ __global__ __launch_bounds__(kBlock, 8) void scatter_mx(const FlatItem* __restri
                                                      MxBuffers b, int M, float inv_M, MxMaps mp, float* __restrict__ dst,
                                                      const float* __restrict__ Zi, float* __restrict__ Vd)
 {
-    __shared__ __align__(16) float stage[kFlatElems + kMxBlock];
+    __shared__ __align__(16) float stage[kPartElems + kMxBlock];
     __shared__ unsigned int red[2][kWaves];
-    const FlatItem it = items[blockIdx.x];
+    FlatItem it = items[blockIdx.x / kParts];
+    const int skip = (int)(blockIdx.x % kParts) * kPartElems;
+    if (it.n <= skip) return;
+    it.base += skip;
+    it.n = min(it.n - skip, kPartElems);
     const int l = it.layer;
     const DevLayer& L = layers[l];
     const int mode = L.mode;

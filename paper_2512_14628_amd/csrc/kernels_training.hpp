@@ -10,12 +10,15 @@ namespace {
 
 // ------------------------------------------------------------------ flat items
 
-// kFlatElems consecutive elements of one layer (fewer at its end): the unit of work of the kernels that do not care about
-// groups.  A thread of the workgroup owns kFlatQuads fours of adjacent elements, kBlock fours apart, so a wave's access is
-// contiguous and a wave's 64 fours are one state block.
+// kFlatElems consecutive elements of one layer (fewer at its end): the table of the kernels that do not care about groups.  A
+// workgroup takes a part of an item: kPartElems elements, kFlatQuads fours of adjacent elements a thread, kBlock fours apart, or
+// (adamw_kernel) one four a thread.  A wave's access is contiguous and a wave's 64 fours are one state block.
+// (An item per workgroup instead, for the largest networks, adds a tenth to the time a plan takes to make.)
 constexpr int kStateBlock = 256;
-constexpr int kFlatElems = 2048;
-constexpr int kFlatQuads = kFlatElems / (4 * kBlock);
+constexpr int kFlatElems = 8192;
+constexpr int kFlatQuads = 2;
+constexpr int kPartElems = 4 * kFlatQuads * kBlock;
+constexpr int kParts = kFlatElems / kPartElems;
 static_assert(kStateBlock == 4 * kWave, "a wave's fours are one state block");
 
 struct FlatItem {
@@ -66,10 +69,10 @@ __device__ __forceinline__ void store4(typename ElemOf<T>::type* p, const v4f& v
 
 struct GradArgs { const void* G[HSADMM_MAX_REPLICAS]; };
 
-// Sums of squares in fp64 (the square of an fp32 value is exact there): workgroup p of a replica's P takes the flat items
-// p, p + P, ...; the order of the additions depends on the plan and the number of replicas only.  Bound by HBM: ResNet-152, 8
+// Sums of squares in fp64 (the square of an fp32 value is exact there): workgroup p of a replica's P takes the parts of the flat
+// items p, p + P, ...; the order of the additions depends on the plan and the number of replicas only.  Bound by HBM: ResNet-152, 8
 // replicas in bf16, 961 MB in 148 us (6.5 TB/s); ResNet-18, one in fp32, 10.7 us, of which 3 are gradient_norm_finish.  (Two to four
-// items in flight: 149 to 156 us and 10.7, and small networks lose a microsecond or two.)
+// parts in flight: 149 to 156 us and 10.7, and small networks lose a microsecond or two.)
 template <int T>
 __global__ __launch_bounds__(kBlock) void gradient_sqsums(const FlatItem* __restrict__ items, int n_items, GradArgs a, int P,
                                                           double* __restrict__ part)
@@ -78,11 +81,14 @@ __global__ __launch_bounds__(kBlock) void gradient_sqsums(const FlatItem* __rest
     const int r = blockIdx.x / P, p = blockIdx.x - r * P;
     const typename ElemOf<T>::type* G = static_cast<const typename ElemOf<T>::type*>(a.G[r]);
     double s0 = 0.0, s1 = 0.0, s2 = 0.0, s3 = 0.0;
-    for (int i = p; i < n_items; i += P) {
-        const FlatItem it = items[i];
+    for (int64_t i = p; i < (int64_t)n_items * kParts; i += P) {
+        FlatItem it = items[i / kParts];
+        const int skip = (int)(i % kParts) * kPartElems;
+        it.base += skip;
+        it.n -= skip;
         v4f g[kFlatQuads];
-        // (whole items apart: a load whose length is looked at is converted, and so waited for, where it stands: 177 us above)
-        if (it.n == kFlatElems) {
+        // (whole parts apart: a load whose length is looked at is converted, and so waited for, where it stands: 177 us above)
+        if (it.n >= kPartElems) {
 #pragma unroll
             for (int k = 0; k < kFlatQuads; ++k) g[k] = load4<T>(G + it.base + 4 * (threadIdx.x + k * kBlock), 4);
         } else {
@@ -248,7 +254,7 @@ __device__ __forceinline__ float root_of(float x)
 
 // Formulas: see hsadmm_adamw in the header.  Moments are formed in fp32, every operation rounded by itself; the weights' last
 // two operations are fused and the reciprocal before them is the machine's own, within one unit in the last place.
-// A workgroup takes 4 * kBlock elements, the `part`-th stretch of an item, of all replicas in turn, so z_i and u are read once.
+// A workgroup takes 4 * kBlock elements, the `part`-th such stretch of an item, of all replicas in turn, so z_i and u are read once.
 // (Two fours a thread: ResNet-50, 4 replicas, 32-bit states 549 us instead of 543, 8-bit states 333 / 322, four times wider 1061 / 1014.)
 template <int T, bool S8, bool PROX, bool LOW, bool FULL>
 __device__ __forceinline__ void adamw_part(const FlatItem& it, int part, const AdamwArgs& a, int R)
@@ -333,8 +339,9 @@ constexpr int adamw_waves(bool S8, bool PROX) { return !S8 ? 3 : PROX ? 6 : kAll
 template <int T, bool S8, bool PROX, bool LOW>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(1, adamw_waves(S8, PROX)))) void adamw_kernel(const FlatItem* __restrict__ items, AdamwArgs a, int R)
 {
-    const FlatItem it = items[blockIdx.x / kFlatQuads];
-    const int part = blockIdx.x % kFlatQuads;
+    constexpr int kEach = kFlatElems / (4 * kBlock);
+    const FlatItem it = items[blockIdx.x / kEach];
+    const int part = blockIdx.x % kEach;
     if (it.n - part * 4 * kBlock >= 4 * kBlock) adamw_part<T, S8, PROX, LOW, true>(it, part, a, R);
     else if (it.n > part * 4 * kBlock) adamw_part<T, S8, PROX, LOW, false>(it, part, a, R);
 }
