@@ -774,7 +774,8 @@ int hsadmm_gradient_norms(const hsadmm_plan_t* plan, const void* const* G, int32
  *     decay = 1 - lr weight_decay,  step_size = lr / (1 - beta_1^t),  root = 1 / sqrt(1 - beta_2^t)
  * formed in fp64 and rounded once; noise as given.  HOST function; out is HOST memory.  step (t) >= 1 counts the updates
  * including this one.
- * Errors: INVALID_ARGUMENT (nothing is written): lr or weight_decay negative or not finite, a beta outside [0, 1), step < 1.
+ * Errors: INVALID_ARGUMENT (nothing is written): lr or weight_decay negative or not finite, a beta outside [0, 1), step < 1,
+ * a result beyond fp32's range.
  */
 typedef struct {
     float decay;

@@ -2034,9 +2034,13 @@ int hsadmm_adamw_coefficients(double lr, double beta_one, double beta_two, doubl
     if (!out || !size(lr) || !size(weight_decay) || !(beta_one >= 0.0 && beta_one < 1.0) ||
         !(beta_two >= 0.0 && beta_two < 1.0) || step < 1)
         return HSADMM_ERR_INVALID_ARGUMENT;
-    out->decay = (float)(1.0 - lr * weight_decay);
-    out->step_size = (float)(lr / (1.0 - std::pow(beta_one, (double)step)));
-    out->root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta_two, (double)step)));
+    const double decay = 1.0 - lr * weight_decay, step_size = lr / (1.0 - std::pow(beta_one, (double)step));
+    const double root = 1.0 / std::sqrt(1.0 - std::pow(beta_two, (double)step));
+    const double most = 3e38;                                               // (within fp32's range)
+    if (!(decay >= -most) || !(step_size <= most) || !(root <= most)) return HSADMM_ERR_INVALID_ARGUMENT;
+    out->decay = (float)decay;
+    out->step_size = (float)step_size;
+    out->root = (float)root;
     out->noise = noise;
     return HSADMM_OK;
 }

@@ -245,6 +245,7 @@ __device__ __forceinline__ unsigned int top_bits(const v4f& v)
 // The root of x >= 0 to nearest, but for about one value in a million that lies next to the middle of two: the machine's
 // reciprocal root and one correction of x times it.  (Codes are cut from the root and the moments: a result that differs by
 // one unit in the last place from the operation's own rounding moves a code in every millionth case, this one hardly ever.)
+// Below fp32's normal range, where x itself has few bits left, the result is not zero but too small.
 __device__ __forceinline__ float root_of(float x)
 {
     const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f));

@@ -53,7 +53,8 @@ def test_coefficients_against_exact_arithmetic():
         assert noise == 0xFFFFFFFF
     for bad in ((-1e-3, 0.9, 0.999, 0, 1), (float("nan"), 0.9, 0.999, 0, 1), (float("inf"), 0.9, 0.999, 0, 1),
                 (1e-3, 1.0, 0.999, 0, 1), (1e-3, -0.1, 0.999, 0, 1), (1e-3, 0.9, 1.0, 0, 1), (1e-3, 0.9, float("nan"), 0, 1),
-                (1e-3, 0.9, 0.999, -1, 1), (1e-3, 0.9, 0.999, 0, 0), (1e-3, 0.9, 0.999, 0, -5)):
+                (1e-3, 0.9, 0.999, -1, 1), (1e-3, 0.9, 0.999, 0, 0), (1e-3, 0.9, 0.999, 0, -5), (1e39, 0.9, 0.999, 0, 1),
+                (1e25, 1 - 2.0 ** -53, 0.999, 0, 1), (1e30, 0.9, 0.999, 1e30, 1)):
         with pytest.raises(pkg.HsadmmError) as e:
             pkg.hsadmm_adamw_coefficients(*bad)
         assert e.value.code == -1
