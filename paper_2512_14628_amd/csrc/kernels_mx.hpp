@@ -11,11 +11,12 @@ namespace {
 
 constexpr int kMxBlock = 32;
 
-// j / d for the unsigned numbers a layer's positions are (see DivKhw).
+// j / d for the unsigned numbers a layer's positions are (see DivKhw; below 2^22 the machine's own reciprocal is near enough for the
+// same single step of correction).
 struct DivPos {
     unsigned int d;
     float rcp;
-    __device__ __forceinline__ explicit DivPos(unsigned int x) : d(x), rcp(1.0f / (float)x) {}
+    __device__ __forceinline__ explicit DivPos(unsigned int x) : d(x), rcp(__builtin_amdgcn_rcpf((float)x)) {}
     __device__ __forceinline__ unsigned int operator()(unsigned int j) const
     {
         if (j >= (1u << 22)) return j / d;
@@ -86,12 +87,13 @@ __device__ __forceinline__ int layer_at(const int64_t* __restrict__ layer_off, i
 // takes them one after the other (a block of 32 is one layer's).  The grid is what the plan's own selection packs; a mask that
 // keeps more has every workgroup take several tiles.  Bound by the latency of a tile's chain of loads (offsets, layer, kept row or
 // column, values) and, on large networks, by the lines that hold kept elements.  Measured (values from three states in turn, us):
-//   a workgroup per stretch of the layer, kept or not    ResNet-50 at 0.4, z + v: 33.3, packed tiles 27.6 (Q = 2), 24.7 (Q = 4: 92 MB,
-//                                                        3.7 TB/s; kMxWide says where which)
+//   a workgroup per stretch of the layer, kept or not    ResNet-50 at 0.4, z + v: 33.3, packed tiles 27.6 (Q = 2), 24.7 (Q = 4;
+//                                                        kMxWide says where which), now 23.3: 92 MB, 4.4 TB/s with a launch's 3 us
 //   eight adjacent positions to a lane                   34.3: a wave's load takes every other 16 bytes and lines are fetched twice
 //   Q = 4 with all the registers it would take (111)     28.0: four waves a SIMD instead of six
-//   columns, a position to a lane through LDS            ResNet-152, channels at 0.3: 113 without, 60.6, non-temporal loads 56.0
-//                                                        (214 MB fetched for 70 MB kept: most lines hold a kept channel, 4.2 TB/s)
+//   no look-up of the kept row, no division (a probe)    2.4 less: the chain of loads
+//   columns, a position to a lane through LDS            ResNet-152, channels at 0.3: 113 without, 60.6, non-temporal loads 55.0, now
+//                                                        52.6 (214 MB fetched for 70 MB kept: most lines hold a kept channel)
 //   columns, rows read whole and kept elements put       133: a look-up of its place for every element, kept or not
 //   into LDS at their places
 template <int FMT, bool SUM, int Q>
@@ -135,7 +137,9 @@ __global__ __launch_bounds__(kBlock, 6) void gather_mx(const DevLayer* __restric
                 // (places up to the end of the layer's last block: the next layer starts behind it)
                 const int64_t g = t0 + at;
                 if (at >= lead && at < kTile && ((unsigned int)(at - lead) & ~(unsigned int)(kMxBlock - 1)) < there) {
-                    if (FMT == HSADMM_MX_FP8) *reinterpret_cast<unsigned int*>(codes + g) = code;
+                    // (non-temporal / ordinary, us: fp8, a line of codes to half a wave, 23.3 / 24.7 and 52.6 / 55.0 below; fp4, a
+                    // line to a wave, the exchange of four nodes with both constraints 113.9 / 110.4)
+                    if (FMT == HSADMM_MX_FP8) __builtin_nontemporal_store(code, reinterpret_cast<unsigned int*>(codes + g));
                     else *reinterpret_cast<uint16_t*>(codes + (g >> 1)) = (uint16_t)code;
                     if ((threadIdx.x & 7) == 0) scales[g / kMxBlock] = (uint8_t)byte;
                 }
