@@ -10,6 +10,7 @@
 namespace {
 
 constexpr int kMxBlock = 32;
+struct __attribute__((aligned(4))) int4_at4 { int x, y, z, w; };      // four ints at any int's address
 
 // j / d for the unsigned numbers a layer's positions are (see DivKhw; below 2^22 the machine's own reciprocal is near enough for the
 // same single step of correction).
@@ -283,24 +284,32 @@ __device__ __forceinline__ v4f mx_mean4(const MxBuffers& b, int M, float inv_M, 
     return z * inv_M;
 }
 
-// Smallest of the workgroup's values, in every thread; `red`: kWaves words.
-__device__ __forceinline__ unsigned int block_umin(unsigned int x, unsigned int* red)
+// Smallest `lo` and largest `hi` of the workgroup, in every thread; `red`: two rows of kWaves words.
+__device__ __forceinline__ void block_range(unsigned int& lo, unsigned int& hi, unsigned int (&red)[2][kWaves])
 {
-    x = ~wave_umax(~x);
-    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = x;
+    lo = ~wave_umax(~lo);
+    hi = wave_umax(hi);
+    if ((threadIdx.x & (kWave - 1)) == 0) { red[0][threadIdx.x / kWave] = lo; red[1][threadIdx.x / kWave] = hi; }
     __syncthreads();
-    return min(min(red[0], red[1]), min(red[2], red[3]));
+    lo = min(min(red[0][0], red[0][1]), min(red[0][2], red[0][3]));
+    hi = max(max(red[1][0], red[1][1]), max(red[1][2], red[1][3]));
 }
 
 // dst <- the mean of M buffers on the kept elements, +0 elsewhere; DUAL: Vd <- Vd + (Zi - dst).  A workgroup takes a part
 // of a flat item, a thread fours of adjacent elements.  Fours of rows that are packed whole and in whole words come straight from the
 // buffers.  Other rows' elements (columns of a row, rows that start anywhere) have their places in one stretch of packed
 // positions: the workgroup finds where it starts and ends, decodes it in order into LDS, a code once, and picks from there.
-// (An element at a time out of the buffers / this way, us: ResNet-50, both constraints, four nodes in fp4 113.0 / 82.7, with every
-// wave there is 77.8; ResNet-18 of width 45, filters, two nodes in fp8 9.7 / 8.9.)  Bound by HBM: ResNet-50, filters, eight nodes in fp8, with the dual update 502 MB
-// in 80.8 us, 6.2 TB/s.
+// An element's row, channel and column follow from the one before it; a four that lies in one row looks its row up once.
+// Bound by HBM where rows are whole (ResNet-50, filters, eight nodes in fp8, with the dual update: 502 MB in 78.5 us, 6.4 TB/s), by the
+// places' arithmetic and the three loads one after the other where they are not.  Measured, us:
+//   an element at a time out of the buffers     ResNet-50, both constraints, four nodes in fp4: 113.0, this way 82.7, with every wave
+//                                               there is 77.8; ResNet-18 of width 45, filters, two nodes in fp8: 9.7 / 8.9
+//   two divisions for every element             basic 3-3-1-2 of width 120, channels, three nodes in fp4: 61.5, step by step 46.5,
+//                                               whole fours 44.0; ResNet-50, channels, one node in fp8: 36.8, 30.4, 26.9
+//   seven / eight waves a SIMD                  with the dual update 103.0 / 105.5 (writing and reading, as above), 78.5 / 79.2;
+//                                               without 46.1 / 43.6, 41.1 / 37.8 (ResNet-18 of width 125, filters), 22.0 / 20.5
 template <int FMT, bool DUAL>
-__global__ __launch_bounds__(kBlock, 8) void scatter_mx(const FlatItem* __restrict__ items, const DevLayer* __restrict__ layers,
+__global__ __launch_bounds__(kBlock, DUAL ? 7 : 8) void scatter_mx(const FlatItem* __restrict__ items, const DevLayer* __restrict__ layers,
                                                      MxBuffers b, int M, float inv_M, MxMaps mp, float* __restrict__ dst,
                                                      const float* __restrict__ Zi, float* __restrict__ Vd)
 {
@@ -346,28 +355,61 @@ __global__ __launch_bounds__(kBlock, 8) void scatter_mx(const FlatItem* __restri
     } else {
         constexpr unsigned int kNone = 0xffffffffu;
         unsigned int k[kFlatQuads][4], first = kNone, last = 0;
+        // kColumns: channels are kept, each a run of khw columns (kRuns: of more than one); kWhole: a four lies in one row
+        auto places = [&](auto with_columns, auto with_runs, auto whole) {
+            constexpr bool kColumns = decltype(with_columns)::value, kRuns = decltype(with_runs)::value;
+            constexpr bool kWhole = decltype(whole)::value;
+            unsigned int row[kFlatQuads][4], add[kFlatQuads][4];
+            int pc[kFlatQuads][4], pr[kFlatQuads][4];
 #pragma unroll
-        for (int h = 0; h < kFlatQuads; ++h) {
-            const int q = 4 * (threadIdx.x + h * kBlock);
-            const unsigned int dr = by_row(c0 + min(q, it.n - 1));
-            unsigned int row = r0 + dr, c = c0 + min(q, it.n - 1) - dr * row_len;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                k[h][e] = kNone;
-                if (q + e >= it.n) continue;
-                const int p = row_pos ? row_pos[row] : (int)row;
-                const unsigned int ch = !channels || khw == 1 ? c : by_khw(c);
-                const int pc = channels ? col_pos[ch] : (int)c;
-                if (p >= 0 && pc >= 0) {
-                    k[h][e] = (unsigned int)p * in_len + (channels ? (unsigned int)pc * khw + (c - ch * khw) : c);
-                    first = min(first, k[h][e]);
-                    last = max(last, k[h][e]);
+            for (int h = 0; h < kFlatQuads; ++h) {
+                // row, channel and column in the channel of the four's first element; the others follow step by step
+                const unsigned int q = (unsigned int)min(4 * (int)(threadIdx.x + h * kBlock), kWhole ? it.n - 4 : it.n - 1);
+                const unsigned int dr = by_row(c0 + q);
+                unsigned int r = r0 + dr, ch = c0 + q - dr * row_len, t = 0;
+                if (kRuns) { t = ch; ch = by_khw(ch); t -= ch * khw; }
+                const unsigned int width = kColumns ? (unsigned int)L.c_in : row_len;
+                if (kWhole && kColumns && !kRuns) {
+                    const int4_at4 v = *reinterpret_cast<const int4_at4*>(col_pos + ch);
+                    pc[h][0] = v.x; pc[h][1] = v.y; pc[h][2] = v.z; pc[h][3] = v.w;
                 }
-                if (++c == row_len) { c = 0; ++row; }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool in = kWhole || (int)q + e < it.n;     // (else the four's first element's look-ups again)
+                    row[h][e] = in ? r : row[h][0];
+                    add[h][e] = kRuns ? t : kColumns ? 0u : ch;
+                    if (!kColumns) pc[h][e] = 0;
+                    else if (!kWhole || kRuns) pc[h][e] = col_pos[in ? ch : 0u];
+                    if (!kRuns || ++t == khw) {
+                        t = 0;
+                        if (++ch == width && !kWhole) { ch = 0; ++r; }
+                    }
+                }
             }
-        }
-        first = block_umin(first, red[0]);
-        last = ~block_umin(~last, red[1]);
+#pragma unroll
+            for (int h = 0; h < kFlatQuads; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    pr[h][e] = !row_pos ? (int)row[h][e] : kWhole && e > 0 ? pr[h][0] : row_pos[row[h][e]];
+#pragma unroll
+            for (int h = 0; h < kFlatQuads; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool on = 4 * (int)(threadIdx.x + h * kBlock) + e < it.n && pr[h][e] >= 0 && pc[h][e] >= 0;
+                    const unsigned int at = (unsigned int)pr[h][e] * in_len +
+                                            (kRuns ? (unsigned int)pc[h][e] * khw : (unsigned int)pc[h][e]) + add[h][e];
+                    k[h][e] = on ? at : kNone;
+                    first = min(first, k[h][e]);
+                    last = max(last, on ? at : 0u);
+                }
+        };
+        const std::true_type yes{};
+        const std::false_type no{};
+        const bool fours = (row_len & 3) == 0;
+        if (!channels) places(no, no, no);
+        else if (khw == 1) fours ? places(yes, no, yes) : places(yes, no, no);
+        else fours ? places(yes, yes, yes) : places(yes, yes, no);
+        block_range(first, last, red);
         const unsigned int from = first & ~(unsigned int)(kMxBlock - 1);
         if (first != kNone)
             for (unsigned int o = 4 * threadIdx.x; from + o <= last; o += 4 * kBlock)
