@@ -42,6 +42,10 @@
 //                   retraining-phase iteration whose kernels also sum the squared residuals of Section 3.4
 //                   (hsadmm_retrain_project, hsadmm_retrain_expand)
 //
+//   gradient_sqsums / gradient_norm_finish, adamw_kernel   the replicas' training between two steps, Eq. (7) with AdamW
+//   gather_mx / scatter_mx   compact_gather into, and expand_scatter out of, blocks of 32 codes with a shared power of two; the second
+//                   takes the mean of several nodes' buffers and the dual update of Eq. (13) with it
+//
 // Nothing here is a dense contraction, so no MFMA is used; every kernel is bound by HBM traffic.
 // Arena data is touched once per kernel, so it is moved with non-temporal 128-bit accesses.
 // fp32 arithmetic is compiled without contraction (-ffp-contract=off); the fp64 accumulation
@@ -146,7 +150,7 @@ struct hsadmm_plan {
     std::vector<WorkItem> items_chan;   // channel_final: the row items of the CHANNEL layers (a subset of items_rows)
     std::vector<WorkItem> items_both;   // composite_colsums: tiles of the layers under both constraints
     std::vector<int32_t> both_layers;   // their indices
-    std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, gather_mx, scatter_mx: every layer cut without regard to rows
+    std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, scatter_mx: every layer cut without regard to rows
     int64_t packed_elems = 0;           // what the plan's own selection packs
     int64_t state_blocks = 0;           // blocks that share a scale in 8-bit optimizer states
     int32_t n_segments = 0;             // scan segments (one per layer, two per BOTH layer)
