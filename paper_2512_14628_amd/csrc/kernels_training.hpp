@@ -195,7 +195,8 @@ __device__ __forceinline__ unsigned int mix_four(unsigned int x)
     return x ^ (x >> 15);
 }
 
-// Codes of four values y (already in units of the scale): rounded stochastically to e4m3, |y| <= 448.
+// Codes of four values y (already in units of the scale): rounded stochastically to e4m3, |y| <= 448.  (To nearest, a state that moves
+// by less than half a code a step, as every root under beta_2 = 0.999 does, would not move at all.)
 __device__ __forceinline__ unsigned int encode4(const v4f& y, unsigned int mix)
 {
     int c = 0;
@@ -245,16 +246,18 @@ __device__ __forceinline__ unsigned int top_bits(const v4f& v)
 // The root of x >= 0 to nearest, but for about one value in a million that lies next to the middle of two: the machine's
 // reciprocal root and one correction of x times it.  (Codes are cut from the root and the moments: a result that differs by
 // one unit in the last place from the operation's own rounding moves a code in every millionth case, this one hardly ever.)
-// Below fp32's normal range, where x itself has few bits left, the result is not zero but too small.
+// Below fp32's normal range, where x itself has few bits left, the result is not zero but too small; infinity's root is infinity.
 __device__ __forceinline__ float root_of(float x)
 {
     const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f));
     const float s = x * y;
-    return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+    const float r = __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+    return x == __builtin_inff() ? x : r;
 }
 
 // Formulas: see hsadmm_adamw in the header.  Moments are formed in fp32, every operation rounded by itself; the weights' last
 // two operations are fused and the reciprocal before them is the machine's own, within one unit in the last place.
+// The working copy is rounded to nearest: it is read by the forward pass only, the fp32 weights carry what the rounding loses.
 // A workgroup takes 4 * kBlock elements, the `part`-th such stretch of an item, of all replicas in turn, so z_i and u are read once.
 // (Two fours a thread: ResNet-50, 4 replicas, 32-bit states 549 us instead of 543, 8-bit states 333 / 322, four times wider 1061 / 1014.)
 template <int T, bool S8, bool PROX, bool LOW, bool FULL>

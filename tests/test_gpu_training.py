@@ -305,6 +305,46 @@ def test_a_block_with_a_value_that_is_not_finite_shows_it():
     plan.close()
 
 
+def test_a_square_beyond_fp32_stops_its_element_and_no_other():
+    """A finite gradient whose square is not: v is infinite, the step of that element zero, and the weight decays as it would."""
+    wl = workload([(2, 300, 1)])
+    plan = pkg.Plan(wl.table())
+    run = Run(wl, 1, pkg.TYPE_F32, seed=12, prox=False)
+    run.scale.fill_(1.0)
+    run.G[0, 7] = 1e20
+    W = host(run.W)[0].copy()
+    want, tol = run.reference()
+    pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), **run.fields())
+    got = host(run.W)[0]
+    decay = 1 - run.hyper["lr"] * run.hyper["weight_decay"]
+    assert abs(got[7] - W[7] * decay) <= 3 * E * abs(W[7]) and np.isinf(host(run.V)[0, 7])
+    rest = np.flatnonzero(run.on)
+    keep = rest != 7
+    check_close("W", got[rest[keep]], want["W"][0][keep], tol["W"][0][keep])
+    plan.close()
+
+
+def test_launches_of_the_new_calls_are_timed_under_their_names():
+    wl = workload([(40, 33, 9)])
+    plan = pkg.Plan(wl.table(), pack_align_elems=32)
+    run = Run(wl, 1, pkg.TYPE_F32, seed=2, prox=False)
+    ws = torch.zeros(plan.workspace_bytes, dtype=torch.uint8, device=DEV)
+    mask = torch.ones(plan.groups_total, dtype=torch.uint8, device=DEV)
+    codes = torch.zeros(plan.packed_capacity_elems, dtype=torch.uint8, device=DEV)
+    scales = torch.zeros(plan.packed_capacity_elems // 32, dtype=torch.uint8, device=DEV)
+    off, kept = torch.zeros(2, dtype=torch.int64, device=DEV), torch.zeros(40, dtype=torch.int32, device=DEV)
+    dst = torch.zeros(wl.n_arena, device=DEV)
+    pkg.hsadmm_kernel_timing_enable(plan, True)
+    pkg.hsadmm_gradient_norms(plan, list(run.G), 1.0, None, run.scale, ws)
+    pkg.hsadmm_adamw(plan, list(run.W), list(run.G), list(run.M), list(run.V), **run.fields())
+    pkg.hsadmm_compact_mx(plan, run.W[0], None, mask, pkg.MX_FP4, codes, scales, off, kept, ws)
+    pkg.hsadmm_expand_mx(plan, [codes], [scales], pkg.MX_FP4, None, dst, None, None, ws)
+    times = pkg.hsadmm_kernel_timing_read(plan)
+    for name in ("gradient_sqsums", "gradient_norm_finish", "adamw", "gather_mx", "scatter_mx"):
+        assert times[name][1] == 1 and times[name][0] > 0, name
+    plan.close()
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_a_replica_whose_scale_is_not_finite_is_left_as_it_is(bits):
     wl = workload()
