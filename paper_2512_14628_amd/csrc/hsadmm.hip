@@ -735,11 +735,21 @@ struct Stretches {
     }
 };
 
+// Replicas a workgroup of the update takes one after the other.  With the pull all of them share what it read of z_i and u, from
+// kAdamwFull stretches (four workgroups a compute unit) on; smaller plans split them in fours.  Without it they share nothing.  All /
+// 4 / 1 at a time, us: with the pull ResNet-50, 4 replicas, 8-bit states 316 / 315 / 401, ResNet-18, 8 replicas 252 / 266 / 345, of
+// width 16 (0.7 M elements, 32 bits) 44.0 / 39.7 / 44.8, plain of width 64 20.3 / 18.9 / 22.3; without, ResNet-50, 4 replicas 291 /
+// 291 / 278, ResNet-18, 8 replicas, 32 bits 445 / 423 / 419.
+constexpr int64_t kAdamwFull = 4 * 256;
+
 template <int T, bool S8>
 hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool prox, bool low, hipStream_t s)
 {
     const auto go = [&](auto kernel) {
-        return launch(p, kAdamw, kernel, (unsigned)p->items_flat.size() * (kFlatElems / (4 * kBlock)), kBlock, s, (const FlatItem*)p->d_items_flat, a, R);
+        const int64_t stretches = (int64_t)p->items_flat.size() * (kFlatElems / (4 * kBlock));
+        const int each = !prox ? 1 : stretches >= kAdamwFull ? R : std::min(R, 4);
+        return launch(p, kAdamw, kernel, (unsigned)(stretches * ((R + each - 1) / each)), kBlock, s,
+                      (const FlatItem*)p->d_items_flat, a, R, each);
     };
     if constexpr (T != HSADMM_TYPE_F32)
         if (low) return prox ? go(adamw_kernel<T, S8, true, true>) : go(adamw_kernel<T, S8, false, true>);
