@@ -742,14 +742,23 @@ struct Stretches {
 // 291 / 278, ResNet-18, 8 replicas, 32 bits 445 / 423 / 419.
 constexpr int64_t kAdamwFull = 4 * 256;
 
+// Workgroups of one launch: a grid has fewer than 2^32 threads.  Arenas of more than 17 G elements (or fewer, of several replicas) take
+// several launches.
+constexpr int64_t kGridMost = (1ll << 32) / kBlock - 1;
+
 template <int T, bool S8>
 hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool prox, bool low, hipStream_t s)
 {
     const auto go = [&](auto kernel) {
-        const int64_t stretches = (int64_t)p->items_flat.size() * (kFlatElems / (4 * kBlock));
-        const int each = !prox ? 1 : stretches >= kAdamwFull ? R : std::min(R, 4);
-        return launch(p, kAdamw, kernel, (unsigned)(stretches * ((R + each - 1) / each)), kBlock, s,
-                      (const FlatItem*)p->d_items_flat, a, R, each);
+        constexpr int64_t kStretches = kFlatElems / (4 * kBlock);                     // of an item
+        const int64_t items = (int64_t)p->items_flat.size();
+        const int each = !prox ? 1 : items * kStretches >= kAdamwFull ? R : std::min(R, 4);
+        const int64_t groups = (R + each - 1) / each, most = kGridMost / (kStretches * groups);
+        hipError_t e = hipSuccess;
+        for (int64_t i = 0; i < items && e == hipSuccess; i += most)
+            e = launch(p, kAdamw, kernel, (unsigned)(std::min(most, items - i) * kStretches * groups), kBlock, s,
+                       (const FlatItem*)p->d_items_flat + i, a, R, each);
+        return e;
     };
     if constexpr (T != HSADMM_TYPE_F32)
         if (low) return prox ? go(adamw_kernel<T, S8, true, true>) : go(adamw_kernel<T, S8, false, true>);
@@ -2216,8 +2225,13 @@ int hsadmm_expand_mx(const hsadmm_plan_t* p, const uint8_t* const* codes, const 
         if (rc != HSADMM_OK) return rc;
     }
     const auto go = [&](auto kernel) {
-        return launch(p, kScatterMx, kernel, (unsigned)p->items_flat.size() * kParts, kBlock, s, (const FlatItem*)p->d_items_flat,
-                      (const DevLayer*)p->d_layers, b, (int)M, 1.0f / (float)M, mx_maps(p, ws), dst, Zi, Vd);
+        const int64_t items = (int64_t)p->items_flat.size(), most = kGridMost / kParts;
+        hipError_t e = hipSuccess;
+        for (int64_t i = 0; i < items && e == hipSuccess; i += most)
+            e = launch(p, kScatterMx, kernel, (unsigned)(std::min(most, items - i) * kParts), kBlock, s,
+                       (const FlatItem*)p->d_items_flat + i, (const DevLayer*)p->d_layers, b, (int)M, 1.0f / (float)M,
+                       mx_maps(p, ws), dst, Zi, Vd);
+        return e;
     };
     const hipError_t e = format == HSADMM_MX_FP8 ? (Zi ? go(scatter_mx<HSADMM_MX_FP8, true>) : go(scatter_mx<HSADMM_MX_FP8, false>))
                                                  : (Zi ? go(scatter_mx<HSADMM_MX_FP4, true>) : go(scatter_mx<HSADMM_MX_FP4, false>));

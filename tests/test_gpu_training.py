@@ -490,6 +490,43 @@ def test_layers_beyond_four_gibi_elements_of_an_arena():
     small_plan.close()
 
 
+def test_more_elements_than_one_launch_takes():
+    """Nine layers of nearly 2^31 elements, 18 G in all: a grid has fewer than 2^32 threads, so the update takes two launches.
+    Known values in the first and the last elements; the middle is whatever the memory held."""
+    rows, row_len = 65535, 32767
+    n = rows * row_len
+    pitch = n + (-n % 256)
+    L = 9
+    t = {"elem_off": pitch * np.arange(L, dtype=np.int64), "c_out": np.full(L, rows, np.int32),
+         "c_in": np.full(L, row_len, np.int32), "khw": np.ones(L, np.int32), "mode": np.ones(L, np.int32),
+         "k": np.full(L, 5, np.int32)}
+    plan = pkg.Plan(t)
+    total = pitch * (L - 1) + n
+    assert total // 1024 > 2 ** 32 // 256
+    free, _ = torch.cuda.mem_get_info()
+    if free < 10 * total:
+        plan.close()
+        pytest.skip("needs %d GB of free memory" % (10 * total >> 30))
+    W = torch.empty(total, device=DEV)
+    G = torch.empty(total, dtype=torch.bfloat16, device=DEV)
+    M, V = (torch.empty(total, dtype=torch.uint8, device=DEV) for _ in range(2))
+    blocks = pkg.hsadmm_plan_state_blocks(plan)
+    Ms, Vs = (torch.zeros(blocks, device=DEV) for _ in range(2))
+    some = 1000
+    for x, value in ((W, 1.0), (G, 0.5), (M, 0), (V, 0)):
+        x[:some] = value
+        x[-some:] = value
+    pkg.hsadmm_adamw(plan, [W], [G], [M], [V], grad_type=pkg.TYPE_BF16, state_bits=8, M_scale=[Ms], V_scale=[Vs], lr=0.25,
+                     weight_decay=0.5, noise=1)
+    # from zero states the first step is lr times the gradient's sign, next to the decay: 1 - 0.125 - 0.25.  A dozen roundings of
+    # 2 E at most on the way to 0.25 (6 E), eps (2e-8 of it), the result's own
+    for part in (W[:some], W[-some:]):
+        assert float((part - 0.625).abs().max()) < 8 * E
+    del W, G, M, V, Ms, Vs
+    plan.close()
+    torch.cuda.empty_cache()
+
+
 # ------------------------------------------------------------------ norms
 
 @pytest.mark.parametrize("grad_type", [pkg.TYPE_F32, pkg.TYPE_BF16, pkg.TYPE_F16])
