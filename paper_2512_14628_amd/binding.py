@@ -6,10 +6,14 @@ runtime the library links against is the one already in the process.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
+import struct
 import subprocess
 from typing import Optional, Sequence
+
+import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
@@ -104,6 +108,11 @@ class _AdamwArgs(ctypes.Structure):
     _fields_ = list(_ADAMW_FIELDS)
 
 
+# the same structure written at once (native sizes and alignment)
+_ADAMW_PACK = struct.Struct("N3iI12P5dqP")
+_COEF_BYTES = ctypes.sizeof(_AdamwCoef)
+
+
 _lib = None
 
 
@@ -129,7 +138,6 @@ def load_library():
     if not os.path.exists(LIB_PATH):
         raise RuntimeError("libhsadmm.so is missing at %s: build it first "
                            "(python -c 'import __graft_entry__ as g; g.build()')" % LIB_PATH)
-    import torch  # noqa: F401  (brings the HIP runtime into the process first)
     lib = ctypes.CDLL(LIB_PATH)
     vp = ctypes.c_void_p
     lib.hsadmm_plan_create.argtypes = [ctypes.POINTER(_Layer), ctypes.c_int32, ctypes.c_int32,
@@ -231,7 +239,7 @@ def load_library():
     lib.hsadmm_adamw_coefficients.restype = ctypes.c_int
     lib.hsadmm_plan_state_blocks.argtypes = [vp, ctypes.POINTER(ctypes.c_int64)]
     lib.hsadmm_plan_state_blocks.restype = ctypes.c_int
-    lib.hsadmm_adamw.argtypes = [vp, ctypes.POINTER(_AdamwArgs)]
+    lib.hsadmm_adamw.argtypes = [vp, vp]
     lib.hsadmm_adamw.restype = ctypes.c_int
     lib.hsadmm_compact_mx.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.hsadmm_compact_mx.restype = ctypes.c_int
@@ -277,7 +285,6 @@ def _nbytes(x) -> int:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
         return int(torch.cuda.current_stream().cuda_stream) or None
     if isinstance(stream, int):
         return stream or None
@@ -325,6 +332,7 @@ class Plan:
             raise HsadmmError(rc, "hsadmm_plan_sizes")
         self.arena_elems, self.groups_total = a.value, g.value
         self.packed_capacity_elems, self.workspace_bytes = c.value, w.value
+        self.state_blocks = hsadmm_plan_state_blocks(self)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -751,19 +759,69 @@ def hsadmm_expand_dual(plan: Plan, packed, mask, dst, Zi, Vd, workspace, stream=
     return rc
 
 
-def _each(buffers):
-    """HOST array of the device addresses of one buffer per replica or node; None -> NULL."""
-    if buffers is None:
-        return None
-    return (ctypes.c_void_p * max(len(buffers), 1))(*[_ptr(b) for b in buffers])
+class _Unfit(Exception):
+    """A tensor that cannot be the buffer it was given as."""
+
+
+def _fit(buffers, name: str, dtype, elems: int) -> list:
+    """Device addresses of buffers (see _ptr; None -> 0).  Arenas come in several element types, and the library sees addresses
+    only: a tensor has to hold `elems` elements of `dtype` (None: of one byte each) in a row, or kernels would run past its
+    end.  An integer address is the caller's word."""
+    at = []
+    for x in buffers:
+        if x is None:
+            x = 0
+        elif not isinstance(x, int):
+            if ((x.dtype is not dtype and (dtype is not None or x.element_size() != 1)) or x.numel() < elems or
+                    not x.is_contiguous()):
+                raise _Unfit("%s: %s of %s, where %d elements of %s have to lie in a row" % (
+                    name, tuple(x.shape), x.dtype, elems, dtype or "one byte"))
+            x = x.data_ptr()
+        at.append(x)
+    return at
+
+
+def _fit_bytes(x, name: str, nbytes: int) -> int:
+    """Address of a buffer of that many bytes, whatever a tensor's type."""
+    if isinstance(x, int):
+        return x
+    if _nbytes(x) < nbytes or not x.is_contiguous():
+        raise _Unfit("%s: %s of %s, where %d bytes have to lie in a row" % (name, tuple(x.shape), x.dtype, nbytes))
+    return x.data_ptr()
+
+
+def _refused(what: str, why: _Unfit, check: bool) -> int:
+    """INVALID_ARGUMENT, as the library itself would have it."""
+    if check:
+        raise HsadmmError(-1, "%s (%s)" % (what, why))
+    return -1
+
+
+_F32 = torch.float32
+_GRAD_DTYPES = {TYPE_F32: _F32, TYPE_BF16: torch.bfloat16, TYPE_F16: torch.float16}
+
+
+def _addresses(at):
+    """HOST array of addresses."""
+    return (_vp * max(len(at), 1))(*at)
 
 
 def hsadmm_gradient_norms(plan: Plan, G: Sequence, max_norm: float, norm, scale, workspace, grad_type: int = TYPE_F32,
                           stream=None, workspace_bytes: Optional[int] = None, check: bool = True) -> int:
-    """Norms of the replicas' gradients and the factors that clip them (NaN: not finite); either output may be None."""
+    """Norms of the replicas' gradients and the factors that clip them (NaN: not finite); either output may be None.  Tensors
+    of another type than grad_type, or too short, are refused (INVALID_ARGUMENT)."""
+    R, grad = len(G), _GRAD_DTYPES.get(grad_type)
+    if R > MAX_REPLICAS or grad is None:                      # (the library refuses these as such)
+        at, norm_at, scale_at = [_ptr(g) for g in G], _ptr(norm), _ptr(scale)
+    else:
+        try:
+            at = _fit(G, "G", grad, plan.arena_elems)
+            norm_at, scale_at = _fit((norm,), "norm", torch.float64, R)[0], _fit((scale,), "scale", _F32, R)[0]
+        except _Unfit as why:
+            return _refused("hsadmm_gradient_norms", why, check)
     wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
-    rc = load_library().hsadmm_gradient_norms(plan.handle, _each(G), len(G), int(grad_type), float(max_norm), _ptr(norm),
-                                              _ptr(scale), _ptr(workspace), wb, _stream(stream))
+    rc = load_library().hsadmm_gradient_norms(plan.handle, _addresses(at), R, int(grad_type), float(max_norm), norm_at,
+                                              scale_at, _ptr(workspace), wb, _stream(stream))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_gradient_norms")
     return rc
@@ -796,25 +854,40 @@ def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence,
                  beta_one: float = 0.9, beta_two: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
                  step: int = 1, noise: int = 0, stream=None, check: bool = True) -> int:
     """One AdamW step of every layer of every replica.  W, G, M, V (and M_scale, V_scale, W_low where they are given): one
-    buffer per replica; the other arguments are the fields of hsadmm_adamw_args_t."""
-    R = len(W)
-    at, places = [], []                     # one HOST array for all lists, and where each of them starts in it
-    for name, buffers in (("W", W), ("G", G), ("M", M), ("V", V), ("M_scale", M_scale), ("V_scale", V_scale),
-                          ("W_low", W_low)):
-        if buffers is None:
-            places.append(None)
-            continue
-        if len(buffers) != R:
-            raise ValueError("hsadmm_adamw: %d buffers in %s, %d replicas" % (len(buffers), name, R))
-        places.append(len(at))
-        at += [_ptr(b) for b in buffers]
-    array = (_vp * max(len(at), 1))(*at)
-    first = ctypes.addressof(array)
-    args = _AdamwArgs(ctypes.sizeof(_AdamwArgs), R, grad_type, state_bits, noise & 0xFFFFFFFF,
-                      *[None if p is None else first + ctypes.sizeof(_vp) * p for p in places],
-                      _ptr(Z), _ptr(U), _ptr(rho), _ptr(grad_scale), _ptr(coef), lr, beta_one, beta_two, eps, weight_decay,
-                      step, _stream(stream))
-    rc = load_library().hsadmm_adamw(plan.handle, ctypes.byref(args))
+    buffer per replica; the other arguments are the fields of hsadmm_adamw_args_t.  Tensors of other types than grad_type
+    and state_bits say, or too short, are refused (INVALID_ARGUMENT)."""
+    R, n, grad = len(W), plan.arena_elems, _GRAD_DTYPES.get(grad_type)
+    fit = _fit
+    if R > MAX_REPLICAS or grad is None or (state_bits != 32 and state_bits != 8):       # (the library refuses these as such)
+        fit = lambda buffers, *_: [_ptr(x) or 0 for x in buffers]        # noqa: E731
+    state = _F32 if state_bits != 8 else None
+    lists = [("W", W, _F32, n), ("G", G, grad, n), ("M", M, state, n), ("V", V, state, n)]
+    if M_scale is not None or V_scale is not None or W_low is not None:
+        lists += [("M_scale", M_scale, _F32, plan.state_blocks), ("V_scale", V_scale, _F32, plan.state_blocks),
+                  ("W_low", W_low, grad, n)]
+    at, places = array.array("Q"), []       # one HOST array for all lists, and where each of them starts in it
+    try:
+        for name, buffers, dtype, elems in lists:
+            if buffers is None:
+                places.append(None)
+                continue
+            if len(buffers) != R:
+                raise ValueError("hsadmm_adamw: %d buffers in %s, %d replicas" % (len(buffers), name, R))
+            places.append(8 * len(at))
+            at.extend(fit(buffers, name, dtype, elems))
+        first = at.buffer_info()[0]
+        fields = [0 if place is None else first + place for place in places] + [0] * (7 - len(places))
+        if Z is not None or U is not None or rho is not None:
+            fields += fit((Z, U), "Z, U", _F32, n) + fit((rho,), "rho", _F32, plan.n_layers)
+        else:
+            fields += (0, 0, 0)
+        fields += fit((grad_scale,), "grad_scale", _F32, R)
+        fields.append(0 if coef is None else _fit_bytes(coef, "coef", _COEF_BYTES))
+    except _Unfit as why:
+        return _refused("hsadmm_adamw", why, check)
+    args = _ADAMW_PACK.pack(_ADAMW_PACK.size, R, grad_type, state_bits, noise & 0xFFFFFFFF, *fields, lr, beta_one, beta_two, eps,
+                            weight_decay, step, _stream(stream) or 0)
+    rc = load_library().hsadmm_adamw(plan.handle, args)
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_adamw")
     return rc
@@ -822,11 +895,17 @@ def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence,
 
 def hsadmm_compact_mx(plan: Plan, src0, src1, mask, format: int, codes, scales, layer_off, kept_idx, workspace, stream=None,
                       workspace_bytes: Optional[int] = None, check: bool = True) -> int:
-    """hsadmm_compact (src1 None) or hsadmm_compact_sum into codes of MX_FP8 or MX_FP4 and a scale byte per 32 of them."""
+    """hsadmm_compact (src1 None) or hsadmm_compact_sum into codes of MX_FP8 or MX_FP4 and a scale byte per 32 of them.  Tensors
+    of other types, or arenas too short, are refused (INVALID_ARGUMENT); codes and scales have to have room for what the mask
+    keeps, which only the caller knows."""
+    try:
+        src = _fit((src0, src1), "src0, src1", _F32, plan.arena_elems)
+        out = _fit((codes, scales), "codes, scales", None, 0)
+    except _Unfit as why:
+        return _refused("hsadmm_compact_mx", why, check)
     wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
-    rc = load_library().hsadmm_compact_mx(plan.handle, _ptr(src0), _ptr(src1), _ptr(mask), int(format), _ptr(codes),
-                                          _ptr(scales), _ptr(layer_off), _ptr(kept_idx), _ptr(workspace), wb,
-                                          _stream(stream))
+    rc = load_library().hsadmm_compact_mx(plan.handle, src[0], src[1], _ptr(mask), int(format), out[0], out[1], _ptr(layer_off),
+                                          _ptr(kept_idx), _ptr(workspace), wb, _stream(stream))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_compact_mx")
     return rc
@@ -834,12 +913,18 @@ def hsadmm_compact_mx(plan: Plan, src0, src1, mask, format: int, codes, scales, 
 
 def hsadmm_expand_mx(plan: Plan, codes: Sequence, scales: Sequence, format: int, mask, dst, Zi, Vd, workspace, stream=None,
                      workspace_bytes: Optional[int] = None, check: bool = True) -> int:
-    """The mean of the nodes' quantised buffers, scattered to full layout; with Zi and Vd also Vd <- Vd + (Zi - dst)."""
+    """The mean of the nodes' quantised buffers, scattered to full layout; with Zi and Vd also Vd <- Vd + (Zi - dst).  Tensors
+    of other types, or arenas too short, are refused (INVALID_ARGUMENT)."""
     if len(codes) != len(scales):
         raise ValueError("hsadmm_expand_mx: %d buffers of codes, %d of scales" % (len(codes), len(scales)))
+    try:
+        codes_at, scales_at = _fit(codes, "codes", None, 0), _fit(scales, "scales", None, 0)
+        full = _fit((dst, Zi, Vd), "dst, Zi, Vd", _F32, plan.arena_elems)
+    except _Unfit as why:
+        return _refused("hsadmm_expand_mx", why, check)
     wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
-    rc = load_library().hsadmm_expand_mx(plan.handle, _each(codes), _each(scales), len(codes), int(format), _ptr(mask),
-                                         _ptr(dst), _ptr(Zi), _ptr(Vd), _ptr(workspace), wb, _stream(stream))
+    rc = load_library().hsadmm_expand_mx(plan.handle, _addresses(codes_at), _addresses(scales_at), len(codes), int(format),
+                                         _ptr(mask), full[0], full[1], full[2], _ptr(workspace), wb, _stream(stream))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_expand_mx")
     return rc
