@@ -920,9 +920,14 @@ int hsadmm_version(void);
  * timestamps; nothing else is put on the stream (such launches cannot be
  * captured into a graph).  At most 8192
  * launches are recorded between two reads; later launches run untimed.
- * hsadmm_kernel_timing_read waits for the recorded kernels, returns for every
- * kernel id 0..HSADMM_KERNEL_COUNT-1 the summed duration in milliseconds and
- * the number of launches, and clears the record.  This record is the only
+ * hsadmm_kernel_timing_read_n waits for the recorded kernels, returns for every
+ * kernel id 0..n-1 the summed duration in milliseconds and the number of
+ * launches (0 for ids that no kernel has), and clears the record.  n is the
+ * length of the caller's arrays: the number of kernels grows from version to
+ * version.  hsadmm_kernel_timing_read is the same with HSADMM_KERNEL_COUNT
+ * entries, as the program that calls it was compiled; the function of that
+ * name, which programs compiled before 2.3 call, fills the 29 entries that
+ * 2.1 had, however many there are now.  This record is the only
  * part of a plan that changes after its creation: launches made from several
  * host threads claim their event pairs atomically, but enabling and reading
  * must not run while another thread is inside a call on this plan.  Off by
@@ -934,7 +939,10 @@ int hsadmm_version(void);
  */
 #define HSADMM_KERNEL_COUNT 34
 int hsadmm_kernel_timing_enable(hsadmm_plan_t* plan, int enable);
+int hsadmm_kernel_timing_read_n(hsadmm_plan_t* plan, double* total_ms, int64_t* launches, int32_t n);
 int hsadmm_kernel_timing_read(hsadmm_plan_t* plan, double* total_ms, int64_t* launches);
+#define hsadmm_kernel_timing_read(plan, total_ms, launches) \
+    hsadmm_kernel_timing_read_n(plan, total_ms, launches, HSADMM_KERNEL_COUNT)
 int hsadmm_kernel_grid(const hsadmm_plan_t* plan, int kernel_id);
 /*
  * 1 if the un-predicted projection of this plan (hsadmm_project, hsadmm_project_compact, hsadmm_step without sel_prev,

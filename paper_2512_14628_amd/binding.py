@@ -35,7 +35,7 @@ HIPCC_FLAGS = [
 
 EXPORTS = ("hsadmm_plan_create", "hsadmm_plan_destroy", "hsadmm_plan_sizes", "hsadmm_project",
            "hsadmm_compact", "hsadmm_expand", "hsadmm_strerror", "hsadmm_version",
-           "hsadmm_kernel_timing_enable", "hsadmm_kernel_timing_read", "hsadmm_kernel_name",
+           "hsadmm_kernel_timing_enable", "hsadmm_kernel_timing_read", "hsadmm_kernel_timing_read_n", "hsadmm_kernel_name",
            "hsadmm_project_frozen", "hsadmm_mask_or", "hsadmm_compact_sum", "hsadmm_node_coefficients",
            "hsadmm_plan_set_node_weights", "hsadmm_project_weighted", "hsadmm_dual_inter", "hsadmm_residuals",
            "hsadmm_average", "hsadmm_mask_drift", "hsadmm_expand_dual", "hsadmm_project_compact",
@@ -225,6 +225,9 @@ def load_library():
     lib.hsadmm_kernel_timing_enable.restype = ctypes.c_int
     lib.hsadmm_kernel_timing_read.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)]
     lib.hsadmm_kernel_timing_read.restype = ctypes.c_int
+    lib.hsadmm_kernel_timing_read_n.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64),
+                                                ctypes.c_int32]
+    lib.hsadmm_kernel_timing_read_n.restype = ctypes.c_int
     lib.hsadmm_layer_sqnorms.argtypes = [vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.hsadmm_layer_sqnorms.restype = ctypes.c_int
     lib.hsadmm_stopping_test.argtypes = [ctypes.POINTER(ctypes.c_int64), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
@@ -357,7 +360,7 @@ def hsadmm_kernel_timing_read(plan: Plan):
     lib = load_library()
     ms = (ctypes.c_double * KERNEL_COUNT)()
     cnt = (ctypes.c_int64 * KERNEL_COUNT)()
-    rc = lib.hsadmm_kernel_timing_read(plan.handle, ms, cnt)
+    rc = lib.hsadmm_kernel_timing_read_n(plan.handle, ms, cnt, KERNEL_COUNT)
     if rc != 0:
         raise HsadmmError(rc, "hsadmm_kernel_timing_read")
     return {lib.hsadmm_kernel_name(i).decode(): (float(ms[i]), int(cnt[i])) for i in range(KERNEL_COUNT)}
