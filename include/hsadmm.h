@@ -772,8 +772,8 @@ int hsadmm_gradient_norms(const hsadmm_plan_t* plan, const void* const* G, int32
 /*
  * The scalars of an AdamW step (decoupled weight decay) that change from step to step:
  *     decay = 1 - lr weight_decay,  step_size = lr / (1 - beta_1^t),  root = 1 / sqrt(1 - beta_2^t)
- * formed in fp64 and rounded once; noise as given.  HOST function; out is HOST memory.  step (t) >= 1 counts the updates
- * including this one.
+ * formed in fp64 and rounded once; noise as given, or where it is 0 a number taken from step.  HOST function; out is HOST
+ * memory.  step (t) >= 1 counts the updates including this one.
  * Errors: INVALID_ARGUMENT (nothing is written): lr or weight_decay negative or not finite, a beta outside [0, 1), step < 1,
  * a result beyond fp32's range.
  */
@@ -781,7 +781,7 @@ typedef struct {
     float decay;
     float step_size;
     float root;
-    uint32_t noise;    /* 8-bit states: a number that differs from step to step (any sequence, e.g. a counter's hash) */
+    uint32_t noise;    /* 8-bit states: a number that differs from step to step (hsadmm_adamw_coefficients gives one) */
 } hsadmm_adamw_coef_t;
 
 int hsadmm_adamw_coefficients(double lr, double beta_one, double beta_two, double weight_decay, int64_t step,
@@ -819,7 +819,9 @@ int hsadmm_plan_state_blocks(const hsadmm_plan_t* plan, int64_t* blocks);
  *   grad_scale       in, optional, R floats (hsadmm_gradient_norms); a replica whose factor is not finite is left untouched
  *   coef             in, optional, DEVICE: takes the place of lr, weight_decay, step and noise (hsadmm_adamw_coefficients).
  *                    Read by the kernel when it runs, so a captured graph follows the buffer's contents from replay to replay.
- *   lr, beta_one, beta_two, eps, weight_decay, step, noise   as in hsadmm_adamw_coefficients; eps >= 2^-126
+ *   lr, beta_one, beta_two, eps, weight_decay, step, noise   as in hsadmm_adamw_coefficients; eps >= 2^-126.  noise: 0 (a number
+ *                    taken from step), or any sequence that differs from step to step, e.g. a counter's hash: with one number
+ *                    for every step an element's rounding would be a fixed threshold and its second moment drift
  *
  * 8-bit states.  A block's scale is its largest |m| (root) / 448, after the update; the update itself uses the unrounded
  * moments.  Codes are rounded stochastically, so a moment that moves by less than a code a step still moves on average (to

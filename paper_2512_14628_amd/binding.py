@@ -833,7 +833,7 @@ def hsadmm_gradient_norms(plan: Plan, G: Sequence, max_norm: float, norm, scale,
 def hsadmm_adamw_coefficients(lr: float, beta_one: float, beta_two: float, weight_decay: float, step: int,
                               noise: int = 0):
     """(decay, step_size, root, noise) of an AdamW step; as bytes on the device (three floats, one uint32) they are
-    hsadmm_adamw's `coef`."""
+    hsadmm_adamw's `coef`.  noise 0: a number taken from step."""
     out = _AdamwCoef()
     rc = load_library().hsadmm_adamw_coefficients(float(lr), float(beta_one), float(beta_two), float(weight_decay),
                                                   int(step), int(noise) & 0xFFFFFFFF, ctypes.byref(out))
@@ -857,7 +857,9 @@ def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence,
                  beta_one: float = 0.9, beta_two: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
                  step: int = 1, noise: int = 0, stream=None, check: bool = True) -> int:
     """One AdamW step of every layer of every replica.  W, G, M, V (and M_scale, V_scale, W_low where they are given): one
-    buffer per replica; the other arguments are the fields of hsadmm_adamw_args_t.  Tensors of other types than grad_type
+    buffer per replica; the other arguments are the fields of hsadmm_adamw_args_t.  With 8-bit states
+    codes are rounded with numbers made of `noise`, or of `step` where noise is 0: one of them has to differ from step to step
+    (or `coef`, which holds both).  Tensors of other types than grad_type
     and state_bits say, or too short, are refused (INVALID_ARGUMENT)."""
     R, n, grad = len(W), plan.arena_elems, _GRAD_DTYPES.get(grad_type)
     fit = _fit

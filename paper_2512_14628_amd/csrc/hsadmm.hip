@@ -2064,7 +2064,9 @@ int hsadmm_adamw_coefficients(double lr, double beta_one, double beta_two, doubl
     out->decay = (float)decay;
     out->step_size = (float)step_size;
     out->root = (float)root;
-    out->noise = noise;
+    // (no number given: a fraction of the golden ratio's multiples, so that steps which follow each other differ in every bit.  With
+    // one number for all steps an element's rounding would be a fixed threshold, and a second moment settle at twice its value.)
+    out->noise = noise ? noise : (uint32_t)(((uint64_t)step * 0x9E3779B97F4A7C15ull) >> 32);
     return HSADMM_OK;
 }
 
