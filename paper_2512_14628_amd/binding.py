@@ -763,7 +763,7 @@ def hsadmm_expand_dual(plan: Plan, packed, mask, dst, Zi, Vd, workspace, stream=
 
 
 class _Unfit(Exception):
-    """A tensor that cannot be the buffer it was given as."""
+    """Arguments that do not go together, above all a tensor that cannot be the buffer it was given as."""
 
 
 def _fit(buffers, name: str, dtype, elems: int) -> list:
@@ -853,14 +853,14 @@ def hsadmm_plan_state_blocks(plan: Plan) -> int:
 
 def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence, *, grad_type: int = TYPE_F32,
                  state_bits: int = 32, M_scale: Optional[Sequence] = None, V_scale: Optional[Sequence] = None,
-                 W_low: Optional[Sequence] = None, Z=None, U=None, rho=None, grad_scale=None, coef=None, lr: float = 0.0,
-                 beta_one: float = 0.9, beta_two: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
-                 step: int = 1, noise: int = 0, stream=None, check: bool = True) -> int:
+                 W_low: Optional[Sequence] = None, Z=None, U=None, rho=None, grad_scale=None, coef=None,
+                 lr: Optional[float] = None, beta_one: float = 0.9, beta_two: float = 0.999, eps: float = 1e-8,
+                 weight_decay: float = 0.0, step: int = 1, noise: int = 0, stream=None, check: bool = True) -> int:
     """One AdamW step of every layer of every replica.  W, G, M, V (and M_scale, V_scale, W_low where they are given): one
-    buffer per replica; the other arguments are the fields of hsadmm_adamw_args_t.  With 8-bit states
-    codes are rounded with numbers made of `noise`, or of `step` where noise is 0: one of them has to differ from step to step
-    (or `coef`, which holds both).  Tensors of other types than grad_type
-    and state_bits say, or too short, are refused (INVALID_ARGUMENT)."""
+    buffer per replica; the other arguments are the fields of hsadmm_adamw_args_t.  `step` is 1 for the first step and grows by
+    one a step; with 8-bit states codes are rounded with numbers made of `noise`, or of `step` where noise is 0, so one of them
+    has to differ from step to step.  `coef` stands for lr, weight_decay, step and noise.  A call without lr and without coef is
+    refused (INVALID_ARGUMENT), as are tensors of other types than grad_type and state_bits say, or too short."""
     R, n, grad = len(W), plan.arena_elems, _GRAD_DTYPES.get(grad_type)
     fit = _fit
     if R > MAX_REPLICAS or grad is None or (state_bits != 32 and state_bits != 8):       # (the library refuses these as such)
@@ -888,6 +888,10 @@ def hsadmm_adamw(plan: Plan, W: Sequence, G: Sequence, M: Sequence, V: Sequence,
             fields += (0, 0, 0)
         fields += fit((grad_scale,), "grad_scale", _F32, R)
         fields.append(0 if coef is None else _fit_bytes(coef, "coef", _COEF_BYTES))
+        if lr is None:
+            if coef is None:
+                raise _Unfit("neither lr nor coef")
+            lr = 0.0
     except _Unfit as why:
         return _refused("hsadmm_adamw", why, check)
     args = _ADAMW_PACK.pack(_ADAMW_PACK.size, R, grad_type, state_bits, noise & 0xFFFFFFFF, *fields, lr, beta_one, beta_two, eps,

@@ -157,3 +157,11 @@ def test_the_structure_written_at_once_is_the_one_that_is_declared(lib):
     update(pkg.TYPE_F32, 32)
     b = binding._AdamwArgs.from_buffer_copy(lib.calls[1][1][1])
     assert (b.M_scale, b.V_scale, b.W_low) == (None, None, None) and b.V - b.W == 48
+
+
+def test_an_update_needs_a_learning_rate_or_coefficients(lib):
+    assert update(coef=None, check=False) == -1
+    with pytest.raises(pkg.HsadmmError) as e:
+        update(coef=None)
+    assert e.value.code == -1 and "lr" in str(e.value) and lib.calls == []
+    assert update(coef=None, lr=0.0) == 0 and update() == 0 and update(coef=4096) == 0
