@@ -795,8 +795,9 @@ int hsadmm_plan_state_blocks(const hsadmm_plan_t* plan, int64_t* blocks);
 
 /*
  * One AdamW step of every layer of R replicas (Algorithm 1, Phase 1: the local problem of Eq. (7), with AdamW in the place of
- * the paper's SGD).  Per replica r and element, in fp32 (every operation rounded by itself, except that the reciprocal in the
- * last line is within one unit in the last place and the multiplications after it are fused with the subtraction):
+ * the paper's SGD).  Per replica r and element, in fp32 over its whole range (every operation rounded by itself, roots
+ * included, except in the last line: sqrt(v) root + eps is fused, the reciprocal of it is within one unit in the last place, and
+ * the multiplication with step_size is fused with the subtraction):
  *     g = scale_r G;  with Z, U, rho:  g = g + rho_l ((W - Z) + U)             the proximal term of Eq. (7)
  *     m = beta_1 m + (1 - beta_1) g;   v = beta_2 v + (1 - beta_2) g^2
  *     W = W decay - step_size m / (sqrt(v) root + eps);  W_low = W rounded to the gradients' type

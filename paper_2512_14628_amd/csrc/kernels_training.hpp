@@ -243,20 +243,22 @@ __device__ __forceinline__ unsigned int top_bits(const v4f& v)
     return max(max(__float_as_uint(v.x) & m, __float_as_uint(v.y) & m), max(__float_as_uint(v.z) & m, __float_as_uint(v.w) & m));
 }
 
-// The root of x >= 0 to nearest, but for about one value in a million that lies next to the middle of two: the machine's
-// reciprocal root and one correction of x times it.  (Codes are cut from the root and the moments: a result that differs by
-// one unit in the last place from the operation's own rounding moves a code in every millionth case, this one hardly ever.)
-// Below fp32's normal range, where x itself has few bits left, the result is not zero but too small; infinity's root is infinity.
+// The root of x >= 0 to nearest: the machine's reciprocal root and one correction of x times it (compared with the rounded fp64
+// root for every fp32 number on gfx950: no difference).  Codes are cut from the root and the moments, and a result that is one unit
+// in the last place off moves a code in every millionth case.  Below 2^-64 the correction's remainder would leave fp32's normal
+// range, below 2^-126 x itself: the root is taken of 2^64 x there.  Infinity's root is infinity.
 __device__ __forceinline__ float root_of(float x)
 {
-    const float y = __builtin_amdgcn_rsqf(fmaxf(x, 0x1p-126f));
-    const float s = x * y;
-    const float r = __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
+    const bool low = x < 0x1p-64f;
+    const float a = x * (low ? 0x1p64f : 1.0f);
+    const float y = __builtin_amdgcn_rsqf(fmaxf(a, 0x1p-126f));
+    const float s = a * y;
+    const float r = __builtin_fmaf(__builtin_fmaf(-s, s, a), 0.5f * y, s) * (low ? 0x1p-32f : 1.0f);
     return x == __builtin_inff() ? x : r;
 }
 
 // Formulas: see hsadmm_adamw in the header.  Moments are formed in fp32, every operation rounded by itself; the weights' last
-// two operations are fused and the reciprocal before them is the machine's own, within one unit in the last place.
+// two operations and the denominator are fused, the reciprocal is the machine's own, within one unit in the last place.
 // The working copy is rounded to nearest: it is read by the forward pass only, the fp32 weights carry what the rounding loses.
 // A workgroup takes 4 * kBlock elements, the `part`-th such stretch of an item, of replicas `first` to R - 1 in turn: z_i and u are read
 // once for them.

@@ -1,0 +1,54 @@
+"""AdamW with second moments below fp32's normal range, and an eps that does not hide them."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2512_14628_amd as pkg
+import workloads as wk
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+E = 2.0 ** -24
+
+
+@pytest.mark.parametrize("eps", [2.0 ** -126, 1e-30, 1e-18])
+def test_the_first_step_of_gradients_whose_squares_are_tiny(eps):
+    """Gradients of 1e-23 to 1e-15: second moments from zero over single units of 2^-149 to 1e-33.  The weights' step from the
+    moments as they were stored: a root, a fused product and sum, a reciprocal of two units, a product and a fused end, each half a
+    unit of 2^-23 (E) but for the reciprocal (2 E) and the root (here 2 E); three constants rounded once."""
+    wl = wk.custom_workload([(64, 1024, 1, wk.MODE_FILTER, 8)], R=1, seed=0)
+    plan = pkg.Plan(wl.table())
+    n = plan.arena_elems
+    rng = np.random.default_rng(0)
+    g = (10.0 ** rng.uniform(-23, -15, n) * rng.choice([-1, 1], n)).astype(np.float32)
+    W, M, V = (torch.zeros(n, device=DEV) for _ in range(3))
+    pkg.hsadmm_adamw(plan, [W], [torch.from_numpy(g).to(DEV)], [M], [V], lr=1e-3, eps=eps, beta_one=0.9, beta_two=0.999, step=1)
+    w, m, v = (x.cpu().numpy().astype(np.float64) for x in (W, M, V))
+    g2 = g.astype(np.float64) ** 2
+    # (the square and the product with 1 - beta_2 round once each, to multiples of 2^-149 at the low end)
+    assert (np.abs(v - (1 - 0.999) * g2) <= 3 * E * v + 1.5 * 2.0 ** -149).all()
+    assert ((v > 0) & (v < 2.0 ** -126)).sum() > n // 8 and (v == 0).any()
+    root = 1 / np.sqrt(1 - 0.999)
+    want = -1e-3 / (1 - 0.9) * m / (np.sqrt(v) * root + eps)
+    assert (np.abs(w - want) <= 12 * E * np.abs(want)).all(), float(np.max(np.abs(w / want - 1)))
+    plan.close()
+
+
+def test_roots_of_8_bits_are_cut_from_the_right_root():
+    """A block whose second moments are all one tiny number: its scale is that number's root / 448 (the root, the division and
+    the constant round by 2 E, 2 E and E)."""
+    wl = wk.custom_workload([(1, 256 * 24, 1, wk.MODE_FILTER, 1)], R=1, seed=0)
+    plan = pkg.Plan(wl.table())
+    n, blocks = plan.arena_elems, plan.state_blocks
+    of_block = (10.0 ** np.linspace(-21, -16, blocks)).astype(np.float32)
+    W, Ms, Vs = torch.zeros(n, device=DEV), torch.zeros(blocks, device=DEV), torch.zeros(blocks, device=DEV)
+    M, V = (torch.zeros(n, dtype=torch.uint8, device=DEV) for _ in range(2))
+    G = torch.from_numpy(np.repeat(of_block, 256)[:n]).to(DEV)
+    pkg.hsadmm_adamw(plan, [W], [G], [M], [V], state_bits=8, M_scale=[Ms], V_scale=[Vs], lr=1e-3, eps=1e-30)
+    v = np.float32(1.0 - 0.999) * (of_block * of_block)                      # fp32, each operation rounded as the kernel's
+    assert ((v > 0) & (v < np.float32(2.0 ** -126))).sum() >= 6
+    want = np.sqrt(v.astype(np.float64)) / 448
+    got = Vs.cpu().numpy().astype(np.float64)
+    assert (np.abs(got - want) <= 5 * E * want).all(), got / want
+    plan.close()
