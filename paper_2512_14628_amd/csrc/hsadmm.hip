@@ -153,6 +153,7 @@ struct hsadmm_plan {
     std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, scatter_mx: every layer cut without regard to rows
     int64_t packed_elems = 0;           // what the plan's own selection packs
     int64_t state_blocks = 0;           // blocks that share a scale in 8-bit optimizer states
+    int64_t flat_stretches = 0;         // stretches of the flat items that hold elements (adamw: a workgroup's)
     int32_t n_segments = 0;             // scan segments (one per layer, two per BOTH layer)
     int32_t pack_align = 1;
     int64_t arena_elems = 0;
@@ -421,6 +422,7 @@ int lay_out(hsadmm_plan* p, const hsadmm_layer_t* layers, const hsadmm_nest_t* n
     p->both_layers.clear();
     p->items_flat.clear();
     p->state_blocks = 0;
+    p->flat_stretches = 0;
     int64_t gb = 0, cp = 0, cap = 0, poff = 0, nest_bytes = 0;
     int32_t seg = 0, kstart = 0;
     group_layer.clear();
@@ -495,6 +497,7 @@ int lay_out(hsadmm_plan* p, const hsadmm_layer_t* layers, const hsadmm_nest_t* n
             p->items_flat.push_back(FlatItem{x.elem_off + o, p->state_blocks + o / kStateBlock,
                                              (int32_t)std::min<int64_t>(kFlatElems, n_layer - o), l});
         p->state_blocks += (n_layer + kStateBlock - 1) / kStateBlock;
+        p->flat_stretches += (n_layer + kAdamwElems - 1) / kAdamwElems;
         if (x.mode == HSADMM_MODE_CHANNEL) {
             add_tile_items(p->items_proj, l, d, kChanRows, wide_strips);
             add_row_items(p->items_chan, l, d, x.mode, fine);
@@ -736,10 +739,12 @@ struct Stretches {
 };
 
 // Replicas a workgroup of the update takes one after the other.  With the pull all of them share what it read of z_i and u, from
-// kAdamwFull stretches (four workgroups a compute unit) on; smaller plans split them in fours.  Without it they share nothing.  All /
-// 4 / 1 at a time, us: with the pull ResNet-50, 4 replicas, 8-bit states 316 / 315 / 401, ResNet-18, 8 replicas 252 / 266 / 345, of
-// width 16 (0.7 M elements, 32 bits) 44.0 / 39.7 / 44.8, plain of width 64 20.3 / 18.9 / 22.3; without, ResNet-50, 4 replicas 291 /
-// 291 / 278, ResNet-18, 8 replicas, 32 bits 445 / 423 / 419.
+// kAdamwFull stretches that hold elements (four workgroups a compute unit) on; smaller plans split them in fours.  Without it they
+// share nothing.  All / 4 / 1 at a time, us: with the pull ResNet-50, 4 replicas, 8-bit states 316 / 315 / 401, ResNet-18, 8 replicas
+// 252 / 266 / 345, of width 16 (0.7 M elements, 32 bits) 44.0 / 39.7 / 44.8, plain of width 64 20.3 / 18.9 / 22.3; without, ResNet-50, 4
+// replicas 291 / 291 / 278, ResNet-18, 8 replicas, 32 bits 445 / 423 / 419.  All / 4 with many small layers, 16 replicas with the pull, 32 and
+// 8 bits: 160 of 900 elements (160 stretches) 60.6 / 49.8, 46.6 / 42.2; 200 of 4000 (800) 89.1 / 82.0, 66.4 / 57.7; 1000 of 1000 (1000)
+// 363 / 311, 233 / 235.
 constexpr int64_t kAdamwFull = 4 * 256;
 
 // Workgroups of one launch: a grid has fewer than 2^32 threads.  Arenas of more than 17 G elements (or fewer, of several replicas) take
@@ -750,9 +755,9 @@ template <int T, bool S8>
 hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool prox, bool low, hipStream_t s)
 {
     const auto go = [&](auto kernel) {
-        constexpr int64_t kStretches = kFlatElems / (4 * kBlock);                     // of an item
+        constexpr int64_t kStretches = kFlatElems / kAdamwElems;                      // of an item
         const int64_t items = (int64_t)p->items_flat.size();
-        const int each = !prox ? 1 : items * kStretches >= kAdamwFull ? R : std::min(R, 4);
+        const int each = !prox ? 1 : p->flat_stretches >= kAdamwFull ? R : std::min(R, 4);
         const int64_t groups = (R + each - 1) / each, most = kGridMost / (kStretches * groups);
         hipError_t e = hipSuccess;
         for (int64_t i = 0; i < items && e == hipSuccess; i += most)

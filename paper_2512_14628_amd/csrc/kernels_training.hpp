@@ -19,6 +19,7 @@ constexpr int kFlatElems = 8192;
 constexpr int kFlatQuads = 2;
 constexpr int kPartElems = 4 * kFlatQuads * kBlock;
 constexpr int kParts = kFlatElems / kPartElems;
+constexpr int kAdamwElems = 4 * kBlock;                // of a workgroup of adamw_kernel
 static_assert(kStateBlock == 4 * kWave, "a wave's fours are one state block");
 
 struct FlatItem {
@@ -346,7 +347,7 @@ constexpr int adamw_waves(bool S8, bool PROX) { return !S8 ? 3 : PROX ? 6 : kAll
 template <int T, bool S8, bool PROX, bool LOW>
 __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(1, adamw_waves(S8, PROX)))) void adamw_kernel(const FlatItem* __restrict__ items, AdamwArgs a, int R, int each)
 {
-    constexpr int kEach = kFlatElems / (4 * kBlock);
+    constexpr int kEach = kFlatElems / kAdamwElems;
     unsigned int stretch = blockIdx.x;
     int first = 0, last = R;
     if (each < R) {                                               // a workgroup takes `each` of the replicas
@@ -357,8 +358,8 @@ __global__ __launch_bounds__(kBlock) __attribute__((amdgpu_waves_per_eu(1, adamw
     }
     const FlatItem it = items[stretch / kEach];
     const int part = stretch % kEach;
-    if (it.n - part * 4 * kBlock >= 4 * kBlock) adamw_part<T, S8, PROX, LOW, true>(it, part, a, first, last);
-    else if (it.n > part * 4 * kBlock) adamw_part<T, S8, PROX, LOW, false>(it, part, a, first, last);
+    if (it.n - part * kAdamwElems >= kAdamwElems) adamw_part<T, S8, PROX, LOW, true>(it, part, a, first, last);
+    else if (it.n > part * kAdamwElems) adamw_part<T, S8, PROX, LOW, false>(it, part, a, first, last);
 }
 
 }  // namespace

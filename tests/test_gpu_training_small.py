@@ -52,3 +52,26 @@ def test_roots_of_8_bits_are_cut_from_the_right_root():
     got = Vs.cpu().numpy().astype(np.float64)
     assert (np.abs(got - want) <= 5 * E * want).all(), got / want
     plan.close()
+
+
+@pytest.mark.parametrize("layers,elems,groups", [(160, 900, 4), (1100, 900, 1), (160, 8000, 1), (20, 8192, 4)])
+def test_replicas_are_shared_out_by_the_work_there_is(layers, elems, groups):
+    """With the pull, 16 replicas are taken in fours unless 1024 stretches of 1024 elements hold anything, in however many
+    layers; the grid has eight stretches for every 8192 elements of a layer, or what it has of them."""
+    pitch = elems + -elems % 4
+    t = {"elem_off": pitch * np.arange(layers, dtype=np.int64), "c_out": np.ones(layers, np.int32),
+         "c_in": np.full(layers, elems, np.int32), "khw": np.ones(layers, np.int32), "mode": np.ones(layers, np.int32),
+         "k": np.ones(layers, np.int32)}
+    plan = pkg.Plan(t)
+    n, R = plan.arena_elems, 16
+    arenas = [torch.zeros(n, device=DEV) for _ in range(3 * R)]
+    G, Z = torch.ones(n, device=DEV), torch.zeros(n, device=DEV)
+    pkg.hsadmm_kernel_timing_enable(plan, True)
+    pkg.hsadmm_adamw(plan, arenas[:R], [G] * R, arenas[R:2 * R], arenas[2 * R:], Z=Z, U=Z, rho=torch.ones(layers, device=DEV),
+                     lr=0.25, step=1)
+    assert pkg.hsadmm_kernel_grids(plan)["adamw"] == layers * -(-elems // 8192) * 8 * groups
+    w = torch.stack(arenas[:R])
+    inside = (torch.arange(n, device=DEV) % pitch) < elems
+    # the first step is lr against the gradient's sign: a dozen roundings of 2 E on 0.25, eps is 1e-8 of it
+    assert float((w[:, inside] + 0.25).abs().max()) < 8 * E and not w[:, ~inside].any()
+    plan.close()
