@@ -974,7 +974,8 @@ int hsadmm_kernel_grid(const hsadmm_plan_t* plan, int kernel_id);
  * hsadmm_plan_create: HSADMM_NO_ESTIMATE (any value) switches the estimate off and the one launch of every kind of plan,
  * HSADMM_FORCE_ESTIMATE takes the estimate whatever the size and no one launch.  HSADMM_HELD_PATIENCE: how long rows wait for their
  * selection in the one launch, in ticks of 10 ns (30000 without it; for tests); rows that have waited so long are written in
- * a form that is finished once the selection is there, within the same launch.
+ * a form that is finished once the selection is there, within the same launch.  HSADMM_GRID_MOST: workgroups that one launch of
+ * hsadmm_adamw or hsadmm_expand_mx takes (16777215 without it, what a grid holds; for tests); more work takes several launches.
  */
 int hsadmm_plan_estimates(const hsadmm_plan_t* plan);
 /* Name of a kernel id ("" when out of range). */

@@ -117,6 +117,9 @@ struct WsLayout {
 enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kKernelCount };
 static_assert(kKernelCount == HSADMM_KERNEL_COUNT, "kernel id table");
 constexpr size_t kTimingPairs = 8192;
+// Workgroups of one launch: a grid has fewer than 2^32 threads.  The update and the expansion of quantised buffers take several launches for
+// arenas of more than 17 G elements (or fewer, of several replicas).
+constexpr int64_t kGridMost = (1ll << 32) / kBlock - 1;
 constexpr size_t kRepairGrid = 2048;       // workgroups of the repair pass under a prediction: 8 per compute unit
 
 // Scratch of the entry point that takes no workspace argument (hsadmm_project_compact_static): one array per
@@ -151,6 +154,7 @@ struct hsadmm_plan {
     std::vector<WorkItem> items_both;   // composite_colsums: tiles of the layers under both constraints
     std::vector<int32_t> both_layers;   // their indices
     std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, scatter_mx: every layer cut without regard to rows
+    int64_t grid_most = kGridMost;      // workgroups of one launch over the flat items
     int64_t packed_elems = 0;           // what the plan's own selection packs
     int64_t state_blocks = 0;           // blocks that share a scale in 8-bit optimizer states
     int64_t flat_stretches = 0;         // stretches of the flat items that hold elements (adamw: a workgroup's)
@@ -747,10 +751,6 @@ struct Stretches {
 // 363 / 311, 233 / 235.
 constexpr int64_t kAdamwFull = 4 * 256;
 
-// Workgroups of one launch: a grid has fewer than 2^32 threads.  Arenas of more than 17 G elements (or fewer, of several replicas) take
-// several launches.
-constexpr int64_t kGridMost = (1ll << 32) / kBlock - 1;
-
 template <int T, bool S8>
 hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool prox, bool low, hipStream_t s)
 {
@@ -758,7 +758,7 @@ hipError_t launch_adamw(const hsadmm_plan* p, const AdamwArgs& a, int R, bool pr
         constexpr int64_t kStretches = kFlatElems / kAdamwElems;                      // of an item
         const int64_t items = (int64_t)p->items_flat.size();
         const int each = !prox ? 1 : p->flat_stretches >= kAdamwFull ? R : std::min(R, 4);
-        const int64_t groups = (R + each - 1) / each, most = kGridMost / (kStretches * groups);
+        const int64_t groups = (R + each - 1) / each, most = std::max<int64_t>(1, p->grid_most / (kStretches * groups));
         hipError_t e = hipSuccess;
         for (int64_t i = 0; i < items && e == hipSuccess; i += most)
             e = launch(p, kAdamw, kernel, (unsigned)(std::min(most, items - i) * kStretches * groups), kBlock, s,
@@ -863,6 +863,9 @@ int hsadmm_plan_create_nested(const hsadmm_layer_t* layers, const hsadmm_nest_t*
         // (environment, read here once per plan: HSADMM_HELD_PATIENCE, ticks of 10 ns, is how the tests have rows written
         // before their selection is known)
         if (const char* t = std::getenv("HSADMM_HELD_PATIENCE")) p->held_patience = std::max(0ll, std::min(std::atoll(t), 100 * kHeldPatience));
+        // (likewise HSADMM_GRID_MOST: workgroups of one launch of the update and of the expansion of quantised buffers, so that small
+        // tables take several)
+        if (const char* t = std::getenv("HSADMM_GRID_MOST")) p->grid_most = std::max(1ll, std::min(std::atoll(t), (long long)kGridMost));
         if (p->n_held > 0) p->use_estimate = false;
         if (p->use_estimate) {
             std::vector<WorkItem> rest;
@@ -2232,7 +2235,7 @@ int hsadmm_expand_mx(const hsadmm_plan_t* p, const uint8_t* const* codes, const 
         if (rc != HSADMM_OK) return rc;
     }
     const auto go = [&](auto kernel) {
-        const int64_t items = (int64_t)p->items_flat.size(), most = kGridMost / kParts;
+        const int64_t items = (int64_t)p->items_flat.size(), most = std::max<int64_t>(1, p->grid_most / kParts);
         hipError_t e = hipSuccess;
         for (int64_t i = 0; i < items && e == hipSuccess; i += most)
             e = launch(p, kScatterMx, kernel, (unsigned)(std::min(most, items - i) * kParts), kBlock, s,
