@@ -798,7 +798,7 @@ int hsadmm_plan_state_blocks(const hsadmm_plan_t* plan, int64_t* blocks);
  * the paper's SGD).  Per replica r and element, in fp32 over its whole range (every operation rounded by itself, roots
  * included, except in the last line: sqrt(v) root + eps is fused, the reciprocal of it is within one unit in the last place, and
  * the multiplication with step_size is fused with the subtraction):
- *     g = scale_r G;  with Z, U, rho:  g = g + rho_l ((W - Z) + U)             the proximal term of Eq. (7)
+ *     g = scale_r G;  with Z, U, rho:  g = g + rho_l ((W - Z) + U)             the proximal term of Eq. (7), see U below
  *     m = beta_1 m + (1 - beta_1) g;   v = beta_2 v + (1 - beta_2) g^2
  *     W = W decay - step_size m / (sqrt(v) root + eps);  W_low = W rounded to the gradients' type
  * Fill a zeroed hsadmm_adamw_args_t; a NULL field means "not wanted" / "not given".  Arena padding is neither read nor written.
@@ -815,9 +815,14 @@ int hsadmm_plan_state_blocks(const hsadmm_plan_t* plan, int64_t* blocks);
  *   M_scale, V_scale in/out, 8 bits only (NULL otherwise): arrays of hsadmm_plan_state_blocks floats
  *   W_low            out, optional, 16-bit grad_type only: arenas that receive the rounded weights (the working copy of
  *                    mixed-precision training)
- *   Z, U, rho        in, all three or none: the node's consensus z_i and the replica-mean scaled dual (full-layout arenas,
- *                    16-byte aligned), and L floats, the layers' rho_1; read once for all replicas
- *   grad_scale       in, optional, R floats (hsadmm_gradient_norms); a replica whose factor is not finite is left untouched
+ *   Z, U, rho        in, all three or none: the node's consensus z_i and a scaled dual (full-layout arenas, 16-byte aligned),
+ *                    and L floats, the layers' rho_1; read once for all replicas.  Eq. (7) has a dual u_ij for every replica.
+ *                    With the replica-mean dual that the other calls carry, the replicas' pulls have the mean that they have
+ *                    in Eq. (7), but no dual acts on what tells the replicas apart (only rho_l (W - Z) does).  A program that
+ *                    keeps u_ij (hsadmm_dual_inter advances each) calls once for every replica, R = 1, with that replica's own.
+ *   grad_scale       in, optional, R floats (hsadmm_gradient_norms); a replica whose factor is not finite is left untouched.
+ *                    Gradients of a loss that was multiplied by S (fp16): hsadmm_gradient_norms with S max_norm, and the factors
+ *                    divided by S before they are handed on
  *   coef             in, optional, DEVICE: takes the place of lr, weight_decay, step and noise (hsadmm_adamw_coefficients).
  *                    Read by the kernel when it runs, so a captured graph follows the buffer's contents from replay to replay.
  *   lr, beta_one, beta_two, eps, weight_decay, step, noise   as in hsadmm_adamw_coefficients; eps >= 2^-126.  noise: 0 (a number

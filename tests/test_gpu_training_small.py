@@ -75,3 +75,36 @@ def test_replicas_are_shared_out_by_the_work_there_is(layers, elems, groups):
     # the first step is lr against the gradient's sign: a dozen roundings of 2 E on 0.25, eps is 1e-8 of it
     assert float((w[:, inside] + 0.25).abs().max()) < 8 * E and not w[:, ~inside].any()
     plan.close()
+
+
+def test_a_call_per_replica_takes_each_replicas_own_dual():
+    """Eq. (7) with u_ij: R calls of one replica; and with the same dual for all they are the one call's bits."""
+    wl = wk.custom_workload([(40, 33, 9, wk.MODE_FILTER, 8), (7, 5, 1, wk.MODE_FILTER, 2)], R=1, seed=0)
+    plan = pkg.Plan(wl.table())
+    n, R = plan.arena_elems, 3
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    W, U = torch.randn(R, n, generator=gen, device=DEV), torch.randn(R, n, generator=gen, device=DEV)
+    G, Z = torch.zeros(n, device=DEV), torch.randn(n, generator=gen, device=DEV)
+    rho = torch.tensor([0.5, 0.25], device=DEV)
+
+    def steps(duals, at_once):
+        w, m, v = W.clone(), torch.zeros_like(W), torch.zeros_like(W)
+        how = dict(Z=Z, rho=rho, lr=1e-2, beta_one=0.0, step=1)
+        if at_once:
+            pkg.hsadmm_adamw(plan, list(w), [G] * R, list(m), list(v), U=duals, **how)
+        else:
+            for r in range(R):
+                pkg.hsadmm_adamw(plan, [w[r]], [G], [m[r]], [v[r]], U=duals[r], **how)
+        return w, m, v
+
+    _, m, _ = steps(U, False)
+    for i, l in enumerate(wl.layers):
+        on = slice(l.elem_off, l.elem_off + l.n)
+        # beta_1 = 0: the first moment is the pull.  A difference, a sum and a product round
+        d = W[:, on].double() - Z[on].double()
+        want = float(rho[i]) * (d + U[:, on].double())
+        assert ((m[:, on].double() - want).abs() <= 3 * E * float(rho[i]) * (d.abs() + U[:, on].double().abs())).all()
+    one, each = steps(U[0], True), steps([U[0]] * R, False)
+    for x, y in zip(one, each):
+        assert torch.equal(x.view(torch.int32), y.view(torch.int32))
+    plan.close()
