@@ -81,7 +81,7 @@ def test_a_call_per_replica_takes_each_replicas_own_dual():
     """Eq. (7) with u_ij: R calls of one replica; and with the same dual for all they are the one call's bits."""
     wl = wk.custom_workload([(40, 33, 9, wk.MODE_FILTER, 8), (7, 5, 1, wk.MODE_FILTER, 2)], R=1, seed=0)
     plan = pkg.Plan(wl.table())
-    n, R = plan.arena_elems, 3
+    n, R = plan.arena_elems + -plan.arena_elems % 64, 3              # (replicas are rows: each of them aligned)
     gen = torch.Generator(device=DEV).manual_seed(2)
     W, U = torch.randn(R, n, generator=gen, device=DEV), torch.randn(R, n, generator=gen, device=DEV)
     G, Z = torch.zeros(n, device=DEV), torch.randn(n, generator=gen, device=DEV)
