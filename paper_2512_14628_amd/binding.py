@@ -234,7 +234,7 @@ def load_library():
                                          dp, dp, dp, dp, ctypes.c_double,
                                          ctypes.c_double, ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int32)]
     lib.hsadmm_stopping_test.restype = ctypes.c_int
-    lib.hsadmm_gradient_norms.argtypes = [vp, ctypes.POINTER(vp), ctypes.c_int32, ctypes.c_int32, ctypes.c_double, vp, vp,
+    lib.hsadmm_gradient_norms.argtypes = [vp, vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_double, vp, vp,
                                           vp, ctypes.c_size_t, vp]
     lib.hsadmm_gradient_norms.restype = ctypes.c_int
     lib.hsadmm_adamw_coefficients.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
@@ -246,7 +246,7 @@ def load_library():
     lib.hsadmm_adamw.restype = ctypes.c_int
     lib.hsadmm_compact_mx.argtypes = [vp, vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
     lib.hsadmm_compact_mx.restype = ctypes.c_int
-    lib.hsadmm_expand_mx.argtypes = [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.c_int32, ctypes.c_int32, vp, vp,
+    lib.hsadmm_expand_mx.argtypes = [vp, vp, vp, ctypes.c_int32, ctypes.c_int32, vp, vp,
                                      vp, vp, vp, ctypes.c_size_t, vp]
     lib.hsadmm_expand_mx.restype = ctypes.c_int
     lib.hsadmm_kernel_grid.argtypes = [vp, ctypes.c_int]
@@ -775,7 +775,7 @@ def _fit(buffers, name: str, dtype, elems: int) -> list:
         if x is None:
             x = 0
         elif not isinstance(x, int):
-            if ((x.dtype is not dtype and (dtype is not None or x.element_size() != 1)) or x.numel() < elems or
+            if ((x.element_size() != 1 if dtype is None else x.dtype is not dtype) or (elems and x.numel() < elems) or
                     not x.is_contiguous()):
                 raise _Unfit("%s: %s of %s, where %d elements of %s have to lie in a row" % (
                     name, tuple(x.shape), x.dtype, elems, dtype or "one byte"))
@@ -804,26 +804,23 @@ _F32 = torch.float32
 _GRAD_DTYPES = {TYPE_F32: _F32, TYPE_BF16: torch.bfloat16, TYPE_F16: torch.float16}
 
 
-def _addresses(at):
-    """HOST array of addresses."""
-    return (_vp * max(len(at), 1))(*at)
-
-
 def hsadmm_gradient_norms(plan: Plan, G: Sequence, max_norm: float, norm, scale, workspace, grad_type: int = TYPE_F32,
                           stream=None, workspace_bytes: Optional[int] = None, check: bool = True) -> int:
     """Norms of the replicas' gradients and the factors that clip them (NaN: not finite); either output may be None.  Tensors
     of another type than grad_type, or too short, are refused (INVALID_ARGUMENT)."""
     R, grad = len(G), _GRAD_DTYPES.get(grad_type)
     if R > MAX_REPLICAS or grad is None:                      # (the library refuses these as such)
-        at, norm_at, scale_at = [_ptr(g) for g in G], _ptr(norm), _ptr(scale)
+        at, norm_at, scale_at = [_ptr(g) or 0 for g in G], _ptr(norm), _ptr(scale)
     else:
         try:
             at = _fit(G, "G", grad, plan.arena_elems)
-            norm_at, scale_at = _fit((norm,), "norm", torch.float64, R)[0], _fit((scale,), "scale", _F32, R)[0]
+            norm_at = 0 if norm is None else _fit((norm,), "norm", torch.float64, R)[0]
+            scale_at = 0 if scale is None else _fit((scale,), "scale", _F32, R)[0]
         except _Unfit as why:
             return _refused("hsadmm_gradient_norms", why, check)
     wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
-    rc = load_library().hsadmm_gradient_norms(plan.handle, _addresses(at), R, int(grad_type), float(max_norm), norm_at,
+    at = array.array("Q", at)
+    rc = load_library().hsadmm_gradient_norms(plan.handle, at.buffer_info()[0], R, int(grad_type), float(max_norm), norm_at,
                                               scale_at, _ptr(workspace), wb, _stream(stream))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_gradient_norms")
@@ -927,13 +924,14 @@ def hsadmm_expand_mx(plan: Plan, codes: Sequence, scales: Sequence, format: int,
     if len(codes) != len(scales):
         raise ValueError("hsadmm_expand_mx: %d buffers of codes, %d of scales" % (len(codes), len(scales)))
     try:
-        codes_at, scales_at = _fit(codes, "codes", None, 0), _fit(scales, "scales", None, 0)
+        at = array.array("Q", _fit([*codes, *scales], "codes, scales", None, 0))      # HOST array of both lists
         full = _fit((dst, Zi, Vd), "dst, Zi, Vd", _F32, plan.arena_elems)
     except _Unfit as why:
         return _refused("hsadmm_expand_mx", why, check)
     wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
-    rc = load_library().hsadmm_expand_mx(plan.handle, _addresses(codes_at), _addresses(scales_at), len(codes), int(format),
-                                         _ptr(mask), full[0], full[1], full[2], _ptr(workspace), wb, _stream(stream))
+    M, first = len(codes), at.buffer_info()[0]
+    rc = load_library().hsadmm_expand_mx(plan.handle, first, first + 8 * M, M, int(format), _ptr(mask), full[0], full[1], full[2],
+                                         _ptr(workspace), wb, _stream(stream))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_expand_mx")
     return rc
