@@ -283,7 +283,7 @@ def _ptr(x) -> Optional[int]:
 
 
 def _nbytes(x) -> int:
-    return int(x.numel() * x.element_size())
+    return x.nbytes
 
 
 def _stream(stream) -> Optional[int]:
