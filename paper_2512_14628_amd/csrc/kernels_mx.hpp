@@ -94,7 +94,7 @@ __device__ __forceinline__ int layer_at(const int64_t* __restrict__ layer_off, i
 //   Q = 4 with all the registers it would take (111)     28.0: four waves a SIMD instead of six
 //   no look-up of the kept row, no division (a probe)    2.4 less: the chain of loads
 //   columns, a position to a lane through LDS            ResNet-152, channels at 0.3: 113 without, 60.6, non-temporal loads 55.0, now
-//                                                        52.6 (214 MB fetched for 70 MB kept: most lines hold a kept channel)
+//                                                        52.6 (221 MB fetched for 70 MB kept: most lines hold a kept channel)
 //   columns, rows read whole and kept elements put       133: a look-up of its place for every element, kept or not
 //   into LDS at their places
 template <int FMT, bool SUM, int Q>

@@ -72,8 +72,9 @@ struct GradArgs { const void* G[HSADMM_MAX_REPLICAS]; };
 
 // Sums of squares in fp64 (the square of an fp32 value is exact there): workgroup p of a replica's P takes the parts of the flat
 // items p, p + P, ...; the order of the additions depends on the plan and the number of replicas only.  Bound by HBM: ResNet-152, 8
-// replicas in bf16, 961 MB in 148 us (6.5 TB/s); ResNet-18, one in fp32, 10.7 us, of which 3 are gradient_norm_finish.  (Two to four
-// parts in flight: 149 to 156 us and 10.7, and small networks lose a microsecond or two.)
+// replicas in bf16, 961 MB in 144 us (6.7 TB/s) and 4.7 in gradient_norm_finish; ResNet-18, one in fp32, 47 MB in 9.8 us and 1.9 or, in
+// other runs, 3.9.  (Two to four parts in flight, both launches together: 149 to 156 us for 148, and small networks lose a microsecond
+// or two.)
 template <int T>
 __global__ __launch_bounds__(kBlock) void gradient_sqsums(const FlatItem* __restrict__ items, int n_items, GradArgs a, int P,
                                                           double* __restrict__ part)
