@@ -824,7 +824,8 @@ int hsadmm_plan_state_blocks(const hsadmm_plan_t* plan, int64_t* blocks);
  *                    Gradients of a loss that was multiplied by S (fp16): hsadmm_gradient_norms with S max_norm, and the factors
  *                    divided by S before they are handed on
  *   coef             in, optional, DEVICE: takes the place of lr, weight_decay, step and noise (hsadmm_adamw_coefficients).
- *                    Read by the kernel when it runs, so a captured graph follows the buffer's contents from replay to replay.
+ *                    Read by the kernel when it runs, so a captured graph follows the buffer's contents from replay to replay
+ *                    (captured without it, every replay is the same step: its bias corrections, its rounding numbers).
  *   lr, beta_one, beta_two, eps, weight_decay, step, noise   as in hsadmm_adamw_coefficients; eps >= 2^-126.  noise: 0 (a number
  *                    taken from step), or any sequence that differs from step to step, e.g. a counter's hash: with one number
  *                    for every step an element's rounding would be a fixed threshold and its second moment drift
@@ -890,7 +891,7 @@ int hsadmm_adamw(const hsadmm_plan_t* plan, const hsadmm_adamw_args_t* args);
  * places of a layer's last block after its last value hold code 0.  Alignment padding beyond that block is not written.
  *   src0, src1  device, full-layout arenas (read only), 16-byte aligned; src1 may be NULL
  *   mask        as in hsadmm_compact (NULL: the index mappings held in this workspace)
- *   codes, scales   device, out
+ *   codes, scales   device, out; they overlap neither each other nor an input
  *   layer_off, kept_idx, workspace  as in hsadmm_compact (layer_off counts elements)
  * Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
  */
@@ -908,7 +909,8 @@ int hsadmm_compact_mx(const hsadmm_plan_t* plan, const float* src0, const float*
  *                  codes 16-byte aligned
  *   mask           as in hsadmm_expand (NULL: the index mappings held in this workspace)
  *   dst            device, out, full-layout arena, 16-byte aligned
- *   Zi, Vd         both or none (INVALID_ARGUMENT), 16-byte aligned; dst, Zi and Vd must not overlap (INVALID_ARGUMENT)
+ *   Zi, Vd         both or none (INVALID_ARGUMENT), 16-byte aligned; dst, Zi and Vd must not overlap (INVALID_ARGUMENT), nor
+ *                  dst or Vd any of the buffers that are read
  * The plan's pack_align_elems must be a multiple of 32 (UNSUPPORTED otherwise).
  * Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
  */
