@@ -918,6 +918,108 @@ int hsadmm_expand_mx(const hsadmm_plan_t* plan, const uint8_t* const* codes, con
                      int32_t format, const uint8_t* mask, float* dst, const float* Zi, float* Vd,
                      void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * The two ends of a language model's local training (Algorithm 1, Phase 1, for models whose first and last layer have a row per
+ * token; the loss is that of any classifier too).  Such a layer is one of the plan's table, V = c_out rows of D = c_in weights with
+ * khw = 1, and these calls read it in an arena of weights (the fp32 arena, or W_low of hsadmm_adamw) and write its gradient in a
+ * gradient arena, where hsadmm_gradient_norms and hsadmm_adamw read it.  A call serves one replica.
+ *   layer       index of the layer in the table (INVALID_ARGUMENT: out of range; UNSUPPORTED: khw != 1)
+ *   type        HSADMM_TYPE_* of arenas and activations alike; sums are fp32, and every output is rounded once
+ *   ids, labels device, n numbers of index_bits 32 or 64, aligned to their size.  One outside [0, V) is no token, no target
+ *   X, Y, ...   activations: rows `stride` elements apart (>= their width, < 2^31), aligned to their element
+ *   W, G        arenas: fp32 aligned to 16 bytes, 16-bit ones to 8 (hsadmm_softmax_loss: W always to 16)
+ * n may be 0.  What is written overlaps neither what is read nor other outputs (INVALID_ARGUMENT), except where it is said.
+ * Results are the same from run to run.  No call reads or writes elements between rows, or other layers.
+ */
+
+/*
+ * out[i] = scale W[id_i] (one rounding), and zeros where id_i is no token.
+ *   out   device, n rows of D elements
+ * n <= 2^30 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ */
+int hsadmm_embedding(const hsadmm_plan_t* plan, int32_t layer, const void* W, int32_t type, const void* ids, int32_t index_bits,
+                     int64_t n, float scale, void* out, int64_t out_stride, void* hip_stream);
+
+/*
+ * The gradient of that: G[v] = scale sum of dY[i] over the i with id_i = v, summed in the order of the tokens (those of a token with
+ * many positions in parts first), for every row of the layer: rows without a token become 0.  With `accumulate` the sums are added
+ * to what G holds (and rows without a token are left alone): several batches, or a layer that is the first and the last at once,
+ * whose other gradient hsadmm_softmax_loss has written.  dY of positions that are no token is not read.
+ *   workspace   device, hsadmm_embedding_workspace bytes, 256-byte aligned; nothing is kept in it between calls
+ * n <= 2^30 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
+ */
+int hsadmm_embedding_workspace(const hsadmm_plan_t* plan, int32_t layer, int64_t n, size_t* bytes);
+int hsadmm_embedding_gradient(const hsadmm_plan_t* plan, int32_t layer, const void* ids, int32_t index_bits, int64_t n, const void* dY,
+                              int64_t dy_stride, int32_t type, float scale, int32_t accumulate, void* G,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Dropout: Y = X * 65536 / (65536 - t) where an element is kept, else 0 (whatever X holds there), plus the residual; fp32, rounded
+ * once.  t = floor(65536 p + 1/2), at most 65535: an element is dropped with probability t / 65536.  No mask is stored: the
+ * gradient with respect to X is the same call on Y's gradient, without the residual.
+ * Element i, counted row by row without strides, is kept iff its 16 random bits are >= t: Philox4x32-10 (Salmon, Moraes, Dror,
+ * Shaw, 2011) of the counter (i / 8, call), two words of 32 bits each, lower one first, and the key `seed`, likewise; of the four
+ * words the halves in ascending order belong to the elements 8 (i / 8) to 8 (i / 8) + 7.
+ *   residual     in, optional, rows like X's
+ *   Y            out; may be X, or the residual, with the same stride
+ *   rows, width  either may be 0
+ *   p            0 <= p < 1
+ *   seed, call   any numbers; `call` differs from call to call (a layer's number and a step's, say)
+ *   call_device  in, optional, DEVICE, 8-byte aligned: takes the place of call, read when the kernel runs (captured graphs)
+ * The plan only carries the diagnostics; no table of it is used.  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ */
+int hsadmm_dropout(const hsadmm_plan_t* plan, const void* X, int64_t x_stride, const void* residual, int64_t residual_stride,
+                   void* Y, int64_t y_stride, int64_t rows, int64_t width, int32_t type, double p, uint64_t seed, uint64_t call,
+                   const uint64_t* call_device, void* hip_stream);
+
+/*
+ * Softmax cross entropy of a linear layer's products against labels, and its gradients.  With l = X W^T and the count of targets:
+ *     lse_i = log(sum_v exp(l_iv));  loss_i = lse_i - l_{i,label_i};  both 0 where label_i is no target
+ *     total = { mean ? sum of the losses / max(count, 1) : sum, count }
+ *     f = mean ? scale / max(count, 1) : scale;   P_iv = exp(l_iv - lse_i) - [v = label_i], rows without a target 0
+ *     dX = f P W;   the layer's rows of G = f P^T X (with `accumulate` added to what G holds)
+ * `scale` multiplies the gradients alone (a loss scale of fp16 training).  Rows without a target cost nothing, and what X holds there
+ * is not looked at.  Logits are formed in fp32 and held for a piece of the vocabulary at a time; P is rounded to `type` (half
+ * precision: 2^15 P) for the products that follow.
+ * Fill a zeroed hsadmm_softmax_loss_args_t; a NULL field means "not wanted"; at least one output is.
+ *   struct_bytes  sizeof(hsadmm_softmax_loss_args_t) as the caller was compiled (INVALID_ARGUMENT if it differs)
+ *   W             in, arena of weights, 16-byte aligned
+ *   X             in, n rows of D elements
+ *   loss, lse     out, optional, n floats;  total  out, optional, 2 floats
+ *   dX            out, optional, n rows of D elements
+ *   G             out (in/out with `accumulate`), optional, gradient arena
+ *   workspace     device, hsadmm_softmax_loss_workspace bytes, 256-byte aligned (`gradients`: whether dX or G is wanted); nothing is
+ *                 kept in it between calls.  Calls that may overlap in time need one each
+ * n <= 2^23 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
+ */
+typedef struct {
+    size_t struct_bytes;
+    int32_t layer;
+    int32_t type;
+    int32_t index_bits;
+    int32_t mean;
+    int32_t accumulate;
+    int32_t reserved;          /* 0 */
+    int64_t n;
+    int64_t x_stride;
+    int64_t dx_stride;
+    double scale;
+    const void* W;
+    const void* X;
+    const void* labels;
+    float* loss;
+    float* lse;
+    float* total;
+    void* dX;
+    void* G;
+    void* workspace;
+    size_t workspace_bytes;
+    void* hip_stream;
+} hsadmm_softmax_loss_args_t;
+
+int hsadmm_softmax_loss_workspace(const hsadmm_plan_t* plan, int32_t layer, int64_t n, int32_t type, int32_t gradients, size_t* bytes);
+int hsadmm_softmax_loss(const hsadmm_plan_t* plan, const hsadmm_softmax_loss_args_t* args);
+
 /* Static string for an error code (never NULL). */
 const char* hsadmm_strerror(int code);
 
@@ -949,7 +1051,7 @@ int hsadmm_version(void);
  * profile taken elsewhere can be matched to the plan it is quoted for.
  * Errors: INVALID_ARGUMENT, HOST_MEMORY, HIP.
  */
-#define HSADMM_KERNEL_COUNT 34
+#define HSADMM_KERNEL_COUNT 52
 int hsadmm_kernel_timing_enable(hsadmm_plan_t* plan, int enable);
 int hsadmm_kernel_timing_read_n(hsadmm_plan_t* plan, double* total_ms, int64_t* launches, int32_t n);
 int hsadmm_kernel_timing_read(hsadmm_plan_t* plan, double* total_ms, int64_t* launches);
@@ -985,6 +1087,7 @@ int hsadmm_kernel_grid(const hsadmm_plan_t* plan, int kernel_id);
  * selection in the one launch, in ticks of 10 ns (30000 without it; for tests); rows that have waited so long are written in
  * a form that is finished once the selection is there, within the same launch.  HSADMM_GRID_MOST: workgroups that one launch of
  * hsadmm_adamw or hsadmm_expand_mx takes (16777215 without it, what a grid holds; for tests); more work takes several launches.
+ * HSADMM_LOSS_HELD: logits that hsadmm_softmax_loss holds at once (2^28 without it; for tests: small vocabularies then take several pieces).
  */
 int hsadmm_plan_estimates(const hsadmm_plan_t* plan);
 /* Name of a kernel id ("" when out of range). */

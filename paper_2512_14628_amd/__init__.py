@@ -11,6 +11,7 @@ from .binding import (  # noqa: F401
     hsadmm_plan_set_node_weights, hsadmm_project_weighted, hsadmm_project_weighted_compact, hsadmm_project_weighted_frozen, hsadmm_project_weighted_frozen_compact, hsadmm_dual_inter, hsadmm_residuals, hsadmm_average, hsadmm_mask_drift, hsadmm_expand_dual, hsadmm_retrain_project, hsadmm_retrain_expand, hsadmm_adapt_penalties, hsadmm_scale_layers,
     hsadmm_project_compact_static, hsadmm_step, hsadmm_selection_from_mask, hsadmm_layer_sqnorms, hsadmm_stopping_test,
     hsadmm_gradient_norms, hsadmm_adamw_coefficients, hsadmm_plan_state_blocks, hsadmm_adamw, hsadmm_compact_mx, hsadmm_expand_mx,
+    hsadmm_embedding, hsadmm_embedding_workspace, hsadmm_embedding_gradient, hsadmm_dropout, hsadmm_softmax_loss_workspace, hsadmm_softmax_loss,
     TYPE_F32, TYPE_BF16, TYPE_F16, MX_FP8, MX_FP4,
     MODE_NONE, MODE_FILTER, MODE_CHANNEL, MODE_BOTH, MAX_REPLICAS,
 )

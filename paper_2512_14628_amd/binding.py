@@ -46,8 +46,10 @@ EXPORTS = ("hsadmm_plan_create", "hsadmm_plan_destroy", "hsadmm_plan_sizes", "hs
            "hsadmm_step", "hsadmm_selection_from_mask", "hsadmm_kernel_grid", "hsadmm_plan_estimates",
            "hsadmm_layer_sqnorms", "hsadmm_stopping_test", "hsadmm_plan_create_nested",
            "hsadmm_gradient_norms", "hsadmm_adamw_coefficients", "hsadmm_plan_state_blocks", "hsadmm_adamw",
-           "hsadmm_compact_mx", "hsadmm_expand_mx")
-KERNEL_COUNT = 34
+           "hsadmm_compact_mx", "hsadmm_expand_mx",
+           "hsadmm_embedding", "hsadmm_embedding_workspace", "hsadmm_embedding_gradient", "hsadmm_dropout",
+           "hsadmm_softmax_loss_workspace", "hsadmm_softmax_loss")
+KERNEL_COUNT = 52
 
 
 class HsadmmError(RuntimeError):
@@ -108,7 +110,22 @@ class _AdamwArgs(ctypes.Structure):
     _fields_ = list(_ADAMW_FIELDS)
 
 
+# hsadmm_softmax_loss_args_t, field by field, in declaration order
+_LOSS_FIELDS = (
+    ("struct_bytes", ctypes.c_size_t), ("layer", ctypes.c_int32), ("type", ctypes.c_int32), ("index_bits", ctypes.c_int32),
+    ("mean", ctypes.c_int32), ("accumulate", ctypes.c_int32), ("reserved", ctypes.c_int32), ("n", ctypes.c_int64),
+    ("x_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64), ("scale", ctypes.c_double),
+    ("W", _vp), ("X", _vp), ("labels", _vp), ("loss", _vp), ("lse", _vp), ("total", _vp), ("dX", _vp), ("G", _vp),
+    ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t), ("hip_stream", _vp),
+)
+
+
+class _LossArgs(ctypes.Structure):
+    _fields_ = list(_LOSS_FIELDS)
+
+
 # the same structure written at once (native sizes and alignment)
+_LOSS_PACK = struct.Struct("N6i3qd9PNP")
 _ADAMW_PACK = struct.Struct("N3iI12P5dqP")
 _COEF_BYTES = ctypes.sizeof(_AdamwCoef)
 
@@ -249,6 +266,20 @@ def load_library():
     lib.hsadmm_expand_mx.argtypes = [vp, vp, vp, ctypes.c_int32, ctypes.c_int32, vp, vp,
                                      vp, vp, vp, ctypes.c_size_t, vp]
     lib.hsadmm_expand_mx.restype = ctypes.c_int
+    i32, i64, size = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+    lib.hsadmm_embedding.argtypes = [vp, i32, vp, i32, vp, i32, i64, ctypes.c_float, vp, i64, vp]
+    lib.hsadmm_embedding.restype = ctypes.c_int
+    lib.hsadmm_embedding_workspace.argtypes = [vp, i32, i64, ctypes.POINTER(size)]
+    lib.hsadmm_embedding_workspace.restype = ctypes.c_int
+    lib.hsadmm_embedding_gradient.argtypes = [vp, i32, vp, i32, i64, vp, i64, i32, ctypes.c_float, i32, vp, vp, size, vp]
+    lib.hsadmm_embedding_gradient.restype = ctypes.c_int
+    lib.hsadmm_dropout.argtypes = [vp, vp, i64, vp, i64, vp, i64, i64, i64, i32, ctypes.c_double, ctypes.c_uint64,
+                                   ctypes.c_uint64, vp, vp]
+    lib.hsadmm_dropout.restype = ctypes.c_int
+    lib.hsadmm_softmax_loss_workspace.argtypes = [vp, i32, i64, i32, i32, ctypes.POINTER(size)]
+    lib.hsadmm_softmax_loss_workspace.restype = ctypes.c_int
+    lib.hsadmm_softmax_loss.argtypes = [vp, vp]
+    lib.hsadmm_softmax_loss.restype = ctypes.c_int
     lib.hsadmm_kernel_grid.argtypes = [vp, ctypes.c_int]
     lib.hsadmm_kernel_grid.restype = ctypes.c_int
     lib.hsadmm_plan_estimates.argtypes = [vp]
@@ -336,6 +367,7 @@ class Plan:
         self.arena_elems, self.groups_total = a.value, g.value
         self.packed_capacity_elems, self.workspace_bytes = c.value, w.value
         self.state_blocks = hsadmm_plan_state_blocks(self)
+        self.widths = [int(c) for c in table["c_in"]]          # (columns of the layers that have one row a token)
 
     def close(self):
         if getattr(self, "handle", None):
@@ -934,4 +966,153 @@ def hsadmm_expand_mx(plan: Plan, codes: Sequence, scales: Sequence, format: int,
                                          _ptr(workspace), wb, _stream(stream))
     if check and rc != 0:
         raise HsadmmError(rc, "hsadmm_expand_mx")
+    return rc
+
+
+_INDEX_DTYPES = {32: torch.int32, 64: torch.int64}
+
+
+def _width(plan: Plan, layer: int) -> int:
+    """Columns of a layer's rows (0: no such layer, which the library refuses)."""
+    return plan.widths[layer] if 0 <= layer < plan.n_layers else 0
+
+
+def _count(ids, n: Optional[int]) -> int:
+    """How many tokens there are: n, or a tensor's length."""
+    if n is not None:
+        return int(n)
+    if ids is None or isinstance(ids, int):
+        raise _Unfit("n has to be given with an address")
+    return ids.numel()
+
+
+def _rows(x, name: str, dtype, n: int, width: int):
+    """Device address and stride of n rows of `width` elements: a tensor of two dimensions whose rows lie in one piece, at least
+    their width apart.  An integer address (the caller's word) stands for rows without gaps."""
+    if x is None or isinstance(x, int):
+        return x or 0, width
+    if x.dtype is not dtype or x.dim() != 2 or x.shape[0] != n or x.shape[1] != width or (
+            n > 0 and width > 1 and x.stride(1) != 1) or (n > 1 and x.stride(0) < width):
+        raise _Unfit("%s: %s of %s with strides %s, where %d rows of %d elements of %s have to lie apart" % (
+            name, tuple(x.shape), x.dtype, tuple(x.stride()), n, width, dtype))
+    return x.data_ptr(), x.stride(0) if n > 1 else width
+
+
+def hsadmm_embedding(plan: Plan, layer: int, W, ids, out, *, scale: float = 1.0, type: int = TYPE_F32, index_bits: int = 32,
+                     n: Optional[int] = None, stream=None, check: bool = True) -> int:
+    """out[i] = scale W[ids[i]], rows of the layer in the arena W; zeros where ids[i] is no token.  `n` only with addresses in the
+    place of tensors.  Tensors of other types or shapes are refused (INVALID_ARGUMENT)."""
+    dtype, width = _GRAD_DTYPES.get(type), _width(plan, layer)
+    try:
+        n = _count(ids, n)
+        if dtype is None or index_bits not in _INDEX_DTYPES:               # (the library refuses these as such)
+            at, ids_at, out_at, stride = _ptr(W), _ptr(ids), _ptr(out), width
+        else:
+            at = _fit((W,), "W", dtype, plan.arena_elems)[0]
+            ids_at = _fit((ids,), "ids", _INDEX_DTYPES[index_bits], n)[0]
+            out_at, stride = _rows(out, "out", dtype, n, width)
+    except _Unfit as why:
+        return _refused("hsadmm_embedding", why, check)
+    rc = load_library().hsadmm_embedding(plan.handle, int(layer), at, int(type), ids_at, int(index_bits), n, float(scale), out_at,
+                                         stride, _stream(stream))
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_embedding")
+    return rc
+
+
+def hsadmm_embedding_workspace(plan: Plan, layer: int, n: int) -> int:
+    """Bytes of the workspace of hsadmm_embedding_gradient for n tokens."""
+    nbytes = ctypes.c_size_t()
+    rc = load_library().hsadmm_embedding_workspace(plan.handle, int(layer), int(n), ctypes.byref(nbytes))
+    if rc != 0:
+        raise HsadmmError(rc, "hsadmm_embedding_workspace")
+    return nbytes.value
+
+
+def hsadmm_embedding_gradient(plan: Plan, layer: int, ids, dY, G, workspace, *, scale: float = 1.0, accumulate: bool = False,
+                              type: int = TYPE_F32, index_bits: int = 32, n: Optional[int] = None, stream=None,
+                              workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    """The layer's rows of the gradient arena G: the scaled sums of their tokens' rows of dY (added to what G holds with
+    `accumulate`).  Tensors of other types or shapes are refused (INVALID_ARGUMENT)."""
+    dtype, width = _GRAD_DTYPES.get(type), _width(plan, layer)
+    try:
+        n = _count(ids, n)
+        if dtype is None or index_bits not in _INDEX_DTYPES:
+            at, ids_at, dy_at, stride = _ptr(G), _ptr(ids), _ptr(dY), width
+        else:
+            at = _fit((G,), "G", dtype, plan.arena_elems)[0]
+            ids_at = _fit((ids,), "ids", _INDEX_DTYPES[index_bits], n)[0]
+            dy_at, stride = _rows(dY, "dY", dtype, n, width)
+    except _Unfit as why:
+        return _refused("hsadmm_embedding_gradient", why, check)
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    rc = load_library().hsadmm_embedding_gradient(plan.handle, int(layer), ids_at, int(index_bits), n, dy_at, stride, int(type),
+                                                  float(scale), 1 if accumulate else 0, at, _ptr(workspace), wb, _stream(stream))
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_embedding_gradient")
+    return rc
+
+
+def hsadmm_dropout(plan: Plan, X, Y, p: float, seed: int, call: int, *, residual=None, type: int = TYPE_F32, rows: Optional[int] = None,
+                   width: Optional[int] = None, call_device=None, stream=None, check: bool = True) -> int:
+    """Y = X without a share p of its elements, the others scaled up, plus the residual.  Which ones follows from seed and call (or
+    the 64-bit number at call_device, read when the kernel runs): the same call on Y's gradient is X's.  Tensors of two dimensions;
+    rows and width only with addresses in their place.  Tensors of other types or shapes are refused (INVALID_ARGUMENT)."""
+    dtype = _GRAD_DTYPES.get(type)
+    try:
+        if X is not None and not isinstance(X, int) and X.dim() == 2:
+            rows, width = X.shape[0] if rows is None else rows, X.shape[1] if width is None else width
+        if rows is None or width is None:
+            raise _Unfit("X: two dimensions, or rows and width")
+        if dtype is None:
+            at = [(_ptr(x) or 0, width) for x in (X, residual, Y)]
+        else:
+            at = [_rows(x, name, dtype, rows, width) for name, x in (("X", X), ("residual", residual), ("Y", Y))]
+        call_at = 0 if call_device is None else _fit_bytes(call_device, "call_device", 8)
+    except _Unfit as why:
+        return _refused("hsadmm_dropout", why, check)
+    rc = load_library().hsadmm_dropout(plan.handle, at[0][0], at[0][1], at[1][0], at[1][1], at[2][0], at[2][1], int(rows), int(width),
+                                       int(type), float(p), int(seed) & (2 ** 64 - 1), int(call) & (2 ** 64 - 1), call_at,
+                                       _stream(stream))
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_dropout")
+    return rc
+
+
+def hsadmm_softmax_loss_workspace(plan: Plan, layer: int, n: int, type: int = TYPE_F32, gradients: bool = True) -> int:
+    """Bytes of the workspace of hsadmm_softmax_loss for n rows, with gradients or for the losses alone."""
+    nbytes = ctypes.c_size_t()
+    rc = load_library().hsadmm_softmax_loss_workspace(plan.handle, int(layer), int(n), int(type), 1 if gradients else 0,
+                                                      ctypes.byref(nbytes))
+    if rc != 0:
+        raise HsadmmError(rc, "hsadmm_softmax_loss_workspace")
+    return nbytes.value
+
+
+def hsadmm_softmax_loss(plan: Plan, layer: int, W, X, labels, *, workspace, loss=None, lse=None, total=None, dX=None, G=None,
+                        mean: bool = True, scale: float = 1.0, accumulate: bool = False, type: int = TYPE_F32, index_bits: int = 32,
+                        n: Optional[int] = None, stream=None, workspace_bytes: Optional[int] = None, check: bool = True) -> int:
+    """Softmax cross entropy of X times the layer's rows of the arena W against labels, and its gradients; outputs that are None are
+    not wanted.  The other arguments are the fields of hsadmm_softmax_loss_args_t.  Tensors of other types or shapes are refused
+    (INVALID_ARGUMENT)."""
+    dtype, width = _GRAD_DTYPES.get(type), _width(plan, layer)
+    try:
+        n = _count(labels, n)
+        if dtype is None or index_bits not in _INDEX_DTYPES:
+            arenas, (x_at, x_stride), (dx_at, dx_stride), labels_at = [_ptr(W), _ptr(G) or 0], (_ptr(X), width), (_ptr(dX) or 0, width), _ptr(labels)
+        else:
+            arenas = _fit((W, G), "W, G", dtype, plan.arena_elems)
+            labels_at = _fit((labels,), "labels", _INDEX_DTYPES[index_bits], n)[0]
+            x_at, x_stride = _rows(X, "X", dtype, n, width)
+            dx_at, dx_stride = _rows(dX, "dX", dtype, n, width)
+        each = _fit((loss, lse), "loss, lse", _F32, n) + _fit((total,), "total", _F32, 2)
+    except _Unfit as why:
+        return _refused("hsadmm_softmax_loss", why, check)
+    wb = _nbytes(workspace) if workspace_bytes is None else int(workspace_bytes)
+    args = _LOSS_PACK.pack(_LOSS_PACK.size, int(layer), int(type), int(index_bits), 1 if mean else 0, 1 if accumulate else 0, 0, n,
+                           x_stride, dx_stride, float(scale), arenas[0], x_at or 0, labels_at or 0, *each, dx_at, arenas[1],
+                           _ptr(workspace) or 0, wb, _stream(stream) or 0)
+    rc = load_library().hsadmm_softmax_loss(plan.handle, args)
+    if check and rc != 0:
+        raise HsadmmError(rc, "hsadmm_softmax_loss")
     return rc

@@ -86,6 +86,8 @@
 #include "kernels_compact.hpp"
 #include "kernels_training.hpp"
 #include "kernels_mx.hpp"
+#include "kernels_loss.hpp"
+#include "kernels_tokens.hpp"
 
 namespace {
 
@@ -114,12 +116,13 @@ struct WsLayout {
     size_t key, colpart, pos, cnt, layer_off, kept_idx, respart, work, rowres, pred, est_cnt, est_keys, est_thr, est_thr_tag, nest, total;
 };
 
-enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kKernelCount };
+enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kLossTargets, kLossRows, kLossLogits, kLossJoin, kLossTotal, kLossSoftmax, kLossLogitGrads, kLossInputGrads, kLossWeightGrads, kLossInputs, kEmbedding, kTokenSort, kTokenCount, kTokenScan, kTokenMove, kEmbedParts, kEmbedGrad, kDropoutRows, kKernelCount };
 static_assert(kKernelCount == HSADMM_KERNEL_COUNT, "kernel id table");
 constexpr size_t kTimingPairs = 8192;
 // Workgroups of one launch: a grid has fewer than 2^32 threads.  The update and the expansion of quantised buffers take several launches for
 // arenas of more than 17 G elements (or fewer, of several replicas).
 constexpr int64_t kGridMost = (1ll << 32) / kBlock - 1;
+constexpr int64_t kLossHeld = 1ll << 28;   // 1 GiB of logits, and half of it of their gradients in 16 bits
 constexpr size_t kRepairGrid = 2048;       // workgroups of the repair pass under a prediction: 8 per compute unit
 
 // Scratch of the entry point that takes no workspace argument (hsadmm_project_compact_static): one array per
@@ -155,6 +158,7 @@ struct hsadmm_plan {
     std::vector<int32_t> both_layers;   // their indices
     std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, scatter_mx: every layer cut without regard to rows
     int64_t grid_most = kGridMost;      // workgroups of one launch over the flat items
+    int64_t loss_held = kLossHeld;      // logits that hsadmm_softmax_loss holds at once
     int64_t packed_elems = 0;           // what the plan's own selection packs
     int64_t state_blocks = 0;           // blocks that share a scale in 8-bit optimizer states
     int64_t flat_stretches = 0;         // stretches of the flat items that hold elements (adamw: a workgroup's)
@@ -866,6 +870,8 @@ int hsadmm_plan_create_nested(const hsadmm_layer_t* layers, const hsadmm_nest_t*
         // (likewise HSADMM_GRID_MOST: workgroups of one launch of the update and of the expansion of quantised buffers, so that small
         // tables take several)
         if (const char* t = std::getenv("HSADMM_GRID_MOST")) p->grid_most = std::max(1ll, std::min(std::atoll(t), (long long)kGridMost));
+        // (likewise HSADMM_LOSS_HELD: logits that hsadmm_softmax_loss holds at once, so that small vocabularies take several pieces)
+        if (const char* t = std::getenv("HSADMM_LOSS_HELD")) p->loss_held = std::max(1ll, std::min(std::atoll(t), (long long)kLossHeld));
         if (p->n_held > 0) p->use_estimate = false;
         if (p->use_estimate) {
             std::vector<WorkItem> rest;
@@ -2354,8 +2360,515 @@ const char* hsadmm_kernel_name(int kernel_id)
         case kAdamw: return "adamw";
         case kGatherMx: return "gather_mx";
         case kScatterMx: return "scatter_mx";
+        case kLossTargets: return "loss_targets";
+        case kLossRows: return "loss_rows";
+        case kLossLogits: return "loss_logits";
+        case kLossJoin: return "loss_join";
+        case kLossTotal: return "loss_total";
+        case kLossSoftmax: return "loss_softmax";
+        case kLossLogitGrads: return "loss_logit_gradients";
+        case kLossInputGrads: return "loss_input_gradients";
+        case kLossWeightGrads: return "loss_weight_gradients";
+        case kLossInputs: return "loss_inputs";
+        case kEmbedding: return "embedding_rows";
+        case kTokenSort: return "token_sort";
+        case kTokenCount: return "token_count";
+        case kTokenScan: return "token_scan";
+        case kTokenMove: return "token_move";
+        case kEmbedParts: return "embedding_parts";
+        case kEmbedGrad: return "embedding_gradient";
+        case kDropoutRows: return "dropout";
         default: return "";
     }
 }
 
 }  // extern "C"
+
+// ------------------------------------------------------------------ a language model's ends
+
+// The layer as a table of V rows of D elements, and where it starts in an arena; false: no such layer, or one with positions.
+static int table_layer(const hsadmm_plan_t* p, int32_t layer, int32_t* V, int32_t* D, int64_t* off)
+{
+    if (!p || layer < 0 || layer >= (int32_t)p->layers.size()) return HSADMM_ERR_INVALID_ARGUMENT;
+    const hsadmm_layer_t& l = p->layers[layer];
+    if (l.khw != 1) return HSADMM_ERR_UNSUPPORTED;
+    *V = l.c_out; *D = l.c_in; *off = l.elem_off;
+    return HSADMM_OK;
+}
+
+static size_t type_size(int32_t type) { return type == HSADMM_TYPE_F32 ? 4 : 2; }
+static bool known_type(int32_t type) { return type >= HSADMM_TYPE_F32 && type <= HSADMM_TYPE_F16; }
+static size_t index_size(int32_t bits) { return bits == 64 ? 8 : 4; }
+// Rows of a call: their positions are held in 32 bits.
+constexpr int64_t kMostRows = 1ll << 30;
+constexpr int64_t kMostLossRows = 1ll << 23;
+// Bytes from the first element of `rows` rows to the last one.
+static size_t span_of(int64_t rows, int64_t ld, int64_t cols, size_t size)
+{
+    return rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * size : 0;
+}
+// Rows that can be moved in pieces of 16 bytes.
+static bool whole_pieces(const void* at, int64_t ld, int64_t cols, size_t size)
+{
+    return is_aligned(at, 16) && ld * (int64_t)size % 16 == 0 && cols * (int64_t)size % 16 == 0;
+}
+static const void* at_elem(const void* arena, int64_t elem, size_t size) { return static_cast<const char*>(arena) + elem * (int64_t)size; }
+
+template <class F>
+static hipError_t for_type(int32_t type, F&& f)
+{
+    switch (type) {
+        case HSADMM_TYPE_BF16: return f(std::integral_constant<int, HSADMM_TYPE_BF16>{});
+        case HSADMM_TYPE_F16: return f(std::integral_constant<int, HSADMM_TYPE_F16>{});
+        default: return f(std::integral_constant<int, HSADMM_TYPE_F32>{});
+    }
+}
+template <class F>
+static hipError_t for_flag(bool flag, F&& f) { return flag ? f(std::true_type{}) : f(std::false_type{}); }
+
+int hsadmm_embedding(const hsadmm_plan_t* p, int32_t layer, const void* W, int32_t type, const void* ids, int32_t index_bits, int64_t n,
+                     float scale, void* out, int64_t out_stride, void* hip_stream)
+{
+    int32_t V, D;
+    int64_t off;
+    if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!known_type(type) || (index_bits != 32 && index_bits != 64) || n > kMostRows) return HSADMM_ERR_UNSUPPORTED;
+    if (n < 0 || out_stride < D || out_stride > INT32_MAX) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (n == 0) return HSADMM_OK;
+    const size_t size = type_size(type);
+    if (!W || !ids || !out || !is_aligned(W, type == HSADMM_TYPE_F32 ? 16 : 8) || !is_aligned(ids, index_size(index_bits)) || !is_aligned(out, size))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    Stretches used;
+    used.add(W, (size_t)p->arena_elems * size, false);
+    used.add(ids, (size_t)n * index_size(index_bits), false);
+    used.add(out, span_of(n, out_stride, D, size), true);
+    if (used.clash()) return HSADMM_ERR_INVALID_ARGUMENT;
+    const void* rows = at_elem(W, off, size);
+    const bool vec = whole_pieces(rows, D, D, size) && whole_pieces(out, out_stride, D, size);
+    const int pieces = vec ? (int)(D * size / 16) : D;
+    int lanes = 1;
+    while (lanes < pieces && lanes < kBlock) lanes *= 2;
+    const int64_t grid = (n + kBlock / lanes - 1) / (kBlock / lanes);
+    if (grid > kGridMost) return HSADMM_ERR_UNSUPPORTED;
+    const hipError_t e = for_type(type, [&](auto t) {
+        return for_flag(vec, [&](auto v) {
+            constexpr int T = decltype(t)::value;
+            typedef typename ElemOf<T>::type E;
+            return launch(p, kEmbedding, embedding_rows<T, decltype(v)::value>, (unsigned)grid, kBlock, static_cast<hipStream_t>(hip_stream),
+                          static_cast<const E*>(rows), V, (int)D, ids, (int)(index_bits == 64), n, scale, static_cast<E*>(out), out_stride,
+                          lanes);
+        });
+    });
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}
+
+// Where the scratch of the embedding's gradient lies in its workspace.
+struct EmbedScratch {
+    size_t key[2], pos[2], counts, sums, total;
+    int tiles, bits, passes, part;
+    int64_t stretches, pitch;
+};
+
+static EmbedScratch embed_scratch(int32_t V, int32_t D, int64_t n)
+{
+    EmbedScratch s{};
+    int width = 1;                                      // bits of the tokens, V (no token) among them
+    while (V >> width) ++width;
+    s.passes = (width + kDigitBits - 1) / kDigitBits;
+    s.bits = (width + s.passes - 1) / s.passes;
+    s.tiles = (int)((n + kSortTile - 1) / kSortTile);
+    // Stretches about as long as there are stretches, so that no row is a chain of more than some of either.
+    s.part = 64;
+    while ((int64_t)s.part * s.part * 4 < n) s.part *= 2;
+    s.stretches = (n + s.part - 1) / s.part;
+    s.pitch = ((int64_t)D + 3) / 4 * 4;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t here = at; at = align_up(at + bytes, 256); return here; };
+    for (int i = 0; i < 2; ++i) s.key[i] = take(4 * (size_t)n);
+    for (int i = 0; i < 2; ++i) s.pos[i] = take(4 * (size_t)n);
+    s.counts = take(s.tiles > 1 ? 4 * (size_t)kDigits * s.tiles : 0);
+    s.sums = take(2 * (size_t)s.stretches * (size_t)s.pitch * 4);
+    s.total = std::max<size_t>(at, 256);
+    return s;
+}
+
+int hsadmm_embedding_workspace(const hsadmm_plan_t* p, int32_t layer, int64_t n, size_t* bytes)
+{
+    int32_t V, D;
+    int64_t off;
+    if (!bytes || n < 0) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
+    if (n > kMostRows) return HSADMM_ERR_UNSUPPORTED;
+    *bytes = embed_scratch(V, D, n).total;
+    return HSADMM_OK;
+}
+
+int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void* ids, int32_t index_bits, int64_t n, const void* dY,
+                              int64_t dy_stride, int32_t type, float scale, int32_t accumulate, void* G, void* workspace,
+                              size_t workspace_bytes, void* hip_stream)
+{
+    int32_t V, D;
+    int64_t off;
+    if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!known_type(type) || (index_bits != 32 && index_bits != 64) || n > kMostRows) return HSADMM_ERR_UNSUPPORTED;
+    if (n < 0 || dy_stride < D || dy_stride > INT32_MAX) return HSADMM_ERR_INVALID_ARGUMENT;
+    const size_t size = type_size(type);
+    if (!G || !workspace || !is_aligned(G, type == HSADMM_TYPE_F32 ? 16 : 8) || !is_aligned(workspace, 256)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (n > 0 && (!ids || !dY || !is_aligned(ids, index_size(index_bits)) || !is_aligned(dY, size))) return HSADMM_ERR_INVALID_ARGUMENT;
+    const EmbedScratch ws = embed_scratch(V, D, n);
+    if (workspace_bytes < ws.total) return HSADMM_ERR_WORKSPACE;
+    Stretches used;
+    used.add(G, (size_t)p->arena_elems * size, true);
+    used.add(workspace, ws.total, true);
+    if (n > 0) {
+        used.add(ids, (size_t)n * index_size(index_bits), false);
+        used.add(dY, span_of(n, dy_stride, D, size), false);
+    }
+    if (used.clash()) return HSADMM_ERR_INVALID_ARGUMENT;
+    char* w = static_cast<char*>(workspace);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    SortArgs a{};
+    a.ids = ids; a.wide = index_bits == 64;
+    a.n = (int32_t)n; a.V = V;
+    for (int i = 0; i < 2; ++i) {
+        a.key[i] = reinterpret_cast<int32_t*>(w + ws.key[i]);
+        a.pos[i] = reinterpret_cast<int32_t*>(w + ws.pos[i]);
+    }
+    a.counts = reinterpret_cast<uint32_t*>(w + ws.counts);
+    a.tiles = ws.tiles; a.bits = ws.bits; a.passes = ws.passes;
+    hipError_t e = hipSuccess;
+    if (ws.tiles == 1) {
+        e = launch(p, kTokenSort, token_sort, 1u, kScanBlock, s, a);
+    } else {
+        for (int pass = 0; pass < a.passes && ws.tiles > 1 && e == hipSuccess; ++pass) {
+            e = launch(p, kTokenCount, token_count, (unsigned)ws.tiles, kScanBlock, s, a, pass);
+            if (e == hipSuccess) e = launch(p, kTokenScan, token_scan, 1u, kScanBlock, s, a.counts, ((int64_t)1 << a.bits) * ws.tiles);
+            if (e == hipSuccess) e = launch(p, kTokenMove, token_move, (unsigned)ws.tiles, kScanBlock, s, a, pass);
+        }
+    }
+    if (e != hipSuccess) return HSADMM_ERR_HIP;
+    EmbedGradArgs g{};
+    g.key = a.key[(a.passes - 1) & 1]; g.pos = a.pos[(a.passes - 1) & 1];
+    g.n = (int32_t)n; g.V = V; g.part = ws.part;
+    g.dY = dY; g.ld = dy_stride; g.cols = D;
+    g.sums = reinterpret_cast<float*>(w + ws.sums); g.pitch = ws.pitch;
+    g.G = const_cast<void*>(at_elem(G, off, size));
+    g.scale = scale; g.add = accumulate != 0;
+    g.rows = 4;
+    while (g.rows < kGradRows && V / g.rows > 2048) g.rows *= 2;
+    g.run = 1;
+    while (g.run < g.rows && g.run * D < 2048) g.run *= 2;
+    const bool vec = whole_pieces(g.G, D, D, size) && (n == 0 || whole_pieces(dY, dy_stride, D, size));
+    e = for_type(type, [&](auto t) {
+        return for_flag(vec, [&](auto v) {
+            constexpr int T = decltype(t)::value;
+            constexpr bool kVec = decltype(v)::value;
+            hipError_t r = hipSuccess;
+            if (n > ws.part) r = launch(p, kEmbedParts, embedding_parts<T, kVec>, (unsigned)ws.stretches, kBlock, s, g);
+            if (r == hipSuccess) r = launch(p, kEmbedGrad, embedding_gradient<T, kVec>, (unsigned)((V + g.rows - 1) / g.rows), kBlock, s, g);
+            return r;
+        });
+    });
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}
+
+int hsadmm_dropout(const hsadmm_plan_t* p, const void* X, int64_t x_stride, const void* residual, int64_t residual_stride, void* Y,
+                   int64_t y_stride, int64_t rows, int64_t width, int32_t type, double prob, uint64_t seed, uint64_t call,
+                   const uint64_t* call_device, void* hip_stream)
+{
+    if (!p || rows < 0 || width < 0 || !(prob >= 0.0 && prob < 1.0)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!known_type(type) || rows > (1ll << 40) || width > INT32_MAX) return HSADMM_ERR_UNSUPPORTED;
+    if (rows == 0 || width == 0) return HSADMM_OK;
+    const size_t size = type_size(type);
+    if (!X || !Y || x_stride < width || y_stride < width || (residual && residual_stride < width) || x_stride > INT32_MAX ||
+        y_stride > INT32_MAX || (residual && residual_stride > INT32_MAX) || !is_aligned(X, size) || !is_aligned(Y, size) ||
+        (residual && !is_aligned(residual, size)) || (call_device && !is_aligned(call_device, 8)))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    DropoutArgs a{};
+    // (65536 p to the nearest whole number, 65535 at most)
+    a.least = (uint32_t)std::min(65535.0, std::floor(prob * 65536.0 + 0.5));
+    a.scale = (float)(65536.0 / (65536.0 - (double)a.least));
+    // every element is read by the thread that writes it: an operand may be the output itself, row for row, and nothing else of it
+    Stretches used;
+    used.add(Y, span_of(rows, y_stride, width, size), true);
+    if (X != Y || (x_stride != y_stride && rows > 1)) used.add(X, span_of(rows, x_stride, width, size), false);
+    if (residual && (residual != Y || (residual_stride != y_stride && rows > 1)))
+        used.add(residual, span_of(rows, residual_stride, width, size), false);
+    if (call_device) used.add(call_device, 8, false);
+    if (used.clash()) return HSADMM_ERR_INVALID_ARGUMENT;
+    a.X = X; a.R = residual; a.Y = Y;
+    a.ldx = x_stride; a.ldr = residual ? residual_stride : x_stride; a.ldy = y_stride;
+    a.n = rows * width; a.cols = width;
+    a.seed = seed; a.call = call; a.call_dev = call_device;
+    bool vec = is_aligned(X, 16) && is_aligned(Y, 16) && (!residual || is_aligned(residual, 16));
+    if (a.ldx == width && a.ldy == width && a.ldr == width) {
+        a.cols = a.n;                                   // one row
+    } else {
+        vec = vec && width % kDropout == 0 && a.ldx % kDropout == 0 && a.ldy % kDropout == 0 && a.ldr % kDropout == 0;
+    }
+    const int64_t groups = (a.n + kDropout - 1) / kDropout;
+    const int64_t grid = std::min<int64_t>((groups + kBlock - 1) / kBlock, 1 << 20);
+    const hipError_t e = for_type(type, [&](auto t) {
+        return for_flag(vec, [&](auto v) {
+            return for_flag(residual != nullptr, [&](auto r) {
+                return launch(p, kDropoutRows, dropout_kernel<decltype(t)::value, decltype(v)::value, decltype(r)::value>, (unsigned)grid, kBlock,
+                              static_cast<hipStream_t>(hip_stream), a);
+            });
+        });
+    });
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}
+
+// How hsadmm_softmax_loss cuts its products, and where its scratch lies in the workspace.
+struct LossScratch {
+    size_t head, row, label, place, held, picked, stat, slab, rows, packed, logits, grads, sums, total;
+    int64_t Np, Dp;             // rows and columns of the held inputs
+    int64_t Vc;                 // classes of a piece, a multiple of 256
+    int pieces;
+    bool pack;                  // W's rows are copied before they are used (not whole pieces of 16 bytes)
+    bool narrow;                        // tiles of 128 x 32, else 128 x 128 or (wide) 256 x 256
+    bool wide, wide_inputs, wide_weights;   // of the logits, of the inputs' and the weights' gradients
+    int splits;                 // of the classes, in the inputs' gradient
+    int64_t k_part;
+    int slab_elems;
+};
+
+// Tiles of 256 x 256 where they are enough to fill the chip, else 128 x 128.
+static bool fills(int64_t a, int64_t b) { return ((a + 255) / 256) * ((b + 255) / 256) >= 256; }
+
+static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int64_t off, int64_t n, int32_t type, bool gradients)
+{
+    LossScratch s{};
+    const int64_t size = (int64_t)type_size(type);
+    s.narrow = n <= 32;
+    s.Np = s.narrow ? 32 : (n + kInputRows - 1) / kInputRows * kInputRows;
+    s.Dp = ((int64_t)D + kInputCols - 1) / kInputCols * kInputCols;
+    s.pack = D * size % 16 != 0 || off * size % 16 != 0;
+    const int64_t most = std::max<int64_t>(256, p->loss_held / s.Np / 256 * 256);
+    s.pieces = gradients || s.pack ? (int)((V + most - 1) / most) : 1;
+    s.Vc = ((V + s.pieces - 1) / s.pieces + 255) / 256 * 256;
+    s.pieces = (int)((V + s.Vc - 1) / s.Vc);
+    s.wide = size == 2 && !s.narrow && fills(n, s.Vc);
+    s.wide_inputs = size == 2 && !s.narrow && fills(n, D);
+    s.wide_weights = size == 2 && fills(s.Vc, D);
+    s.slab_elems = s.narrow ? 32 : s.wide ? 128 : 64;
+    const int64_t tiles = s.narrow ? (D + 127) / 128 : s.wide_inputs ? ((n + 255) / 256) * ((D + 255) / 256) : ((n + 127) / 128) * ((D + 127) / 128);
+    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, s.Vc / 256, 64}));
+    s.k_part = ((s.Vc + s.splits - 1) / s.splits + 63) / 64 * 64;
+    s.splits = (int)((s.Vc + s.k_part - 1) / s.k_part);
+    const int64_t slabs = (V + s.slab_elems - 1) / s.slab_elems + 256 / s.slab_elems;
+    size_t at = 0;
+    const auto take = [&](int64_t bytes) { const size_t here = at; at = align_up(at + (size_t)bytes, 256); return here; };
+    s.head = take(sizeof(LossHead));
+    s.row = take(4 * s.Np);
+    s.label = take(4 * s.Np);
+    s.place = take(4 * s.Np);
+    s.held = take(4 * s.Np);
+    s.picked = take(4 * s.Np);
+    s.stat = take(8 * s.Np);
+    s.slab = take(8 * slabs * s.Np);
+    s.rows = take(size * s.Np * s.Dp);
+    s.packed = take(s.pack ? size * s.Vc * s.Dp : 0);
+    s.logits = take(gradients ? 4 * s.Np * s.Vc : 0);
+    s.grads = gradients && size == 2 ? take(2 * s.Np * s.Vc) : s.logits;
+    s.sums = take(gradients ? 4 * (int64_t)s.splits * s.Np * s.Dp : 0);
+    s.total = at;
+    return s;
+}
+
+int hsadmm_softmax_loss_workspace(const hsadmm_plan_t* p, int32_t layer, int64_t n, int32_t type, int32_t gradients, size_t* bytes)
+{
+    int32_t V, D;
+    int64_t off;
+    if (!bytes || n < 0) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
+    if (!known_type(type) || n > kMostLossRows) return HSADMM_ERR_UNSUPPORTED;
+    *bytes = loss_scratch(p, V, D, off, n, type, gradients != 0).total;
+    return HSADMM_OK;
+}
+
+// One product over all tiles of its output; the tile's form by the sizes.
+template <int T, bool PMAJOR, bool QMAJOR, int WHAT>
+static hipError_t launch_product(const hsadmm_plan* p, KernelId kid, bool narrow, bool wide, int64_t out_p, int64_t out_q, ProductArgs a,
+                                 hipStream_t s)
+{
+    const auto go = [&](auto kernel, int bp, int bq, int threads) {
+        a.tiles_p = (int)((out_p + bp - 1) / bp);
+        a.tiles_q = (int)((out_q + bq - 1) / bq);
+        const int64_t grid = ((int64_t)a.tiles_p * a.tiles_q * a.splits + 7) / 8 * 8;
+        if (grid >= (1ll << 32) / threads) return hipErrorInvalidConfiguration;
+        return launch(p, kid, kernel, (unsigned)grid, (unsigned)threads, s, a);
+    };
+    if constexpr (WHAT != kWeightGrads)
+        if (narrow) return go(loss_product<T, 128, 32, 4, 1, PMAJOR, QMAJOR, WHAT>, 128, 32, 256);
+    if constexpr (T != HSADMM_TYPE_F32)
+        if (wide) return go(loss_product<T, 256, 256, 2, 4, PMAJOR, QMAJOR, WHAT>, 256, 256, 512);
+    return go(loss_product<T, 128, 128, 2, 2, PMAJOR, QMAJOR, WHAT>, 128, 128, 256);
+}
+
+template <int T>
+static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_args_t* x, const LossScratch& ws, int32_t V, int32_t D,
+                              int64_t off, hipStream_t s)
+{
+    typedef typename ElemOf<T>::type E;
+    const int64_t size = sizeof(E), n = x->n;
+    const bool gradients = x->dX || x->G;
+    char* w = static_cast<char*>(x->workspace);
+    LossRows r{reinterpret_cast<LossHead*>(w + ws.head), reinterpret_cast<int32_t*>(w + ws.row), reinterpret_cast<int32_t*>(w + ws.label),
+               reinterpret_cast<int32_t*>(w + ws.place)};
+    float* held = reinterpret_cast<float*>(w + ws.held);
+    float2* stat = reinterpret_cast<float2*>(w + ws.stat);
+    E* rows = reinterpret_cast<E*>(w + ws.rows);
+    E* packed = reinterpret_cast<E*>(w + ws.packed);
+    const E* W = static_cast<const E*>(at_elem(x->W, off, size));
+    hipError_t e = launch(p, kLossTargets, loss_targets, 1u, kScanBlock, s, x->labels, (int)(x->index_bits == 64), n, V, x->scale,
+                          (int)(x->mean != 0), r, x->loss, x->lse);
+    if (e == hipSuccess && n > 0)
+        e = for_flag(whole_pieces(x->X, x->x_stride, D, size), [&](auto v) {
+            return launch(p, kLossRows, loss_rows<T, decltype(v)::value, true>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s,
+                          static_cast<const E*>(x->X), x->x_stride, n, (int)D, r, rows, (int)ws.Dp);
+        });
+    ProductArgs a{};
+    a.head = r.head;
+    a.splits = 1;
+    a.V = V;
+    a.label = r.label;
+    a.picked = reinterpret_cast<float*>(w + ws.picked);
+    a.slab = reinterpret_cast<float2*>(w + ws.slab);
+    a.rows = ws.Np;
+    a.logit_ld = ws.Vc;
+    a.stat = stat;
+    a.grads = w + ws.grads;
+    a.sums = reinterpret_cast<float*>(w + ws.sums);
+    a.sum_ld = ws.Dp;
+    a.sum_part = ws.Np * ws.Dp;
+    a.out_ld = D;
+    const Operand inputs{rows, ws.Dp, ws.Np, ws.Dp};
+    // the weights of the classes from v0 on, `classes` of them
+    const auto weights = [&](int32_t v0, int64_t classes, Operand* o) -> hipError_t {
+        if (!ws.pack) {
+            *o = Operand{W + (int64_t)v0 * D, D, classes, D};
+            return hipSuccess;
+        }
+        *o = Operand{packed, ws.Dp, classes, ws.Dp};
+        return launch(p, kLossRows, loss_rows<T, false, false>, (unsigned)((classes + kWaves - 1) / kWaves), kBlock, s, W + (int64_t)v0 * D,
+                      (int64_t)D, classes, (int)D, r, packed, (int)ws.Dp);
+    };
+    const int32_t last = (int32_t)((ws.pieces - 1) * ws.Vc);
+    if (n > 0) {
+        // forward: all classes at once, or, where the weights are copied, piece by piece; the last piece's logits are kept
+        for (int i = 0; i < (ws.pack ? ws.pieces : 1) && e == hipSuccess; ++i) {
+            const int32_t v0 = ws.pack ? (int32_t)(i * ws.Vc) : 0;
+            const int64_t classes = ws.pack ? std::min<int64_t>(ws.Vc, V - v0) : V;
+            ProductArgs f = a;
+            e = weights(v0, classes, &f.p);
+            if (e != hipSuccess) break;
+            f.q = inputs;
+            f.k_part = ws.Dp;
+            f.v0 = v0;
+            f.keep0 = last;
+            f.logits = gradients && v0 + classes == V ? reinterpret_cast<float*>(w + ws.logits) : nullptr;
+            e = launch_product<T, false, false, kLogits>(p, kLossLogits, ws.narrow, ws.wide, classes, n, f, s);
+        }
+        const int slabs = (int)((V + ws.slab_elems - 1) / ws.slab_elems);
+        const auto join = [&](auto rows_at_once) {
+            constexpr int kRows = decltype(rows_at_once)::value;
+            return launch(p, kLossJoin, loss_join<kRows>, (unsigned)((n + kRows - 1) / kRows), kBlock, s, (const float2*)a.slab, slabs, ws.Np,
+                          (const float*)a.picked, r, stat, held, x->loss, x->lse);
+        };
+        if (e == hipSuccess) e = n <= 256 ? join(std::integral_constant<int, 1>{}) : join(std::integral_constant<int, 32>{});
+    }
+    if (e == hipSuccess && x->total)
+        e = launch(p, kLossTotal, loss_total, 1u, kBlock, s, (const LossHead*)r.head, (const float*)held, (int)(x->mean != 0), x->total);
+    if (!gradients) return e;
+    for (int i = ws.pieces - 1; i >= 0 && e == hipSuccess; --i) {
+        const int32_t v0 = (int32_t)(i * ws.Vc);
+        const int64_t classes = std::min<int64_t>(ws.Vc, V - v0);
+        Operand some{};
+        if (v0 != last || !ws.pack) e = weights(v0, classes, &some);
+        else some = Operand{packed, ws.Dp, classes, ws.Dp};
+        if (e != hipSuccess) break;
+        if (n > 0) {
+            if (v0 == last) {
+                const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(ws.Vc / (4 * kBlock), 65536 / std::max<int64_t>(1, n)));
+                e = launch(p, kLossSoftmax, loss_softmax<T>, (unsigned)(n * parts), kBlock, s, (const float*)(w + ws.logits),
+                           reinterpret_cast<E*>(w + ws.grads), ws.Vc, v0, V, (const float2*)stat, (const int32_t*)r.label,
+                           (const LossHead*)r.head, parts);
+            } else {
+                ProductArgs f = a;
+                f.p = some;
+                f.q = inputs;
+                f.k_part = ws.Dp;
+                f.v0 = v0;
+                e = launch_product<T, false, false, kLogitGrads>(p, kLossLogitGrads, ws.narrow, ws.wide, classes, n, f, s);
+            }
+        }
+        // (classes behind the last one have gradients of zero up to the end of a tile of 64 at least)
+        if (e == hipSuccess && x->dX && n > 0) {
+            ProductArgs f = a;
+            f.p = Operand{some.at, some.ld, D, classes};
+            f.q = Operand{w + ws.grads, ws.Vc, ws.Np, (classes + 63) / 64 * 64};
+            f.splits = ws.splits;
+            f.k_part = ws.k_part;
+            f.add = v0 != last;
+            e = launch_product<T, true, false, kInputGrads>(p, kLossInputGrads, ws.narrow, ws.wide_inputs, D, n, f, s);
+        }
+        if (e == hipSuccess && x->G) {
+            ProductArgs f = a;
+            f.p = Operand{rows, ws.Dp, ws.Dp, 0};
+            f.q = Operand{w + ws.grads, ws.Vc, classes, 0};
+            f.k_part = INT64_MAX / 2;
+            f.out = static_cast<E*>(x->G) + off + (int64_t)v0 * D;
+            f.add = x->accumulate != 0;
+            e = launch_product<T, true, true, kWeightGrads>(p, kLossWeightGrads, false, ws.wide_weights, D, classes, f, s);
+        }
+    }
+    if (e == hipSuccess && x->dX && n > 0)
+        e = launch(p, kLossInputs, loss_inputs<T>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s, (const float*)a.sums, ws.splits, a.sum_part,
+                   a.sum_ld, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D,
+                   (int)(x->dx_stride % 4 == 0 && is_aligned(x->dX, 4 * size)));
+    return e;
+}
+
+int hsadmm_softmax_loss(const hsadmm_plan_t* p, const hsadmm_softmax_loss_args_t* x)
+{
+    if (!p || !x || x->struct_bytes != sizeof(hsadmm_softmax_loss_args_t)) return HSADMM_ERR_INVALID_ARGUMENT;
+    int32_t V, D;
+    int64_t off;
+    if (const int rc = table_layer(p, x->layer, &V, &D, &off); rc != HSADMM_OK) return rc;
+    if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!known_type(x->type) || x->reserved != 0 || (x->index_bits != 32 && x->index_bits != 64) || x->n > kMostLossRows) return HSADMM_ERR_UNSUPPORTED;
+    const size_t size = type_size(x->type);
+    if (x->n < 0 || !x->W || !is_aligned(x->W, 16) || !x->workspace || !is_aligned(x->workspace, 256) || !(std::fabs(x->scale) <= 3e38))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if (x->n > 0 && (!x->X || !x->labels || !is_aligned(x->X, size) || !is_aligned(x->labels, index_size(x->index_bits)) ||
+                     x->x_stride < D || x->x_stride > INT32_MAX))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if ((x->loss && !is_aligned(x->loss, 4)) || (x->lse && !is_aligned(x->lse, 4)) || (x->total && !is_aligned(x->total, 4)) ||
+        (x->G && !is_aligned(x->G, x->type == HSADMM_TYPE_F32 ? 16 : 8)) ||
+        (x->dX && x->n > 0 && (!is_aligned(x->dX, size) || x->dx_stride < D || x->dx_stride > INT32_MAX)))
+        return HSADMM_ERR_INVALID_ARGUMENT;
+    if (!x->loss && !x->lse && !x->total && !x->dX && !x->G) return HSADMM_ERR_INVALID_ARGUMENT;
+    const LossScratch ws = loss_scratch(p, V, D, off, x->n, x->type, x->dX || x->G);
+    if (x->workspace_bytes < ws.total) return HSADMM_ERR_WORKSPACE;
+    Stretches used;
+    const size_t rows = (size_t)x->n;
+    used.add(x->W, (size_t)p->arena_elems * size, false);
+    used.add(x->workspace, ws.total, true);
+    if (x->G) used.add(x->G, (size_t)p->arena_elems * size, true);
+    if (x->total) used.add(x->total, 8, true);
+    if (rows > 0) {
+        used.add(x->X, span_of(x->n, x->x_stride, D, size), false);
+        used.add(x->labels, rows * index_size(x->index_bits), false);
+        if (x->dX) used.add(x->dX, span_of(x->n, x->dx_stride, D, size), true);
+        if (x->loss) used.add(x->loss, 4 * rows, true);
+        if (x->lse) used.add(x->lse, 4 * rows, true);
+    }
+    if (used.clash()) return HSADMM_ERR_INVALID_ARGUMENT;
+    hipStream_t s = static_cast<hipStream_t>(x->hip_stream);
+    const hipError_t e = for_type(x->type, [&](auto t) { return launch_loss<decltype(t)::value>(p, x, ws, V, D, off, s); });
+    return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
+}

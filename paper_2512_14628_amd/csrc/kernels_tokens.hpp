@@ -1,0 +1,459 @@
+// hsadmm_embedding / hsadmm_embedding_gradient / hsadmm_dropout: what a language model's tokens pass on their way into the network.
+// Part of the single translation unit built from hsadmm.hip (included there, in order).
+#ifndef KERNELS_TOKENS_HPP
+#define KERNELS_TOKENS_HPP
+#include "hsadmm_device.hpp"
+#include "kernels_training.hpp"
+#include "kernels_loss.hpp"
+
+namespace {
+
+// A piece of 16 bytes, or (VEC false: rows that are not whole pieces) a single element.
+template <int T, bool VEC> struct Piece {
+    typedef typename ElemOf<T>::type E;
+    static constexpr int n = VEC ? Wide<T>::n : 1;
+    static __device__ __forceinline__ void load(const E* p, float (&x)[n])
+    {
+        if constexpr (VEC) {
+            const typename Wide<T>::vec v = *reinterpret_cast<const typename Wide<T>::vec*>(p);
+#pragma unroll
+            for (int i = 0; i < n; ++i) x[i] = (float)v[i];
+        } else {
+            x[0] = (float)*p;
+        }
+    }
+    static __device__ __forceinline__ void store(E* p, const float (&x)[n])
+    {
+        if constexpr (VEC) {
+            typename Wide<T>::vec v;
+#pragma unroll
+            for (int i = 0; i < n; ++i) v[i] = (E)x[i];
+            *reinterpret_cast<typename Wide<T>::vec*>(p) = v;
+        } else {
+            *p = (E)x[0];
+        }
+    }
+};
+
+// ------------------------------------------------------------------ embedding
+
+// out[i] = scale W[id_i], zeros for an id outside [0, V).  `lanes` threads (a power of two) share a row.
+template <int T, bool VEC>
+__global__ __launch_bounds__(kBlock) void embedding_rows(const typename ElemOf<T>::type* __restrict__ W, int32_t V, int cols,
+                                                         const void* __restrict__ ids, int wide, int64_t n, float scale,
+                                                         typename ElemOf<T>::type* __restrict__ out, int64_t ld, int lanes)
+{
+    typedef Piece<T, VEC> P;
+    const int64_t i = (int64_t)blockIdx.x * (kBlock / lanes) + threadIdx.x / lanes;
+    if (i >= n) return;
+    const int64_t id = index_at(ids, wide != 0, i);
+    const bool has = id >= 0 && id < V;
+    const typename ElemOf<T>::type* from = W + (has ? id * cols : 0);
+    for (int c = (threadIdx.x & (lanes - 1)) * P::n; c < cols; c += lanes * P::n) {
+        float x[P::n] = {};
+        if (has) {
+            P::load(from + c, x);
+#pragma unroll
+            for (int e = 0; e < P::n; ++e) x[e] *= scale;
+        }
+        P::store(out + i * ld + c, x);
+    }
+}
+
+// ------------------------------------------------------------------ tokens in order
+
+// Positions sorted by their token, tokens that are equal in the order of their positions: radix sort from the lowest digit, of up to
+// kDigitBits bits each.  Ids outside [0, V) become V and so come last.  A workgroup takes a tile of kSortTile positions, a wave of it
+// adjacent ones; lanes with equal digits find each other by ballots, so places depend on the ids alone.
+constexpr int kDigitBits = 9;
+constexpr int kDigits = 1 << kDigitBits;
+constexpr int kSortTile = 32768;
+
+struct SortArgs {
+    const void* ids;
+    int wide;
+    int32_t n, V;
+    int32_t* key[2];
+    int32_t* pos[2];
+    uint32_t* counts;           // [digit][tile], several tiles only
+    int tiles;
+    int bits, passes;
+};
+
+__device__ __forceinline__ int digit_of(int32_t key, int shift, int bits) { return (key >> shift) & ((1 << bits) - 1); }
+
+// The lanes (of those that are active) with this lane's digit.
+__device__ __forceinline__ unsigned long long same_digit(int digit, int bits, bool active)
+{
+    unsigned long long same = __ballot(active);
+    for (int b = 0; b < bits; ++b) {
+        const unsigned long long set = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? set : ~set;
+    }
+    return same;
+}
+
+__device__ __forceinline__ int32_t sort_key(const SortArgs& a, int pass, int64_t i)
+{
+    if (pass > 0) return a.key[(pass - 1) & 1][i];
+    const int64_t id = index_at(a.ids, a.wide != 0, i);
+    return id >= 0 && id < a.V ? (int32_t)id : a.V;
+}
+
+struct SortShared {
+    uint32_t count[kScanWaves][kDigits];
+    uint32_t sums[kScanWaves];
+};
+
+// Counts the digits of a tile, wave by wave.
+__device__ void sort_count(const SortArgs& a, int pass, int tile, SortShared& s)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, shift = pass * a.bits;
+    const int64_t from = (int64_t)tile * kSortTile, end = min((int64_t)a.n, from + kSortTile);
+    const int each = (int)((end - from + kScanBlock - 1) / kScanBlock) * kWave;     // of a wave
+    for (int d = lane; d < kDigits; d += kWave) s.count[wave][d] = 0;
+    __syncthreads();
+    const int64_t w0 = from + (int64_t)wave * each, w1 = min(end, w0 + each);
+    for (int64_t i0 = w0; i0 < w1; i0 += kWave) {
+        const bool active = i0 + lane < w1;
+        const int d = digit_of(active ? sort_key(a, pass, i0 + lane) : 0, shift, a.bits);
+        const unsigned long long same = same_digit(d, a.bits, active);
+        if (active && __ffsll((long long)same) - 1 == lane) atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
+    }
+    __syncthreads();
+}
+
+// Moves a tile's positions to their places.  s.count: where each wave's first of a digit goes.
+__device__ void sort_move(const SortArgs& a, int pass, int tile, SortShared& s)
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, shift = pass * a.bits;
+    const int64_t from = (int64_t)tile * kSortTile, end = min((int64_t)a.n, from + kSortTile);
+    const int each = (int)((end - from + kScanBlock - 1) / kScanBlock) * kWave;
+    const int64_t w0 = from + (int64_t)wave * each, w1 = min(end, w0 + each);
+    for (int64_t i0 = w0; i0 < w1; i0 += kWave) {
+        const bool active = i0 + lane < w1;
+        const int32_t key = active ? sort_key(a, pass, i0 + lane) : 0;
+        const int32_t pos = active && pass > 0 ? a.pos[(pass - 1) & 1][i0 + lane] : (int32_t)(i0 + lane);
+        const int d = digit_of(key, shift, a.bits);
+        const unsigned long long same = same_digit(d, a.bits, active);
+        const int first = active ? __ffsll((long long)same) - 1 : lane;
+        uint32_t at = 0;
+        if (active && first == lane) at = atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
+        at = __shfl(at, first, kWave) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+        if (active) {
+            a.key[pass & 1][at] = key;
+            a.pos[pass & 1][at] = pos;
+        }
+    }
+    __syncthreads();
+}
+
+// s.count from counts to places: behind the digits below, then the waves before.  `start`: the tile's places of its digits, or null
+// (a single tile).
+__device__ void sort_places(SortShared& s, const uint32_t* start, int stride)
+{
+    const int d = threadIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    uint32_t all = 0;
+    if (d < kDigits)
+        for (int w = 0; w < kScanWaves; ++w) all += s.count[w][d];
+    uint32_t upto = all;
+    for (int o = 1; o < kWave; o <<= 1) {
+        const uint32_t x = __shfl_up(upto, o, kWave);
+        if (lane >= o) upto += x;
+    }
+    if (lane == kWave - 1) s.sums[wave] = upto;
+    __syncthreads();
+    uint32_t at = upto - all;
+    for (int w = 0; w < wave; ++w) at += s.sums[w];
+    if (d < kDigits) {
+        if (start) at = start[(int64_t)d * stride];
+        for (int w = 0; w < kScanWaves; ++w) {
+            const uint32_t c = s.count[w][d];
+            s.count[w][d] = at;
+            at += c;
+        }
+    }
+    __syncthreads();
+}
+
+// A single tile: all passes in one workgroup.
+__global__ __launch_bounds__(kScanBlock) void token_sort(SortArgs a)
+{
+    __shared__ SortShared s;
+    for (int pass = 0; pass < a.passes; ++pass) {
+        sort_count(a, pass, 0, s);
+        sort_places(s, nullptr, 0);
+        sort_move(a, pass, 0, s);
+    }
+}
+
+// Several tiles, a pass in three launches: digits of every tile, their places, the move.
+__global__ __launch_bounds__(kScanBlock) void token_count(SortArgs a, int pass)
+{
+    __shared__ SortShared s;
+    sort_count(a, pass, blockIdx.x, s);
+    for (int d = threadIdx.x; d < kDigits; d += kScanBlock) {
+        uint32_t all = 0;
+        for (int w = 0; w < kScanWaves; ++w) all += s.count[w][d];
+        a.counts[(int64_t)d * a.tiles + blockIdx.x] = all;
+    }
+}
+
+__global__ __launch_bounds__(kScanBlock) void token_scan(uint32_t* __restrict__ counts, int64_t n)
+{
+    __shared__ uint32_t sums[2][kScanWaves];
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    uint32_t before = 0;
+    int turn = 0;
+    for (int64_t i0 = 0; i0 < n; i0 += kScanBlock, turn ^= 1) {
+        const int64_t i = i0 + threadIdx.x;
+        const uint32_t own = i < n ? counts[i] : 0;
+        uint32_t upto = own;
+        for (int o = 1; o < kWave; o <<= 1) {
+            const uint32_t x = __shfl_up(upto, o, kWave);
+            if (lane >= o) upto += x;
+        }
+        if (lane == kWave - 1) sums[turn][wave] = upto;
+        __syncthreads();
+        uint32_t at = before + upto - own;
+        for (int w = 0; w < kScanWaves; ++w) {
+            before += sums[turn][w];
+            if (w < wave) at += sums[turn][w];
+        }
+        if (i < n) counts[i] = at;
+    }
+}
+
+__global__ __launch_bounds__(kScanBlock) void token_move(SortArgs a, int pass)
+{
+    __shared__ SortShared s;
+    sort_count(a, pass, blockIdx.x, s);
+    sort_places(s, a.counts + blockIdx.x, a.tiles);
+    sort_move(a, pass, blockIdx.x, s);
+}
+
+// ------------------------------------------------------------------ gradient of the embedding
+
+// dW[v] = scale times the sum of dY over v's tokens, in the order of their positions; in fp32, rounded once.  A token with more than
+// `part` positions is summed in parts first, those of the sorted list's stretches of `part`: a stretch holds the end of at most one
+// such token and the beginning of at most one (or the whole stretch is one's), so it has two rows of sums: [2 b] for the token of its
+// first position, [2 b + 1] for another that begins in it.
+struct EmbedGradArgs {
+    const int32_t* key;
+    const int32_t* pos;
+    int32_t n, V;
+    int part;
+    const void* dY;
+    int64_t ld;
+    int cols;
+    float* sums;        // [2 stretches][pitch]
+    int64_t pitch;
+    void* G;
+    float scale;
+    int add;
+    int rows, run;      // of a workgroup (see embedding_gradient), powers of two
+};
+
+// First place in the sorted list whose token is at least v.
+__device__ __forceinline__ int lower_bound(const int32_t* __restrict__ key, int n, int32_t v)
+{
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = lo + (hi - lo) / 2;
+        if (key[mid] < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// x += dY rows of the sorted places [from, to), one piece of columns.
+template <int T, bool VEC>
+__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, int c, float (&x)[Piece<T, VEC>::n])
+{
+    typedef Piece<T, VEC> P;
+    const typename ElemOf<T>::type* dY = static_cast<const typename ElemOf<T>::type*>(a.dY);
+    constexpr int kAtOnce = 8;
+    for (int i = from; i < to; i += kAtOnce) {
+        float y[kAtOnce][P::n];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            // (places behind the last are read again and not added: the loads stay in flight together)
+            P::load(dY + (int64_t)a.pos[min(i + u, to - 1)] * a.ld + c, y[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u)
+            if (i + u < to)
+#pragma unroll
+                for (int e = 0; e < P::n; ++e) x[e] += y[u][e];
+    }
+}
+
+template <int T, bool VEC>
+__global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
+{
+    typedef Piece<T, VEC> P;
+    __shared__ int bound[4];
+    const int64_t b = blockIdx.x;
+    const int from = (int)(b * a.part), to = (int)min((int64_t)a.n, (b + 1) * a.part);
+    // the extent of the tokens of the first and the last position
+    if (threadIdx.x < 4) bound[threadIdx.x] = lower_bound(a.key, a.n, a.key[threadIdx.x < 2 ? from : to - 1] + (threadIdx.x & 1));
+    __syncthreads();
+    const bool first = a.key[from] < a.V && bound[1] - bound[0] > a.part;
+    const bool last = a.key[to - 1] < a.V && bound[3] - bound[2] > a.part && bound[2] != bound[0];
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if (!(which ? last : first)) continue;
+        const int f = which ? bound[2] : from, t = which ? to : min(to, bound[1]);
+        for (int c = threadIdx.x * P::n; c < a.cols; c += kBlock * P::n) {
+            float x[P::n] = {};
+            add_rows<T, VEC>(a, f, t, c, x);
+            float* to_sums = a.sums + (2 * b + which) * a.pitch + c;
+#pragma unroll
+            for (int e = 0; e < P::n; ++e) to_sums[e] = x[e];
+        }
+    }
+}
+
+// The rows of dW: a workgroup takes `rows` of them, a wave one after the other; runs of `run` adjacent rows, the runs of a workgroup
+// as far apart as the grid is wide, as the frequent tokens often are the first ones.
+constexpr int kGradRows = 64;           // at most
+
+template <int T, bool VEC>
+__global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
+{
+    typedef Piece<T, VEC> P;
+    typedef typename ElemOf<T>::type E;
+    __shared__ int bound[kGradRows][2];
+    const auto row_of = [&](int i) { return ((int64_t)(i / a.run) * gridDim.x + blockIdx.x) * a.run + i % a.run; };
+    if (threadIdx.x < 2 * a.rows) {
+        const int64_t v = row_of(threadIdx.x >> 1);
+        bound[threadIdx.x >> 1][threadIdx.x & 1] = v < a.V ? lower_bound(a.key, a.n, (int32_t)v + (int)(threadIdx.x & 1)) : 0;
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & (kWave - 1);
+    for (int i = threadIdx.x / kWave; i < a.rows; i += kWaves) {
+        const int64_t v = row_of(i);
+        if (v >= a.V) continue;
+        const int from = bound[i][0], to = bound[i][1];
+        if (from == to && a.add) continue;
+        E* row = static_cast<E*>(a.G) + v * a.cols;
+        for (int c = lane * P::n; c < a.cols; c += kWave * P::n) {
+            float x[P::n] = {};
+            if (to - from <= a.part) {
+                add_rows<T, VEC>(a, from, to, c, x);
+            } else {
+                const int64_t b0 = from / a.part, b1 = (to - 1) / a.part;
+                for (int64_t b = b0; b <= b1; ++b) {
+                    // (the token's first stretch holds it as the second one if it begins inside)
+                    const float* sums = a.sums + (2 * b + (b == b0 && b0 * a.part != from ? 1 : 0)) * a.pitch + c;
+#pragma unroll
+                    for (int e = 0; e < P::n; ++e) x[e] += sums[e];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < P::n; ++e) x[e] *= a.scale;
+            if (a.add) {
+                float g[P::n];
+                P::load(row + c, g);
+#pragma unroll
+                for (int e = 0; e < P::n; ++e) x[e] += g[e];
+            }
+            P::store(row + c, x);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ dropout
+
+// Philox4x32-10 (Salmon, Moraes, Dror, Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011): four words from a counter of four
+// and a key of two.
+__device__ __forceinline__ void philox(uint64_t group, uint64_t call, uint64_t seed, uint32_t (&w)[4])
+{
+    uint32_t c0 = (uint32_t)group, c1 = (uint32_t)(group >> 32), c2 = (uint32_t)call, c3 = (uint32_t)(call >> 32);
+    uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
+        c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c3 = (uint32_t)a;
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
+}
+
+struct DropoutArgs {
+    const void* X;
+    const void* R;              // residual, or null
+    void* Y;
+    int64_t ldx, ldr, ldy;
+    int64_t n, cols;            // elements, and those of a row
+    uint32_t least;             // the smallest 16 bits that keep an element
+    float scale;
+    uint64_t seed, call;
+    const uint64_t* call_dev;   // takes the place of call, or null
+};
+
+constexpr int kDropout = 8;     // elements that share a counter
+
+// VEC: rows are whole groups of 16-byte aligned elements; else, and for the last elements, one by one.
+template <int T, bool VEC, bool RES>
+__global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a)
+{
+    typedef typename ElemOf<T>::type E;
+    const int64_t groups = (a.n + kDropout - 1) / kDropout;
+    const uint64_t call = a.call_dev ? *a.call_dev : a.call;
+    for (int64_t g = (int64_t)blockIdx.x * kBlock + threadIdx.x; g < groups; g += (int64_t)gridDim.x * kBlock) {
+        uint32_t w[4];
+        philox((uint64_t)g, call, a.seed, w);
+        const int64_t i = g * kDropout;
+        int64_t row, col;
+        if (a.cols >= a.n) { row = 0; col = i; }
+        else if (a.n <= 0xffffffffll) { row = (uint32_t)i / (uint32_t)a.cols; col = i - row * a.cols; }
+        else { row = i / a.cols; col = i - row * a.cols; }
+        const E* x = static_cast<const E*>(a.X) + row * a.ldx + col;
+        const E* r = RES ? static_cast<const E*>(a.R) + row * a.ldr + col : nullptr;
+        E* y = static_cast<E*>(a.Y) + row * a.ldy + col;
+        // (what is dropped is zero whatever it held)
+        const auto one = [&](int j, float v, float res) {
+            const float kept = ((w[j >> 1] >> (16 * (j & 1))) & 0xffffu) >= a.least ? v * a.scale : 0.f;
+            return RES ? kept + res : kept;
+        };
+        if (VEC && i + kDropout <= a.n) {
+            constexpr int kPieces = kDropout / Wide<T>::n;
+            typedef typename Wide<T>::vec V;
+            V vx[kPieces], vr[kPieces];
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                vx[p] = __builtin_nontemporal_load(reinterpret_cast<const V*>(x) + p);
+                if (RES) vr[p] = __builtin_nontemporal_load(reinterpret_cast<const V*>(r) + p);
+            }
+#pragma unroll
+            for (int p = 0; p < kPieces; ++p) {
+                V out;
+#pragma unroll
+                for (int e = 0; e < Wide<T>::n; ++e) out[e] = (E)one(p * Wide<T>::n + e, (float)vx[p][e], RES ? (float)vr[p][e] : 0.f);
+                __builtin_nontemporal_store(out, reinterpret_cast<V*>(y) + p);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < kDropout; ++j) {
+                if (i + j >= a.n) break;
+                *y = (E)one(j, (float)*x, RES ? (float)*r : 0.f);
+                ++x; ++y;
+                if (RES) ++r;
+                if (++col == a.cols) {
+                    col = 0;
+                    x += a.ldx - a.cols;
+                    y += a.ldy - a.cols;
+                    if (RES) r += a.ldr - a.cols;
+                }
+            }
+        }
+    }
+}
+
+}  // namespace
+#endif
