@@ -979,8 +979,9 @@ int hsadmm_dropout(const hsadmm_plan_t* plan, const void* X, int64_t x_stride, c
  *     f = mean ? scale / max(count, 1) : scale;   P_iv = exp(l_iv - lse_i) - [v = label_i], rows without a target 0
  *     dX = f P W;   the layer's rows of G = f P^T X (with `accumulate` added to what G holds)
  * `scale` multiplies the gradients alone (a loss scale of fp16 training).  Rows without a target cost nothing, and what X holds there
- * is not looked at.  Logits are formed in fp32 and held for a piece of the vocabulary at a time; P is rounded to `type` (half
- * precision: 2^15 P) for the products that follow.
+ * is not looked at.  Logits are formed in fp32; P is rounded to `type` (half precision: 2^15 P) for the products that follow, some of it
+ * from exponentials that were rounded to `type` before.  At most 2^30 bytes of either are held, a piece of the vocabulary: where it
+ * takes several, the logits of all but the last are formed twice.
  * Fill a zeroed hsadmm_softmax_loss_args_t; a NULL field means "not wanted"; at least one output is.
  *   struct_bytes  sizeof(hsadmm_softmax_loss_args_t) as the caller was compiled (INVALID_ARGUMENT if it differs)
  *   W             in, arena of weights, 16-byte aligned
@@ -1051,7 +1052,7 @@ int hsadmm_version(void);
  * profile taken elsewhere can be matched to the plan it is quoted for.
  * Errors: INVALID_ARGUMENT, HOST_MEMORY, HIP.
  */
-#define HSADMM_KERNEL_COUNT 52
+#define HSADMM_KERNEL_COUNT 51
 int hsadmm_kernel_timing_enable(hsadmm_plan_t* plan, int enable);
 int hsadmm_kernel_timing_read_n(hsadmm_plan_t* plan, double* total_ms, int64_t* launches, int32_t n);
 int hsadmm_kernel_timing_read(hsadmm_plan_t* plan, double* total_ms, int64_t* launches);
@@ -1087,7 +1088,8 @@ int hsadmm_kernel_grid(const hsadmm_plan_t* plan, int kernel_id);
  * selection in the one launch, in ticks of 10 ns (30000 without it; for tests); rows that have waited so long are written in
  * a form that is finished once the selection is there, within the same launch.  HSADMM_GRID_MOST: workgroups that one launch of
  * hsadmm_adamw or hsadmm_expand_mx takes (16777215 without it, what a grid holds; for tests); more work takes several launches.
- * HSADMM_LOSS_HELD: logits that hsadmm_softmax_loss holds at once (2^28 without it; for tests: small vocabularies then take several pieces).
+ * HSADMM_LOSS_HELD: bytes of logits that hsadmm_softmax_loss holds at once (2^30 without it; for tests: small vocabularies then take
+ * several pieces).
  */
 int hsadmm_plan_estimates(const hsadmm_plan_t* plan);
 /* Name of a kernel id ("" when out of range). */

@@ -116,13 +116,13 @@ struct WsLayout {
     size_t key, colpart, pos, cnt, layer_off, kept_idx, respart, work, rowres, pred, est_cnt, est_keys, est_thr, est_thr_tag, nest, total;
 };
 
-enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kLossTargets, kLossRows, kLossLogits, kLossJoin, kLossTotal, kLossSoftmax, kLossLogitGrads, kLossInputGrads, kLossWeightGrads, kLossInputs, kEmbedding, kTokenSort, kTokenCount, kTokenScan, kTokenMove, kEmbedParts, kEmbedGrad, kDropoutRows, kKernelCount };
+enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kLossTargets, kLossRows, kLossLogits, kLossTotal, kLossSoftmax, kLossLogitGrads, kLossInputGrads, kLossWeightGrads, kLossInputs, kEmbedding, kTokenSort, kTokenCount, kTokenScan, kTokenMove, kEmbedParts, kEmbedGrad, kDropoutRows, kKernelCount };
 static_assert(kKernelCount == HSADMM_KERNEL_COUNT, "kernel id table");
 constexpr size_t kTimingPairs = 8192;
 // Workgroups of one launch: a grid has fewer than 2^32 threads.  The update and the expansion of quantised buffers take several launches for
 // arenas of more than 17 G elements (or fewer, of several replicas).
 constexpr int64_t kGridMost = (1ll << 32) / kBlock - 1;
-constexpr int64_t kLossHeld = 1ll << 28;   // 1 GiB of logits, and half of it of their gradients in 16 bits
+constexpr int64_t kLossHeld = 1ll << 30;   // bytes of logits, and then their gradients, that hsadmm_softmax_loss holds at once
 constexpr size_t kRepairGrid = 2048;       // workgroups of the repair pass under a prediction: 8 per compute unit
 
 // Scratch of the entry point that takes no workspace argument (hsadmm_project_compact_static): one array per
@@ -158,7 +158,7 @@ struct hsadmm_plan {
     std::vector<int32_t> both_layers;   // their indices
     std::vector<FlatItem> items_flat;   // adamw, gradient_sqsums, scatter_mx: every layer cut without regard to rows
     int64_t grid_most = kGridMost;      // workgroups of one launch over the flat items
-    int64_t loss_held = kLossHeld;      // logits that hsadmm_softmax_loss holds at once
+    int64_t loss_held = kLossHeld;      // bytes of logits that hsadmm_softmax_loss holds at once
     int64_t packed_elems = 0;           // what the plan's own selection packs
     int64_t state_blocks = 0;           // blocks that share a scale in 8-bit optimizer states
     int64_t flat_stretches = 0;         // stretches of the flat items that hold elements (adamw: a workgroup's)
@@ -870,7 +870,7 @@ int hsadmm_plan_create_nested(const hsadmm_layer_t* layers, const hsadmm_nest_t*
         // (likewise HSADMM_GRID_MOST: workgroups of one launch of the update and of the expansion of quantised buffers, so that small
         // tables take several)
         if (const char* t = std::getenv("HSADMM_GRID_MOST")) p->grid_most = std::max(1ll, std::min(std::atoll(t), (long long)kGridMost));
-        // (likewise HSADMM_LOSS_HELD: logits that hsadmm_softmax_loss holds at once, so that small vocabularies take several pieces)
+        // (likewise HSADMM_LOSS_HELD: bytes of logits that hsadmm_softmax_loss holds at once, so that small vocabularies take several pieces)
         if (const char* t = std::getenv("HSADMM_LOSS_HELD")) p->loss_held = std::max(1ll, std::min(std::atoll(t), (long long)kLossHeld));
         if (p->n_held > 0) p->use_estimate = false;
         if (p->use_estimate) {
@@ -2363,7 +2363,6 @@ const char* hsadmm_kernel_name(int kernel_id)
         case kLossTargets: return "loss_targets";
         case kLossRows: return "loss_rows";
         case kLossLogits: return "loss_logits";
-        case kLossJoin: return "loss_join";
         case kLossTotal: return "loss_total";
         case kLossSoftmax: return "loss_softmax";
         case kLossLogitGrads: return "loss_logit_gradients";
@@ -2407,11 +2406,6 @@ static size_t span_of(int64_t rows, int64_t ld, int64_t cols, size_t size)
 {
     return rows > 0 && cols > 0 ? ((size_t)(rows - 1) * (size_t)ld + (size_t)cols) * size : 0;
 }
-// Rows that can be moved in pieces of 16 bytes.
-static bool whole_pieces(const void* at, int64_t ld, int64_t cols, size_t size)
-{
-    return is_aligned(at, 16) && ld * (int64_t)size % 16 == 0 && cols * (int64_t)size % 16 == 0;
-}
 static const void* at_elem(const void* arena, int64_t elem, size_t size) { return static_cast<const char*>(arena) + elem * (int64_t)size; }
 
 template <class F>
@@ -2445,20 +2439,16 @@ int hsadmm_embedding(const hsadmm_plan_t* p, int32_t layer, const void* W, int32
     used.add(out, span_of(n, out_stride, D, size), true);
     if (used.clash()) return HSADMM_ERR_INVALID_ARGUMENT;
     const void* rows = at_elem(W, off, size);
-    const bool vec = whole_pieces(rows, D, D, size) && whole_pieces(out, out_stride, D, size);
-    const int pieces = vec ? (int)(D * size / 16) : D;
+    const int pieces = (int)((D * size + 15) / 16);
     int lanes = 1;
     while (lanes < pieces && lanes < kBlock) lanes *= 2;
     const int64_t grid = (n + kBlock / lanes - 1) / (kBlock / lanes);
     if (grid > kGridMost) return HSADMM_ERR_UNSUPPORTED;
     const hipError_t e = for_type(type, [&](auto t) {
-        return for_flag(vec, [&](auto v) {
-            constexpr int T = decltype(t)::value;
-            typedef typename ElemOf<T>::type E;
-            return launch(p, kEmbedding, embedding_rows<T, decltype(v)::value>, (unsigned)grid, kBlock, static_cast<hipStream_t>(hip_stream),
-                          static_cast<const E*>(rows), V, (int)D, ids, (int)(index_bits == 64), n, scale, static_cast<E*>(out), out_stride,
-                          lanes);
-        });
+        constexpr int T = decltype(t)::value;
+        typedef typename ElemOf<T>::type E;
+        return launch(p, kEmbedding, embedding_rows<T>, (unsigned)grid, kBlock, static_cast<hipStream_t>(hip_stream), static_cast<const E*>(rows),
+                      V, (int)D, ids, (int)(index_bits == 64), n, scale, static_cast<E*>(out), out_stride, lanes);
     });
     return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
 }
@@ -2466,7 +2456,7 @@ int hsadmm_embedding(const hsadmm_plan_t* p, int32_t layer, const void* W, int32
 // Where the scratch of the embedding's gradient lies in its workspace.
 struct EmbedScratch {
     size_t key[2], pos[2], counts, sums, total;
-    int tiles, bits, passes, part;
+    int tile, tiles, bits, passes, part;
     int64_t stretches, pitch;
 };
 
@@ -2477,12 +2467,13 @@ static EmbedScratch embed_scratch(int32_t V, int32_t D, int64_t n)
     while (V >> width) ++width;
     s.passes = (width + kDigitBits - 1) / kDigitBits;
     s.bits = (width + s.passes - 1) / s.passes;
-    s.tiles = (int)((n + kSortTile - 1) / kSortTile);
+    s.tile = n <= kSortMost ? kSortMost : kSortTile;
+    s.tiles = (int)((n + s.tile - 1) / s.tile);
     // Stretches about as long as there are stretches, so that no row is a chain of more than some of either.
     s.part = 64;
     while ((int64_t)s.part * s.part * 4 < n) s.part *= 2;
     s.stretches = (n + s.part - 1) / s.part;
-    s.pitch = ((int64_t)D + 3) / 4 * 4;
+    s.pitch = ((int64_t)D + 7) / 8 * 8;
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t here = at; at = align_up(at + bytes, 256); return here; };
     for (int i = 0; i < 2; ++i) s.key[i] = take(4 * (size_t)n);
@@ -2537,7 +2528,7 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
         a.pos[i] = reinterpret_cast<int32_t*>(w + ws.pos[i]);
     }
     a.counts = reinterpret_cast<uint32_t*>(w + ws.counts);
-    a.tiles = ws.tiles; a.bits = ws.bits; a.passes = ws.passes;
+    a.tile = ws.tile; a.tiles = ws.tiles; a.bits = ws.bits; a.passes = ws.passes;
     hipError_t e = hipSuccess;
     if (ws.tiles == 1) {
         e = launch(p, kTokenSort, token_sort, 1u, kScanBlock, s, a);
@@ -2560,16 +2551,12 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     while (g.rows < kGradRows && V / g.rows > 2048) g.rows *= 2;
     g.run = 1;
     while (g.run < g.rows && g.run * D < 2048) g.run *= 2;
-    const bool vec = whole_pieces(g.G, D, D, size) && (n == 0 || whole_pieces(dY, dy_stride, D, size));
     e = for_type(type, [&](auto t) {
-        return for_flag(vec, [&](auto v) {
-            constexpr int T = decltype(t)::value;
-            constexpr bool kVec = decltype(v)::value;
-            hipError_t r = hipSuccess;
-            if (n > ws.part) r = launch(p, kEmbedParts, embedding_parts<T, kVec>, (unsigned)ws.stretches, kBlock, s, g);
-            if (r == hipSuccess) r = launch(p, kEmbedGrad, embedding_gradient<T, kVec>, (unsigned)((V + g.rows - 1) / g.rows), kBlock, s, g);
-            return r;
-        });
+        constexpr int T = decltype(t)::value;
+        hipError_t r = hipSuccess;
+        if (n > ws.part) r = launch(p, kEmbedParts, embedding_parts<T>, (unsigned)ws.stretches, kBlock, s, g);
+        if (r == hipSuccess) r = launch(p, kEmbedGrad, embedding_gradient<T>, (unsigned)((V + g.rows - 1) / g.rows), kBlock, s, g);
+        return r;
     });
     return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
 }
@@ -2603,78 +2590,102 @@ int hsadmm_dropout(const hsadmm_plan_t* p, const void* X, int64_t x_stride, cons
     a.ldx = x_stride; a.ldr = residual ? residual_stride : x_stride; a.ldy = y_stride;
     a.n = rows * width; a.cols = width;
     a.seed = seed; a.call = call; a.call_dev = call_device;
-    bool vec = is_aligned(X, 16) && is_aligned(Y, 16) && (!residual || is_aligned(residual, 16));
-    if (a.ldx == width && a.ldy == width && a.ldr == width) {
-        a.cols = a.n;                                   // one row
-    } else {
-        vec = vec && width % kDropout == 0 && a.ldx % kDropout == 0 && a.ldy % kDropout == 0 && a.ldr % kDropout == 0;
-    }
+    if (a.ldx == width && a.ldy == width && a.ldr == width) a.cols = a.n;         // one row
     const int64_t groups = (a.n + kDropout - 1) / kDropout;
     const int64_t grid = std::min<int64_t>((groups + kBlock - 1) / kBlock, 1 << 20);
     const hipError_t e = for_type(type, [&](auto t) {
-        return for_flag(vec, [&](auto v) {
-            return for_flag(residual != nullptr, [&](auto r) {
-                return launch(p, kDropoutRows, dropout_kernel<decltype(t)::value, decltype(v)::value, decltype(r)::value>, (unsigned)grid, kBlock,
-                              static_cast<hipStream_t>(hip_stream), a);
-            });
+        return for_flag(residual != nullptr, [&](auto r) {
+            return launch(p, kDropoutRows, dropout_kernel<decltype(t)::value, decltype(r)::value>, (unsigned)grid, kBlock,
+                          static_cast<hipStream_t>(hip_stream), a);
         });
     });
     return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
 }
 
+// The tile of a product: b by b elements of the output (kNarrow: 128 by 32), in `splits` parts of the k axis.
+constexpr int kNarrow = 32, kNarrowTile = 128;
+struct ProductPlan {
+    int b;
+    int splits;
+    int64_t k_part;
+    bool fills;          // tiles enough for the chip without parts
+};
+
+// The largest tile that has a workgroup for each of the chip's 256 compute units (tiles of 256: 16-bit types only); with parts
+// allowed, parts of `least` of k count too, and their number is the one that leaves the fewest compute units idle in the last round.
+static ProductPlan plan_product(int64_t out_p, int64_t out_q, int64_t k, bool sixteen, bool narrow, bool parts)
+{
+    constexpr int64_t kUnits = 256;
+    const auto tiles = [&](int64_t b) { return narrow ? (out_p + kNarrowTile - 1) / kNarrowTile : ((out_p + b - 1) / b) * ((out_q + b - 1) / b); };
+    const auto most_parts = [&](int64_t b) { return parts ? std::max<int64_t>(1, k / (4 * b)) : 1; };
+    ProductPlan r{};
+    r.b = narrow ? kNarrow : sixteen && tiles(256) * most_parts(256) >= kUnits ? 256 : tiles(128) * most_parts(128) >= kUnits ? 128 : 64;
+    const int64_t n = tiles(r.b);
+    r.fills = n >= kUnits;
+    r.splits = 1;
+    if (parts && k > 0) {
+        const int64_t at_once = kUnits * (r.b == 256 ? 1 : r.b == 128 ? 2 : 4);        // workgroups that share the chip
+        const int64_t most = std::min<int64_t>({r.b >= 128 ? most_parts(r.b) : std::max<int64_t>(1, k / 128), std::max<int64_t>(1, 2 * at_once / n), 64});
+        double best = 0.0;
+        for (int64_t s = 1; s <= most; ++s) {
+            const int64_t rounds = (n * s + at_once - 1) / at_once;
+            const double part = (double)(n * s) / (double)(rounds * at_once) * (1.0 - 0.01 * (double)s);
+            if (part > best) { best = part; r.splits = (int)s; }
+        }
+    }
+    r.k_part = std::max<int64_t>(64, (k + r.splits * 64 - 1) / (r.splits * 64) * 64);
+    r.splits = (int)std::max<int64_t>(1, (k + r.k_part - 1) / r.k_part);
+    return r;
+}
+
 // How hsadmm_softmax_loss cuts its products, and where its scratch lies in the workspace.
 struct LossScratch {
-    size_t head, row, label, place, held, picked, stat, slab, rows, packed, logits, grads, sums, total;
+    size_t head, row, label, place, held_loss, picked, stat, slab, rows, packed, parts, grads, sums, total;
     int64_t Np, Dp;             // rows and columns of the held inputs
     int64_t Vc;                 // classes of a piece, a multiple of 256
     int pieces;
     bool pack;                  // W's rows are copied before they are used (not whole pieces of 16 bytes)
-    bool narrow;                        // tiles of 128 x 32, else 128 x 128 or (wide) 256 x 256
-    bool wide, wide_inputs, wide_weights;   // of the logits, of the inputs' and the weights' gradients
-    int splits;                 // of the classes, in the inputs' gradient
-    int64_t k_part;
+    bool small;                 // logits in parts, joined by rows
+    ProductPlan logits, inputs, weights;
     int slab_elems;
+    int64_t slabs;
 };
-
-// Tiles of 256 x 256 where they are enough to fill the chip, else 128 x 128.
-static bool fills(int64_t a, int64_t b) { return ((a + 255) / 256) * ((b + 255) / 256) >= 256; }
 
 static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int64_t off, int64_t n, int32_t type, bool gradients)
 {
     LossScratch s{};
     const int64_t size = (int64_t)type_size(type);
-    s.narrow = n <= 32;
-    s.Np = s.narrow ? 32 : (n + kInputRows - 1) / kInputRows * kInputRows;
+    const bool narrow = n <= kNarrow, sixteen = size == 2;
+    s.Np = n <= 128 ? 128 : (n + kInputRows - 1) / kInputRows * kInputRows;
     s.Dp = ((int64_t)D + kInputCols - 1) / kInputCols * kInputCols;
     s.pack = D * size % 16 != 0 || off * size % 16 != 0;
-    const int64_t most = std::max<int64_t>(256, p->loss_held / s.Np / 256 * 256);
+    const int64_t most = std::max<int64_t>(256, p->loss_held / size / s.Np / 256 * 256);
     s.pieces = gradients || s.pack ? (int)((V + most - 1) / most) : 1;
     s.Vc = ((V + s.pieces - 1) / s.pieces + 255) / 256 * 256;
     s.pieces = (int)((V + s.Vc - 1) / s.Vc);
-    s.wide = size == 2 && !s.narrow && fills(n, s.Vc);
-    s.wide_inputs = size == 2 && !s.narrow && fills(n, D);
-    s.wide_weights = size == 2 && fills(s.Vc, D);
-    s.slab_elems = s.narrow ? 32 : s.wide ? 128 : 64;
-    const int64_t tiles = s.narrow ? (D + 127) / 128 : s.wide_inputs ? ((n + 255) / 256) * ((D + 255) / 256) : ((n + 127) / 128) * ((D + 127) / 128);
-    s.splits = (int)std::max<int64_t>(1, std::min<int64_t>({512 / tiles, s.Vc / 256, 64}));
-    s.k_part = ((s.Vc + s.splits - 1) / s.splits + 63) / 64 * 64;
-    s.splits = (int)((s.Vc + s.k_part - 1) / s.k_part);
-    const int64_t slabs = (V + s.slab_elems - 1) / s.slab_elems + 256 / s.slab_elems;
+    s.logits = plan_product(V, n, s.Dp, sixteen, narrow, false);
+    s.small = !s.logits.fills && s.pieces == 1;
+    if (s.small) s.logits = plan_product(V, n, s.Dp, sixteen, narrow, true);
+    else if (!narrow && s.logits.b == 64) s.logits.b = 128;
+    s.inputs = plan_product(D, n, s.Vc, sixteen, narrow, true);
+    s.weights = plan_product(D, std::min<int64_t>(V, s.Vc), n, sixteen, false, false);
+    s.slab_elems = s.logits.b == kNarrow ? 32 : s.logits.b / 2;
+    s.slabs = s.small ? 0 : (V + 255) / 256 * (256 / s.slab_elems);
     size_t at = 0;
     const auto take = [&](int64_t bytes) { const size_t here = at; at = align_up(at + (size_t)bytes, 256); return here; };
     s.head = take(sizeof(LossHead));
     s.row = take(4 * s.Np);
     s.label = take(4 * s.Np);
     s.place = take(4 * s.Np);
-    s.held = take(4 * s.Np);
+    s.held_loss = take(4 * s.Np);
     s.picked = take(4 * s.Np);
     s.stat = take(8 * s.Np);
-    s.slab = take(8 * slabs * s.Np);
+    s.slab = take(8 * s.slabs * s.Np);
     s.rows = take(size * s.Np * s.Dp);
     s.packed = take(s.pack ? size * s.Vc * s.Dp : 0);
-    s.logits = take(gradients ? 4 * s.Np * s.Vc : 0);
-    s.grads = gradients && size == 2 ? take(2 * s.Np * s.Vc) : s.logits;
-    s.sums = take(gradients ? 4 * (int64_t)s.splits * s.Np * s.Dp : 0);
+    s.parts = take(s.small ? 4 * (int64_t)s.logits.splits * s.Np * s.Vc : 0);
+    s.grads = take(gradients ? size * s.Np * s.Vc : 0);
+    s.sums = take(gradients ? 4 * (int64_t)s.inputs.splits * s.Np * s.Dp : 0);
     s.total = at;
     return s;
 }
@@ -2690,11 +2701,13 @@ int hsadmm_softmax_loss_workspace(const hsadmm_plan_t* p, int32_t layer, int64_t
     return HSADMM_OK;
 }
 
-// One product over all tiles of its output; the tile's form by the sizes.
+// One product over all tiles of its output.
 template <int T, bool PMAJOR, bool QMAJOR, int WHAT>
-static hipError_t launch_product(const hsadmm_plan* p, KernelId kid, bool narrow, bool wide, int64_t out_p, int64_t out_q, ProductArgs a,
+static hipError_t launch_product(const hsadmm_plan* p, KernelId kid, const ProductPlan& how, int64_t out_p, int64_t out_q, ProductArgs a,
                                  hipStream_t s)
 {
+    a.splits = how.splits;
+    a.k_part = how.k_part;
     const auto go = [&](auto kernel, int bp, int bq, int threads) {
         a.tiles_p = (int)((out_p + bp - 1) / bp);
         a.tiles_q = (int)((out_q + bq - 1) / bq);
@@ -2702,10 +2715,13 @@ static hipError_t launch_product(const hsadmm_plan* p, KernelId kid, bool narrow
         if (grid >= (1ll << 32) / threads) return hipErrorInvalidConfiguration;
         return launch(p, kid, kernel, (unsigned)grid, (unsigned)threads, s, a);
     };
-    if constexpr (WHAT != kWeightGrads)
-        if (narrow) return go(loss_product<T, 128, 32, 4, 1, PMAJOR, QMAJOR, WHAT>, 128, 32, 256);
+    constexpr bool kBySlabs = WHAT == kLogits || WHAT == kLogitGrads;
+    if constexpr (WHAT == kLogits || WHAT == kSums)
+        if (how.b == kNarrow) return go(loss_product<T, kNarrowTile, kNarrow, 4, 1, PMAJOR, QMAJOR, WHAT>, kNarrowTile, kNarrow, 256);
     if constexpr (T != HSADMM_TYPE_F32)
-        if (wide) return go(loss_product<T, 256, 256, 2, 4, PMAJOR, QMAJOR, WHAT>, 256, 256, 512);
+        if (how.b == 256) return go(loss_product<T, 256, 256, 2, 4, PMAJOR, QMAJOR, WHAT>, 256, 256, 512);
+    if constexpr (!kBySlabs)
+        if (how.b == 64) return go(loss_product<T, 64, 64, 2, 2, PMAJOR, QMAJOR, WHAT>, 64, 64, 256);
     return go(loss_product<T, 128, 128, 2, 2, PMAJOR, QMAJOR, WHAT>, 128, 128, 256);
 }
 
@@ -2717,35 +2733,27 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
     const int64_t size = sizeof(E), n = x->n;
     const bool gradients = x->dX || x->G;
     char* w = static_cast<char*>(x->workspace);
-    LossRows r{reinterpret_cast<LossHead*>(w + ws.head), reinterpret_cast<int32_t*>(w + ws.row), reinterpret_cast<int32_t*>(w + ws.label),
-               reinterpret_cast<int32_t*>(w + ws.place)};
-    float* held = reinterpret_cast<float*>(w + ws.held);
-    float2* stat = reinterpret_cast<float2*>(w + ws.stat);
+    const LossRows r{reinterpret_cast<LossHead*>(w + ws.head), reinterpret_cast<int32_t*>(w + ws.row), reinterpret_cast<int32_t*>(w + ws.label),
+                     reinterpret_cast<int32_t*>(w + ws.place)};
+    float* held_loss = reinterpret_cast<float*>(w + ws.held_loss);
     E* rows = reinterpret_cast<E*>(w + ws.rows);
     E* packed = reinterpret_cast<E*>(w + ws.packed);
     const E* W = static_cast<const E*>(at_elem(x->W, off, size));
     hipError_t e = launch(p, kLossTargets, loss_targets, 1u, kScanBlock, s, x->labels, (int)(x->index_bits == 64), n, V, x->scale,
                           (int)(x->mean != 0), r, x->loss, x->lse);
     if (e == hipSuccess && n > 0)
-        e = for_flag(whole_pieces(x->X, x->x_stride, D, size), [&](auto v) {
-            return launch(p, kLossRows, loss_rows<T, decltype(v)::value, true>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s,
-                          static_cast<const E*>(x->X), x->x_stride, n, (int)D, r, rows, (int)ws.Dp);
-        });
+        e = launch(p, kLossRows, loss_rows<T, true>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s, static_cast<const E*>(x->X), x->x_stride,
+                   n, (int)D, r, rows, (int)ws.Dp);
     ProductArgs a{};
     a.head = r.head;
-    a.splits = 1;
     a.V = V;
     a.label = r.label;
     a.picked = reinterpret_cast<float*>(w + ws.picked);
     a.slab = reinterpret_cast<float2*>(w + ws.slab);
-    a.rows = ws.Np;
-    a.logit_ld = ws.Vc;
-    a.stat = stat;
-    a.grads = w + ws.grads;
-    a.sums = reinterpret_cast<float*>(w + ws.sums);
-    a.sum_ld = ws.Dp;
-    a.sum_part = ws.Np * ws.Dp;
-    a.out_ld = D;
+    a.slabs = ws.slabs;
+    a.held = w + ws.grads;
+    a.ld = ws.Vc;
+    a.stat = reinterpret_cast<float2*>(w + ws.stat);
     const Operand inputs{rows, ws.Dp, ws.Np, ws.Dp};
     // the weights of the classes from v0 on, `classes` of them
     const auto weights = [&](int32_t v0, int64_t classes, Operand* o) -> hipError_t {
@@ -2754,12 +2762,12 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
             return hipSuccess;
         }
         *o = Operand{packed, ws.Dp, classes, ws.Dp};
-        return launch(p, kLossRows, loss_rows<T, false, false>, (unsigned)((classes + kWaves - 1) / kWaves), kBlock, s, W + (int64_t)v0 * D,
+        return launch(p, kLossRows, loss_rows<T, false>, (unsigned)((classes + kWaves - 1) / kWaves), kBlock, s, W + (int64_t)v0 * D,
                       (int64_t)D, classes, (int)D, r, packed, (int)ws.Dp);
     };
     const int32_t last = (int32_t)((ws.pieces - 1) * ws.Vc);
     if (n > 0) {
-        // forward: all classes at once, or, where the weights are copied, piece by piece; the last piece's logits are kept
+        // forward: all classes at once, or, where the weights are copied, piece by piece; the last piece's logits are held
         for (int i = 0; i < (ws.pack ? ws.pieces : 1) && e == hipSuccess; ++i) {
             const int32_t v0 = ws.pack ? (int32_t)(i * ws.Vc) : 0;
             const int64_t classes = ws.pack ? std::min<int64_t>(ws.Vc, V - v0) : V;
@@ -2767,69 +2775,82 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
             e = weights(v0, classes, &f.p);
             if (e != hipSuccess) break;
             f.q = inputs;
-            f.k_part = ws.Dp;
             f.v0 = v0;
             f.keep0 = last;
-            f.logits = gradients && v0 + classes == V ? reinterpret_cast<float*>(w + ws.logits) : nullptr;
-            e = launch_product<T, false, false, kLogits>(p, kLossLogits, ws.narrow, ws.wide, classes, n, f, s);
+            if (!gradients || v0 + classes != V) f.held = nullptr;
+            if (ws.small) {
+                f.sums = reinterpret_cast<float*>(w + ws.parts);
+                f.sum_part = ws.Np * ws.Vc;
+                e = launch_product<T, false, false, kSums>(p, kLossLogits, ws.logits, classes, n, f, s);
+            } else {
+                e = launch_product<T, false, false, kLogits>(p, kLossLogits, ws.logits, classes, n, f, s);
+            }
         }
-        const int slabs = (int)((V + ws.slab_elems - 1) / ws.slab_elems);
-        const auto join = [&](auto rows_at_once) {
-            constexpr int kRows = decltype(rows_at_once)::value;
-            return launch(p, kLossJoin, loss_join<kRows>, (unsigned)((n + kRows - 1) / kRows), kBlock, s, (const float2*)a.slab, slabs, ws.Np,
-                          (const float*)a.picked, r, stat, held, x->loss, x->lse);
-        };
-        if (e == hipSuccess) e = n <= 256 ? join(std::integral_constant<int, 1>{}) : join(std::integral_constant<int, 32>{});
+        SoftmaxArgs m{};
+        m.r = r;
+        if (!ws.small) m.slab = a.slab;
+        m.slabs = (int)((V + ws.slab_elems - 1) / ws.slab_elems);
+        m.pitch = ws.slabs;
+        m.slab_elems = ws.slab_elems;
+        m.picked = a.picked;
+        m.sums = reinterpret_cast<const float*>(w + ws.parts);
+        m.parts = ws.logits.splits;
+        m.sum_part = ws.Np * ws.Vc;
+        m.stat = reinterpret_cast<float2*>(w + ws.stat);
+        m.held_loss = held_loss;
+        m.loss = x->loss; m.lse = x->lse;
+        m.held = w + ws.grads;
+        m.grads = gradients ? w + ws.grads : nullptr;
+        m.ld = ws.Vc;
+        m.v0 = last; m.V = V;
+        // (a row of few elements keeps a small workgroup busy; few rows have to share the chip by themselves)
+        const int64_t work = gradients || ws.small ? ws.Vc / 8 : m.slabs;
+        const unsigned threads = work <= 256 ? 64 : work <= 2048 && n >= 512 ? kBlock : kScanBlock;
+        if (e == hipSuccess) e = launch(p, kLossSoftmax, loss_softmax<T>, (unsigned)n, threads, s, m);
     }
     if (e == hipSuccess && x->total)
-        e = launch(p, kLossTotal, loss_total, 1u, kBlock, s, (const LossHead*)r.head, (const float*)held, (int)(x->mean != 0), x->total);
+        e = launch(p, kLossTotal, loss_total, 1u, kBlock, s, (const LossHead*)r.head, (const float*)held_loss, (int)(x->mean != 0), x->total);
     if (!gradients) return e;
     for (int i = ws.pieces - 1; i >= 0 && e == hipSuccess; --i) {
         const int32_t v0 = (int32_t)(i * ws.Vc);
         const int64_t classes = std::min<int64_t>(ws.Vc, V - v0);
-        Operand some{};
+        Operand some{packed, ws.Dp, classes, ws.Dp};
         if (v0 != last || !ws.pack) e = weights(v0, classes, &some);
-        else some = Operand{packed, ws.Dp, classes, ws.Dp};
-        if (e != hipSuccess) break;
-        if (n > 0) {
-            if (v0 == last) {
-                const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(ws.Vc / (4 * kBlock), 65536 / std::max<int64_t>(1, n)));
-                e = launch(p, kLossSoftmax, loss_softmax<T>, (unsigned)(n * parts), kBlock, s, (const float*)(w + ws.logits),
-                           reinterpret_cast<E*>(w + ws.grads), ws.Vc, v0, V, (const float2*)stat, (const int32_t*)r.label,
-                           (const LossHead*)r.head, parts);
-            } else {
-                ProductArgs f = a;
-                f.p = some;
-                f.q = inputs;
-                f.k_part = ws.Dp;
-                f.v0 = v0;
-                e = launch_product<T, false, false, kLogitGrads>(p, kLossLogitGrads, ws.narrow, ws.wide, classes, n, f, s);
-            }
+        if (e == hipSuccess && v0 != last && n > 0) {
+            ProductArgs f = a;
+            f.p = some;
+            f.q = inputs;
+            f.v0 = v0;
+            ProductPlan how = ws.logits;
+            if (how.b == kNarrow) how.b = 128;
+            e = launch_product<T, false, false, kLogitGrads>(p, kLossLogitGrads, how, classes, n, f, s);
         }
         // (classes behind the last one have gradients of zero up to the end of a tile of 64 at least)
         if (e == hipSuccess && x->dX && n > 0) {
             ProductArgs f = a;
             f.p = Operand{some.at, some.ld, D, classes};
             f.q = Operand{w + ws.grads, ws.Vc, ws.Np, (classes + 63) / 64 * 64};
-            f.splits = ws.splits;
-            f.k_part = ws.k_part;
+            f.sums = reinterpret_cast<float*>(w + ws.sums);
+            f.sum_part = ws.Np * ws.Dp;
+            f.ld = ws.Dp;
             f.add = v0 != last;
-            e = launch_product<T, true, false, kInputGrads>(p, kLossInputGrads, ws.narrow, ws.wide_inputs, D, n, f, s);
+            e = launch_product<T, true, false, kSums>(p, kLossInputGrads, ws.inputs, D, n, f, s);
         }
         if (e == hipSuccess && x->G) {
             ProductArgs f = a;
             f.p = Operand{rows, ws.Dp, ws.Dp, 0};
             f.q = Operand{w + ws.grads, ws.Vc, classes, 0};
-            f.k_part = INT64_MAX / 2;
             f.out = static_cast<E*>(x->G) + off + (int64_t)v0 * D;
+            f.ld = D;
             f.add = x->accumulate != 0;
-            e = launch_product<T, true, true, kWeightGrads>(p, kLossWeightGrads, false, ws.wide_weights, D, classes, f, s);
+            ProductPlan how = ws.weights;
+            how.k_part = INT64_MAX / 2;
+            e = launch_product<T, true, true, kWeightGrads>(p, kLossWeightGrads, how, D, classes, f, s);
         }
     }
     if (e == hipSuccess && x->dX && n > 0)
-        e = launch(p, kLossInputs, loss_inputs<T>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s, (const float*)a.sums, ws.splits, a.sum_part,
-                   a.sum_ld, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D,
-                   (int)(x->dx_stride % 4 == 0 && is_aligned(x->dX, 4 * size)));
+        e = launch(p, kLossInputs, loss_inputs<T>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s, (const float*)(w + ws.sums), ws.inputs.splits,
+                   ws.Np * ws.Dp, ws.Dp, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D);
     return e;
 }
 

@@ -17,9 +17,36 @@ typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-template <int T> struct Wide { typedef v4f vec; static constexpr int n = 4; };        // 16 bytes of elements
-template <> struct Wide<HSADMM_TYPE_BF16> { typedef v8bf vec; static constexpr int n = 8; };
-template <> struct Wide<HSADMM_TYPE_F16> { typedef v8h vec; static constexpr int n = 8; };
+typedef __bf16 v8bf_at2 __attribute__((ext_vector_type(8), aligned(2)));      // at any element's address
+typedef _Float16 v8h_at2 __attribute__((ext_vector_type(8), aligned(2)));
+
+template <int T> struct Wide { typedef v4f vec; typedef v4f_at4 any; static constexpr int n = 4; };        // 16 bytes of elements
+template <> struct Wide<HSADMM_TYPE_BF16> { typedef v8bf vec; typedef v8bf_at2 any; static constexpr int n = 8; };
+template <> struct Wide<HSADMM_TYPE_F16> { typedef v8h vec; typedef v8h_at2 any; static constexpr int n = 8; };
+
+// 16 bytes of a row from p on, of which `left` elements belong to the row (zeros behind them).  Rows may start at any element: an
+// access of 16 bytes that is aligned to its elements only costs a wave a cache line more.
+template <int T>
+__device__ __forceinline__ typename Wide<T>::vec load_piece(const typename ElemOf<T>::type* p, int left)
+{
+    if (left >= Wide<T>::n) return *reinterpret_cast<const typename Wide<T>::any*>(p);
+    typename Wide<T>::vec v = {};
+#pragma unroll
+    for (int i = 0; i < Wide<T>::n; ++i)
+        if (i < left) v[i] = p[i];
+    return v;
+}
+template <int T>
+__device__ __forceinline__ void store_piece(typename ElemOf<T>::type* p, typename Wide<T>::vec v, int left)
+{
+    if (left >= Wide<T>::n) {
+        *reinterpret_cast<typename Wide<T>::any*>(p) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < Wide<T>::n; ++i)
+        if (i < left) p[i] = v[i];
+}
 
 __device__ __forceinline__ int64_t index_at(const void* p, bool wide, int64_t i)
 {
@@ -89,30 +116,17 @@ __global__ __launch_bounds__(kScanBlock) void loss_targets(const void* __restric
 
 // Copies rows of `cols` elements that lie ld apart to rows of `pitch` (a multiple of kInputCols), zeros behind the last column.  LIST:
 // the rows of the list (those that have a target: what the others hold, NaN included, is not looked at again).  The products then
-// load whole 16-byte pieces and know no strides.  A wave takes a row; VEC: the source's rows are whole 16-byte pieces.
-template <int T, bool VEC, bool LIST>
+// load whole 16-byte pieces and know no strides.  A wave takes a row.
+template <int T, bool LIST>
 __global__ __launch_bounds__(kBlock) void loss_rows(const typename ElemOf<T>::type* __restrict__ src, int64_t ld, int64_t rows, int cols,
                                                     LossRows r, typename ElemOf<T>::type* __restrict__ dst, int pitch)
 {
-    typedef typename ElemOf<T>::type E;
-    typedef typename Wide<T>::vec V;
     constexpr int n = Wide<T>::n;
     const int64_t j = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
-    const int lane = threadIdx.x % kWave;
     if (j >= (LIST ? (int64_t)r.head->count : rows)) return;
-    const E* from = src + (LIST ? (int64_t)r.row[j] : j) * ld;
-    E* to = dst + j * pitch;
-    for (int c = lane * n; c < pitch; c += kWave * n) {
-        V v = {};
-        if constexpr (VEC) {
-            if (c < cols) v = *reinterpret_cast<const V*>(from + c);
-        } else {
-#pragma unroll
-            for (int i = 0; i < n; ++i)
-                if (c + i < cols) v[i] = from[c + i];
-        }
-        *reinterpret_cast<V*>(to + c) = v;
-    }
+    const typename ElemOf<T>::type* from = src + (LIST ? (int64_t)r.row[j] : j) * ld;
+    for (int c = (threadIdx.x % kWave) * n; c < pitch; c += kWave * n)
+        *reinterpret_cast<typename Wide<T>::vec*>(dst + j * pitch + c) = load_piece<T>(from + c, cols - c);
 }
 
 // ------------------------------------------------------------------ products
@@ -125,30 +139,30 @@ struct Operand {
     int64_t mn, k;
 };
 
-enum LossProduct { kLogits = 0, kLogitGrads, kInputGrads, kWeightGrads };
+// kSums: the product itself in fp32, in parts of the k axis that somebody adds up (the inputs' gradients; logits of small calls).
+enum LossProduct { kLogits = 0, kLogitGrads, kSums, kWeightGrads };
 
 struct ProductArgs {
     Operand p, q;               // p: the output's adjacent index, q: its rows
     const LossHead* head;
     int tiles_p, tiles_q;       // tiles of the output
-    int splits;                 // parts of the k axis (kInputGrads)
+    int splits;                 // parts of the k axis (kSums)
     int64_t k_part;             // length of a part, a multiple of the tile's
     // kLogits, kLogitGrads
     int32_t v0, V;              // first class of the piece, all classes
     const int32_t* label;
     float* picked;              // [rows] the label's logit
-    float2* slab;               // [classes / slab][rows]: largest logit and sum of exponentials of a slab of classes
-    int64_t rows;               // pitch of slab
-    float* logits;              // [rows][logit_ld], classes from keep0 on, or null
+    float2* slab;               // [rows][slabs]: largest logit and sum of exponentials of a slab of classes
+    int64_t slabs;
+    void* held;                 // [rows][ld], classes from keep0 on, or null.  kLogits: fp32 logits, or in 16 bits the exponentials of
+                                // what is left of them when their slab's largest is taken off; kLogitGrads: their gradients
     int32_t keep0;
-    int64_t logit_ld;
+    int64_t ld;
     const float2* stat;         // [rows] largest logit, 1 / sum
-    void* grads;                // kLogitGrads: [rows][logit_ld]
-    // kInputGrads: sums [splits][rows][sum_ld], kWeightGrads: rows of D elements
+    // kSums: [splits][rows][ld]; kWeightGrads: rows of ld elements, part of an arena
     float* sums;
-    int64_t sum_ld, sum_part;
+    int64_t sum_part;
     void* out;
-    int64_t out_ld;
     int add;                    // to what is there
 };
 
@@ -361,26 +375,31 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) sum += exp_of(acc[i][j][e] - from);
+                for (int e = 0; e < 16; ++e) {
+                    const float x = exp_of(acc[i][j][e] - from);
+                    sum += x;
+                    if constexpr (T != HSADMM_TYPE_F32) acc[i][j][e] = x;
+                }
             sum += __shfl_xor(sum, 32, kWave);
-            const int64_t slab = (a.v0 + p0 + wp) / (BP / WP);
-            if (half == 0) a.slab[slab * a.rows + q] = make_float2(top, sum);
-            if (a.logits) {
-                float* row = a.logits + q * a.logit_ld;
+            if (half == 0) a.slab[q * a.slabs + (a.v0 + p0 + wp) / (BP / WP)] = make_float2(top, sum);
+            if (a.held) {
+                typedef typename ElemOf<T>::vec V4;
+                E* row = static_cast<E*>(a.held) + q * a.ld;
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
 #pragma unroll
                     for (int g = 0; g < 4; ++g) {
                         const int64_t c = a.v0 + p0 + wp + 32 * i + 8 * g + 4 * half - a.keep0;
-                        const v4f x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                        if (c >= 0 && c < a.logit_ld) *reinterpret_cast<v4f*>(row + c) = x;
+                        v4f x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                        if constexpr (T != HSADMM_TYPE_F32) x *= grad_unit<T>();
+                        if (c >= 0 && c < a.ld) *reinterpret_cast<V4*>(row + c) = __builtin_convertvector(x, V4);
                     }
             }
         } else if constexpr (WHAT == kLogitGrads) {
             const bool live = q < count;
             const int label = live ? a.label[q] : -1;
             const float2 stat = live ? a.stat[q] : make_float2(0.f, 0.f);
-            E* row = static_cast<E*>(a.grads) + q * a.logit_ld;
+            E* row = static_cast<E*>(a.held) + q * a.ld;
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
@@ -393,17 +412,17 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                         const float y = (exp_of(acc[i][j][4 * g + e] - stat.x) * stat.y - (v == label ? 1.f : 0.f)) * grad_unit<T>();
                         x[e] = live && v < a.V ? y : 0.f;
                     }
-                    if (c < a.logit_ld) *reinterpret_cast<typename ElemOf<T>::vec*>(row + c) = __builtin_convertvector(x, typename ElemOf<T>::vec);
+                    if (c < a.ld) *reinterpret_cast<typename ElemOf<T>::vec*>(row + c) = __builtin_convertvector(x, typename ElemOf<T>::vec);
                 }
-        } else if constexpr (WHAT == kInputGrads) {
-            float* row = a.sums + part * a.sum_part + q * a.sum_ld;
+        } else if constexpr (WHAT == kSums) {
+            float* row = a.sums + part * a.sum_part + q * a.ld;
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int64_t c = p0 + wp + 32 * i + 8 * g + 4 * half;
                     v4f x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                    if (c < a.sum_ld) {
+                    if (c < a.ld) {
                         if (a.add) x += *reinterpret_cast<const v4f*>(row + c);
                         *reinterpret_cast<v4f*>(row + c) = x;
                     }
@@ -411,15 +430,15 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
         } else {
             if (q >= a.q.mn) continue;
             const float f = a.head->factor * (1.f / grad_unit<T>());
-            E* row = static_cast<E*>(a.out) + q * a.out_ld;
-            const bool whole = a.out_ld % 4 == 0;       // (an arena's layers start at multiples of four elements)
+            E* row = static_cast<E*>(a.out) + q * a.ld;
+            const bool whole = a.ld % 4 == 0;       // (an arena's layers start at multiples of four elements)
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int64_t c = p0 + wp + 32 * i + 8 * g + 4 * half;
                     const v4f x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                    const int nv = (int)min((int64_t)4, a.out_ld - c);
+                    const int nv = (int)min((int64_t)4, a.ld - c);
                     if (nv > 0) put4<T>(row + c, x * f, nv, whole, a.add != 0);
                 }
         }
@@ -428,50 +447,101 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
 
 // ------------------------------------------------------------------ between the products
 
-// Every row's slabs joined: the largest logit, the sum, the loss.  ROWS rows a workgroup (adjacent lanes read adjacent rows); the order
-// of the additions depends on the sizes alone.
-template <int ROWS>
-__global__ __launch_bounds__(kBlock) void loss_join(const float2* __restrict__ slab, int n_slabs, int64_t pitch, const float* __restrict__ picked,
-                                                    LossRows r, float2* __restrict__ stat, float* __restrict__ held,
-                                                    float* __restrict__ loss, float* __restrict__ lse)
+struct SoftmaxArgs {
+    LossRows r;
+    const float2* slab;         // what kLogits wrote of a row ...
+    int slabs;                  // (its slabs)
+    int64_t pitch;
+    int slab_elems;
+    const float* picked;
+    const float* sums;          // ... or, slab null, the logits in parts: [parts][rows][ld]
+    int parts;
+    int64_t sum_part;
+    float2* stat;
+    float* held_loss;           // [rows], for the total
+    float* loss;                // by original rows, may be null
+    float* lse;
+    const void* held;           // with slabs: of the classes from v0 on, as kLogits wrote them
+    void* grads;                // [rows][ld] gradients of the logits, may be null; with slabs held itself
+    int64_t ld;
+    int32_t v0, V;
+};
+
+__device__ __forceinline__ float2 join(float2 a, float2 b)
 {
-    constexpr int kGroups = kBlock / ROWS;
-    __shared__ float2 red[kBlock];
-    const int lane = threadIdx.x % ROWS, g = threadIdx.x / ROWS;
-    const int64_t q = (int64_t)blockIdx.x * ROWS + lane;
-    const int count = r.head->count;
-    if ((int64_t)blockIdx.x * ROWS >= count) return;
-    const auto join = [](float2 a, float2 b) {
-        // (a side without any value has the sum 0 and the largest value -inf; NaN in a sum stays)
-        const float top = fmaxf(a.x, b.x), from = top == -__builtin_inff() ? 0.f : top;
-        return make_float2(top, a.y * exp_of(a.x - from) + b.y * exp_of(b.x - from));
-    };
+    // (a side without any value has the sum 0 and the largest value -inf; NaN in a sum stays)
+    const float top = fmaxf(a.x, b.x), from = top == -__builtin_inff() ? 0.f : top;
+    return make_float2(top, a.y * exp_of(a.x - from) + b.y * exp_of(b.x - from));
+}
+
+// A row per workgroup: largest logit, sum, loss, and the gradients of the logits that are held (softmax minus the label's one).  The order
+// of the additions depends on the sizes alone.  16 bits: what kLogits held is rounded already, so a gradient here carries two
+// roundings; the label's own comes from its logit in fp32, as softmax - 1 of a confident row has far fewer digits than either.
+template <int T>
+__global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
+{
+    typedef typename ElemOf<T>::type E;
+    typedef typename Wide<T>::vec V;
+    constexpr int n = Wide<T>::n;
+    __shared__ float2 red[kScanWaves];
+    const int64_t q = blockIdx.x;
+    if (q >= a.r.head->count) return;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave, threads = blockDim.x;
+    const int label = a.r.label[q];
     float2 s = make_float2(-__builtin_inff(), 0.f);
-    if (q < count) {
-        int i = g;
-        for (; i + 7 * kGroups < n_slabs; i += 8 * kGroups) {
-            float2 x[8];
+    float* sum_row = const_cast<float*>(a.sums) + q * a.ld;
+    if (a.slab) {
+        const float2* row = a.slab + q * a.pitch;
+        for (int i = tid; i < a.slabs; i += threads) s = join(s, row[i]);
+    } else {
+        for (int c = tid * 4; c < a.V; c += threads * 4) {
+            v4f x = *reinterpret_cast<const v4f*>(sum_row + c);
+            for (int p = 1; p < a.parts; ++p) x += *reinterpret_cast<const v4f*>(sum_row + p * a.sum_part + c);
+            if (a.parts > 1) *reinterpret_cast<v4f*>(sum_row + c) = x;      // (read again by this thread, and for the label below)
 #pragma unroll
-            for (int u = 0; u < 8; ++u) x[u] = slab[(int64_t)(i + u * kGroups) * pitch + q];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) s = join(s, x[u]);
+            for (int e = 0; e < 4; ++e)
+                if (c + e < a.V) s = join(s, make_float2(x[e], x[e] == x[e] ? 1.f : x[e]));
         }
-        for (; i < n_slabs; i += kGroups) s = join(s, slab[(int64_t)i * pitch + q]);
     }
-    red[threadIdx.x] = s;
+    for (int o = kWave / 2; o > 0; o >>= 1) s = join(s, make_float2(__shfl_xor(s.x, o, kWave), __shfl_xor(s.y, o, kWave)));
+    if (lane == 0) red[wave] = s;
     __syncthreads();
-    for (int o = kGroups / 2; o > 0; o >>= 1) {
-        if (g < o) red[threadIdx.x] = join(red[threadIdx.x], red[threadIdx.x + o * ROWS]);
-        __syncthreads();
+    s = red[0];
+    for (int w = 1; w < threads / kWave; ++w) s = join(s, red[w]);
+    const float picked = a.slab ? a.picked[q] : sum_row[label], inv = 1.f / s.y;
+    if (tid == 0) {
+        const float log_sum = s.x + logf(s.y), x = log_sum - picked;
+        a.stat[q] = make_float2(s.x, inv);
+        a.held_loss[q] = x;
+        const int64_t i = a.r.row[q];
+        if (a.loss) a.loss[i] = x;
+        if (a.lse) a.lse[i] = log_sum;
     }
-    if (g == 0 && q < count) {
-        s = red[lane];
-        const float log_sum = s.x + logf(s.y), x = log_sum - picked[q];
-        stat[q] = make_float2(s.x, 1.f / s.y);
-        held[q] = x;
-        const int64_t i = r.row[q];
-        if (loss) loss[i] = x;
-        if (lse) lse[i] = log_sum;
+    if (!a.grads) return;
+    const float own = (exp_of(picked - s.x) * inv - 1.f) * grad_unit<T>();
+    E* to = static_cast<E*>(a.grads) + q * a.ld;
+    const E* held = static_cast<const E*>(a.held) + q * a.ld;
+    for (int64_t c = (int64_t)tid * n; c < a.ld; c += threads * n) {
+        const int64_t v = a.v0 + c;
+        V x = {};
+        if (v < a.V) {
+            if (T != HSADMM_TYPE_F32 && a.slab) {
+                const float f = exp_of(a.slab[q * a.pitch + v / a.slab_elems].x - s.x) * inv;
+                x = *reinterpret_cast<const V*>(held + c);
+#pragma unroll
+                for (int e = 0; e < n; ++e) x[e] = (E)((float)x[e] * f);
+            } else {
+                const float* from = a.slab ? reinterpret_cast<const float*>(held) : sum_row;
+#pragma unroll
+                for (int e = 0; e < n; ++e) x[e] = (E)(exp_of(from[c + e] - s.x) * inv * grad_unit<T>());
+            }
+#pragma unroll
+            for (int e = 0; e < n; ++e) {
+                if (v + e == label) x[e] = (E)own;
+                if (v + e >= a.V) x[e] = (E)0.f;
+            }
+        }
+        *reinterpret_cast<V*>(to + c) = x;
     }
 }
 
@@ -493,43 +563,26 @@ __global__ __launch_bounds__(kBlock) void loss_total(const LossHead* __restrict_
     }
 }
 
-// The gradients of the logits that are held (the last piece): softmax minus the label's one.  In fp32 they take the logits' place.
-template <int T>
-__global__ __launch_bounds__(kBlock) void loss_softmax(const float* logits, typename ElemOf<T>::type* grads, int64_t ld, int32_t v0, int32_t V,
-                                                       const float2* __restrict__ stat, const int32_t* __restrict__ label,
-                                                       const LossHead* __restrict__ head, int parts)
-{
-    const int64_t q = blockIdx.x / parts;
-    if (q >= head->count) return;
-    const float2 st = stat[q];
-    const int own = label[q] - v0;
-    for (int64_t c = ((int64_t)(blockIdx.x % parts) * kBlock + threadIdx.x) * 4; c < ld; c += (int64_t)parts * kBlock * 4) {
-        v4f x = *reinterpret_cast<const v4f*>(logits + q * ld + c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float y = (exp_of(x[e] - st.x) * st.y - (c + e == own ? 1.f : 0.f)) * grad_unit<T>();
-            x[e] = v0 + c + e < V ? y : 0.f;
-        }
-        *reinterpret_cast<typename ElemOf<T>::vec*>(grads + q * ld + c) = __builtin_convertvector(x, typename ElemOf<T>::vec);
-    }
-}
-
 // The gradients of the inputs: the parts' sums in order, times the factor, to the rows they belong to; zeros where there is no target.
 template <int T>
 __global__ __launch_bounds__(kBlock) void loss_inputs(const float* __restrict__ sums, int splits, int64_t part, int64_t sum_ld, LossRows r,
-                                                      typename ElemOf<T>::type* __restrict__ dX, int64_t ld, int64_t n, int cols, int whole)
+                                                      typename ElemOf<T>::type* __restrict__ dX, int64_t ld, int64_t n, int cols)
 {
+    constexpr int m = Wide<T>::n;
     const int64_t i = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
     if (i >= n) return;
     const int64_t q = r.place[i];
     const float f = r.head->factor * (1.f / grad_unit<T>());
-    for (int c = (threadIdx.x % kWave) * 4; c < cols; c += kWave * 4) {
-        v4f x = {0.f, 0.f, 0.f, 0.f};
-        if (q >= 0) {
-            for (int s = 0; s < splits; ++s) x += *reinterpret_cast<const v4f*>(sums + s * part + q * sum_ld + c);
-            x *= f;
-        }
-        put4<T>(dX + i * ld + c, x, min(4, cols - c), whole != 0, false);
+    for (int c = (threadIdx.x % kWave) * m; c < cols; c += kWave * m) {
+        v4f x[m / 4] = {};
+        if (q >= 0)
+            for (int s = 0; s < splits; ++s)
+#pragma unroll
+                for (int h = 0; h < m / 4; ++h) x[h] += *reinterpret_cast<const v4f*>(sums + s * part + q * sum_ld + c + 4 * h);
+        typename Wide<T>::vec y;
+#pragma unroll
+        for (int e = 0; e < m; ++e) y[e] = (typename ElemOf<T>::type)(x[e / 4][e % 4] * f);
+        store_piece<T>(dX + i * ld + c, y, cols - c);
     }
 }
 

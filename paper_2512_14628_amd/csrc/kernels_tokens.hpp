@@ -8,66 +8,43 @@
 
 namespace {
 
-// A piece of 16 bytes, or (VEC false: rows that are not whole pieces) a single element.
-template <int T, bool VEC> struct Piece {
-    typedef typename ElemOf<T>::type E;
-    static constexpr int n = VEC ? Wide<T>::n : 1;
-    static __device__ __forceinline__ void load(const E* p, float (&x)[n])
-    {
-        if constexpr (VEC) {
-            const typename Wide<T>::vec v = *reinterpret_cast<const typename Wide<T>::vec*>(p);
-#pragma unroll
-            for (int i = 0; i < n; ++i) x[i] = (float)v[i];
-        } else {
-            x[0] = (float)*p;
-        }
-    }
-    static __device__ __forceinline__ void store(E* p, const float (&x)[n])
-    {
-        if constexpr (VEC) {
-            typename Wide<T>::vec v;
-#pragma unroll
-            for (int i = 0; i < n; ++i) v[i] = (E)x[i];
-            *reinterpret_cast<typename Wide<T>::vec*>(p) = v;
-        } else {
-            *p = (E)x[0];
-        }
-    }
-};
-
 // ------------------------------------------------------------------ embedding
 
 // out[i] = scale W[id_i], zeros for an id outside [0, V).  `lanes` threads (a power of two) share a row.
-template <int T, bool VEC>
+template <int T>
 __global__ __launch_bounds__(kBlock) void embedding_rows(const typename ElemOf<T>::type* __restrict__ W, int32_t V, int cols,
                                                          const void* __restrict__ ids, int wide, int64_t n, float scale,
                                                          typename ElemOf<T>::type* __restrict__ out, int64_t ld, int lanes)
 {
-    typedef Piece<T, VEC> P;
+    typedef typename ElemOf<T>::type E;
+    constexpr int m = Wide<T>::n;
     const int64_t i = (int64_t)blockIdx.x * (kBlock / lanes) + threadIdx.x / lanes;
     if (i >= n) return;
     const int64_t id = index_at(ids, wide != 0, i);
     const bool has = id >= 0 && id < V;
-    const typename ElemOf<T>::type* from = W + (has ? id * cols : 0);
-    for (int c = (threadIdx.x & (lanes - 1)) * P::n; c < cols; c += lanes * P::n) {
-        float x[P::n] = {};
+    const E* from = W + (has ? id * cols : 0);
+    for (int c = (threadIdx.x & (lanes - 1)) * m; c < cols; c += lanes * m) {
+        typename Wide<T>::vec x = {};
         if (has) {
-            P::load(from + c, x);
+            x = load_piece<T>(from + c, cols - c);
 #pragma unroll
-            for (int e = 0; e < P::n; ++e) x[e] *= scale;
+            for (int e = 0; e < m; ++e) x[e] = (E)((float)x[e] * scale);
         }
-        P::store(out + i * ld + c, x);
+        store_piece<T>(out + i * ld + c, x, cols - c);
     }
 }
 
 // ------------------------------------------------------------------ tokens in order
 
 // Positions sorted by their token, tokens that are equal in the order of their positions: radix sort from the lowest digit, of up to
-// kDigitBits bits each.  Ids outside [0, V) become V and so come last.  A workgroup takes a tile of kSortTile positions, a wave of it
-// adjacent ones; lanes with equal digits find each other by ballots, so places depend on the ids alone.
+// kDigitBits bits each.  Ids outside [0, V) become V and so come last.  A workgroup takes a tile of positions, a wave of it adjacent
+// ones, kSortAtOnce for each lane at a time (their loads are in flight together: one after the other, 32768 positions took 146 us);
+// lanes with equal digits find each other by ballots, so places depend on the ids alone.
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
-constexpr int kSortTile = 32768;
+constexpr int kSortAtOnce = 8;
+constexpr int kSortMost = 32768;        // positions that one workgroup sorts in one launch; more: tiles of kSortTile
+constexpr int kSortTile = 8192;
 
 struct SortArgs {
     const void* ids;
@@ -76,11 +53,9 @@ struct SortArgs {
     int32_t* key[2];
     int32_t* pos[2];
     uint32_t* counts;           // [digit][tile], several tiles only
-    int tiles;
+    int tile, tiles;
     int bits, passes;
 };
-
-__device__ __forceinline__ int digit_of(int32_t key, int shift, int bits) { return (key >> shift) & ((1 << bits) - 1); }
 
 // The lanes (of those that are active) with this lane's digit.
 __device__ __forceinline__ unsigned long long same_digit(int digit, int bits, bool active)
@@ -105,44 +80,72 @@ struct SortShared {
     uint32_t sums[kScanWaves];
 };
 
+// A wave's part of a tile.
+struct SortPart {
+    int64_t from, to;
+    __device__ __forceinline__ SortPart(const SortArgs& a, int tile)
+    {
+        const int64_t begin = (int64_t)tile * a.tile, end = min((int64_t)a.n, begin + a.tile);
+        const int each = (int)((end - begin + kScanBlock - 1) / kScanBlock) * kWave;
+        from = begin + (int64_t)(threadIdx.x / kWave) * each;
+        to = min(end, from + each);
+    }
+};
+
 // Counts the digits of a tile, wave by wave.
 __device__ void sort_count(const SortArgs& a, int pass, int tile, SortShared& s)
 {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, shift = pass * a.bits;
-    const int64_t from = (int64_t)tile * kSortTile, end = min((int64_t)a.n, from + kSortTile);
-    const int each = (int)((end - from + kScanBlock - 1) / kScanBlock) * kWave;     // of a wave
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, shift = pass * a.bits, mask = (1 << a.bits) - 1;
     for (int d = lane; d < kDigits; d += kWave) s.count[wave][d] = 0;
     __syncthreads();
-    const int64_t w0 = from + (int64_t)wave * each, w1 = min(end, w0 + each);
-    for (int64_t i0 = w0; i0 < w1; i0 += kWave) {
-        const bool active = i0 + lane < w1;
-        const int d = digit_of(active ? sort_key(a, pass, i0 + lane) : 0, shift, a.bits);
-        const unsigned long long same = same_digit(d, a.bits, active);
-        if (active && __ffsll((long long)same) - 1 == lane) atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
+    const SortPart part(a, tile);
+    for (int64_t i0 = part.from + lane; i0 - lane < part.to; i0 += kSortAtOnce * kWave) {
+        int32_t key[kSortAtOnce];
+#pragma unroll
+        for (int u = 0; u < kSortAtOnce; ++u) key[u] = i0 + u * kWave < part.to ? sort_key(a, pass, i0 + u * kWave) : 0;
+#pragma unroll
+        for (int u = 0; u < kSortAtOnce; ++u) {
+            const bool active = i0 + u * kWave < part.to;
+            const int d = (key[u] >> shift) & mask;
+            const unsigned long long same = same_digit(d, a.bits, active);
+            if (active && __ffsll((long long)same) - 1 == lane) atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
+        }
     }
     __syncthreads();
 }
 
-// Moves a tile's positions to their places.  s.count: where each wave's first of a digit goes.
+// Moves a tile's positions to their places.  s.count: where each wave's next of a digit goes.
 __device__ void sort_move(const SortArgs& a, int pass, int tile, SortShared& s)
 {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, shift = pass * a.bits;
-    const int64_t from = (int64_t)tile * kSortTile, end = min((int64_t)a.n, from + kSortTile);
-    const int each = (int)((end - from + kScanBlock - 1) / kScanBlock) * kWave;
-    const int64_t w0 = from + (int64_t)wave * each, w1 = min(end, w0 + each);
-    for (int64_t i0 = w0; i0 < w1; i0 += kWave) {
-        const bool active = i0 + lane < w1;
-        const int32_t key = active ? sort_key(a, pass, i0 + lane) : 0;
-        const int32_t pos = active && pass > 0 ? a.pos[(pass - 1) & 1][i0 + lane] : (int32_t)(i0 + lane);
-        const int d = digit_of(key, shift, a.bits);
-        const unsigned long long same = same_digit(d, a.bits, active);
-        const int first = active ? __ffsll((long long)same) - 1 : lane;
-        uint32_t at = 0;
-        if (active && first == lane) at = atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
-        at = __shfl(at, first, kWave) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
-        if (active) {
-            a.key[pass & 1][at] = key;
-            a.pos[pass & 1][at] = pos;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, shift = pass * a.bits, mask = (1 << a.bits) - 1;
+    const SortPart part(a, tile);
+    for (int64_t i0 = part.from + lane; i0 - lane < part.to; i0 += kSortAtOnce * kWave) {
+        int32_t key[kSortAtOnce], pos[kSortAtOnce];
+        uint32_t at[kSortAtOnce], behind[kSortAtOnce];
+        int first[kSortAtOnce];
+#pragma unroll
+        for (int u = 0; u < kSortAtOnce; ++u) {
+            const int64_t i = i0 + u * kWave;
+            key[u] = i < part.to ? sort_key(a, pass, i) : 0;
+            pos[u] = i < part.to && pass > 0 ? a.pos[(pass - 1) & 1][i] : (int32_t)i;
+        }
+#pragma unroll
+        for (int u = 0; u < kSortAtOnce; ++u) {
+            const bool active = i0 + u * kWave < part.to;
+            const int d = (key[u] >> shift) & mask;
+            const unsigned long long same = same_digit(d, a.bits, active);
+            first[u] = active ? __ffsll((long long)same) - 1 : lane;
+            behind[u] = (uint32_t)__popcll(same & ((1ull << lane) - 1));
+            at[u] = 0;
+            if (active && first[u] == lane) at[u] = atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
+        }
+#pragma unroll
+        for (int u = 0; u < kSortAtOnce; ++u) {
+            const uint32_t to = __shfl(at[u], first[u], kWave) + behind[u];
+            if (i0 + u * kWave < part.to) {
+                a.key[pass & 1][to] = key[u];
+                a.pos[pass & 1][to] = pos[u];
+            }
         }
     }
     __syncthreads();
@@ -266,32 +269,29 @@ __device__ __forceinline__ int lower_bound(const int32_t* __restrict__ key, int 
     return lo;
 }
 
-// x += dY rows of the sorted places [from, to), one piece of columns.
-template <int T, bool VEC>
-__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, int c, float (&x)[Piece<T, VEC>::n])
+// x += dY rows of the sorted places [from, to), a piece of 16 bytes of each at column c.
+template <int T>
+__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, int c, float (&x)[Wide<T>::n])
 {
-    typedef Piece<T, VEC> P;
     const typename ElemOf<T>::type* dY = static_cast<const typename ElemOf<T>::type*>(a.dY);
-    constexpr int kAtOnce = 8;
+    constexpr int kAtOnce = 16;
     for (int i = from; i < to; i += kAtOnce) {
-        float y[kAtOnce][P::n];
+        typename Wide<T>::vec y[kAtOnce];
+        // (places behind the last are read again and not added: the loads stay in flight together)
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) {
-            // (places behind the last are read again and not added: the loads stay in flight together)
-            P::load(dY + (int64_t)a.pos[min(i + u, to - 1)] * a.ld + c, y[u]);
-        }
+        for (int u = 0; u < kAtOnce; ++u) y[u] = load_piece<T>(dY + (int64_t)a.pos[min(i + u, to - 1)] * a.ld + c, a.cols - c);
 #pragma unroll
         for (int u = 0; u < kAtOnce; ++u)
             if (i + u < to)
 #pragma unroll
-                for (int e = 0; e < P::n; ++e) x[e] += y[u][e];
+                for (int e = 0; e < Wide<T>::n; ++e) x[e] += (float)y[u][e];
     }
 }
 
-template <int T, bool VEC>
+template <int T>
 __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
 {
-    typedef Piece<T, VEC> P;
+    constexpr int m = Wide<T>::n;
     __shared__ int bound[4];
     const int64_t b = blockIdx.x;
     const int from = (int)(b * a.part), to = (int)min((int64_t)a.n, (b + 1) * a.part);
@@ -304,25 +304,28 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
     for (int which = 0; which < 2; ++which) {
         if (!(which ? last : first)) continue;
         const int f = which ? bound[2] : from, t = which ? to : min(to, bound[1]);
-        for (int c = threadIdx.x * P::n; c < a.cols; c += kBlock * P::n) {
-            float x[P::n] = {};
-            add_rows<T, VEC>(a, f, t, c, x);
+        for (int c = threadIdx.x * m; c < a.cols; c += kBlock * m) {
+            float x[m] = {};
+            add_rows<T>(a, f, t, c, x);
             float* to_sums = a.sums + (2 * b + which) * a.pitch + c;
 #pragma unroll
-            for (int e = 0; e < P::n; ++e) to_sums[e] = x[e];
+            for (int e = 0; e < m; e += 4) *reinterpret_cast<v4f*>(to_sums + e) = v4f{x[e], x[e + 1], x[e + 2], x[e + 3]};
         }
     }
 }
 
 // The rows of dW: a workgroup takes `rows` of them, a wave one after the other; runs of `run` adjacent rows, the runs of a workgroup
-// as far apart as the grid is wide, as the frequent tokens often are the first ones.
+// as far apart as the grid is wide, as the frequent tokens often are the first ones.  A wave has kAcross pieces of 16 bytes a lane of
+// one or a few tokens' rows in flight at once.
 constexpr int kGradRows = 64;           // at most
+constexpr int kAcross = 4;
 
-template <int T, bool VEC>
+template <int T>
 __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
 {
-    typedef Piece<T, VEC> P;
     typedef typename ElemOf<T>::type E;
+    typedef typename Wide<T>::vec V;
+    constexpr int m = Wide<T>::n;
     __shared__ int bound[kGradRows][2];
     const auto row_of = [&](int i) { return ((int64_t)(i / a.run) * gridDim.x + blockIdx.x) * a.run + i % a.run; };
     if (threadIdx.x < 2 * a.rows) {
@@ -331,34 +334,72 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
     }
     __syncthreads();
     const int lane = threadIdx.x & (kWave - 1);
+    const E* dY = static_cast<const E*>(a.dY);
     for (int i = threadIdx.x / kWave; i < a.rows; i += kWaves) {
         const int64_t v = row_of(i);
         if (v >= a.V) continue;
-        const int from = bound[i][0], to = bound[i][1];
+        const int from = __builtin_amdgcn_readfirstlane(bound[i][0]), to = __builtin_amdgcn_readfirstlane(bound[i][1]);
         if (from == to && a.add) continue;
         E* row = static_cast<E*>(a.G) + v * a.cols;
-        for (int c = lane * P::n; c < a.cols; c += kWave * P::n) {
-            float x[P::n] = {};
+        for (int c0 = lane * m; c0 - lane * m < a.cols; c0 += kAcross * kWave * m) {
+            float x[kAcross][m] = {};
+            // `count` tokens' rows, all their pieces at once
+            const auto add = [&](auto count, int at, int32_t pos) {
+                constexpr int kCount = decltype(count)::value;
+                V y[kCount][kAcross];
+#pragma unroll
+                for (int u = 0; u < kCount; ++u) {
+                    const E* from_row = dY + (int64_t)__builtin_amdgcn_readlane(pos, at + u) * a.ld;
+#pragma unroll
+                    for (int k = 0; k < kAcross; ++k) {
+                        const int c = c0 + k * kWave * m;
+                        if (c < a.cols) y[u][k] = load_piece<T>(from_row + c, a.cols - c);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < kCount; ++u)
+#pragma unroll
+                    for (int k = 0; k < kAcross; ++k)
+                        if (c0 + k * kWave * m < a.cols)
+#pragma unroll
+                            for (int e = 0; e < m; ++e) x[k][e] += (float)y[u][k][e];
+            };
             if (to - from <= a.part) {
-                add_rows<T, VEC>(a, from, to, c, x);
+                for (int t = from; t < to; t += kWave) {
+                    const int n = min(kWave, to - t);
+                    const int32_t pos = a.pos[t + min(lane, n - 1)];
+                    int u = 0;
+                    for (; u + 4 <= n; u += 4) add(std::integral_constant<int, 4>{}, u, pos);
+                    if (u + 2 <= n) { add(std::integral_constant<int, 2>{}, u, pos); u += 2; }
+                    if (u < n) add(std::integral_constant<int, 1>{}, u, pos);
+                }
             } else {
                 const int64_t b0 = from / a.part, b1 = (to - 1) / a.part;
                 for (int64_t b = b0; b <= b1; ++b) {
                     // (the token's first stretch holds it as the second one if it begins inside)
-                    const float* sums = a.sums + (2 * b + (b == b0 && b0 * a.part != from ? 1 : 0)) * a.pitch + c;
+                    const float* sums = a.sums + (2 * b + (b == b0 && b0 * a.part != from ? 1 : 0)) * a.pitch;
 #pragma unroll
-                    for (int e = 0; e < P::n; ++e) x[e] += sums[e];
+                    for (int k = 0; k < kAcross; ++k) {
+                        const int c = c0 + k * kWave * m;
+                        if (c < a.cols)
+#pragma unroll
+                            for (int e = 0; e < m; e += 4) {
+                                const v4f y = *reinterpret_cast<const v4f*>(sums + c + e);
+                                x[k][e] += y.x; x[k][e + 1] += y.y; x[k][e + 2] += y.z; x[k][e + 3] += y.w;
+                            }
+                    }
                 }
             }
 #pragma unroll
-            for (int e = 0; e < P::n; ++e) x[e] *= a.scale;
-            if (a.add) {
-                float g[P::n];
-                P::load(row + c, g);
+            for (int k = 0; k < kAcross; ++k) {
+                const int c = c0 + k * kWave * m;
+                if (c >= a.cols) break;
+                V g = {};
+                if (a.add) g = load_piece<T>(row + c, a.cols - c);
 #pragma unroll
-                for (int e = 0; e < P::n; ++e) x[e] += g[e];
+                for (int e = 0; e < m; ++e) g[e] = (E)(a.add ? x[k][e] * a.scale + (float)g[e] : x[k][e] * a.scale);
+                store_piece<T>(row + c, g, a.cols - c);
             }
-            P::store(row + c, x);
         }
     }
 }
@@ -398,8 +439,7 @@ struct DropoutArgs {
 
 constexpr int kDropout = 8;     // elements that share a counter
 
-// VEC: rows are whole groups of 16-byte aligned elements; else, and for the last elements, one by one.
-template <int T, bool VEC, bool RES>
+template <int T, bool RES>
 __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a)
 {
     typedef typename ElemOf<T>::type E;
@@ -410,7 +450,7 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a)
         philox((uint64_t)g, call, a.seed, w);
         const int64_t i = g * kDropout;
         int64_t row, col;
-        if (a.cols >= a.n) { row = 0; col = i; }
+        if (a.cols == a.n) { row = 0; col = i; }
         else if (a.n <= 0xffffffffll) { row = (uint32_t)i / (uint32_t)a.cols; col = i - row * a.cols; }
         else { row = i / a.cols; col = i - row * a.cols; }
         const E* x = static_cast<const E*>(a.X) + row * a.ldx + col;
@@ -421,21 +461,23 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a)
             const float kept = ((w[j >> 1] >> (16 * (j & 1))) & 0xffffu) >= a.least ? v * a.scale : 0.f;
             return RES ? kept + res : kept;
         };
-        if (VEC && i + kDropout <= a.n) {
+        if (col + kDropout <= a.cols) {
+            // (the group lies in one row, at any element's address)
             constexpr int kPieces = kDropout / Wide<T>::n;
             typedef typename Wide<T>::vec V;
+            typedef typename Wide<T>::any A;
             V vx[kPieces], vr[kPieces];
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
-                vx[p] = __builtin_nontemporal_load(reinterpret_cast<const V*>(x) + p);
-                if (RES) vr[p] = __builtin_nontemporal_load(reinterpret_cast<const V*>(r) + p);
+                vx[p] = __builtin_nontemporal_load(reinterpret_cast<const A*>(x) + p);
+                if (RES) vr[p] = __builtin_nontemporal_load(reinterpret_cast<const A*>(r) + p);
             }
 #pragma unroll
             for (int p = 0; p < kPieces; ++p) {
                 V out;
 #pragma unroll
                 for (int e = 0; e < Wide<T>::n; ++e) out[e] = (E)one(p * Wide<T>::n + e, (float)vx[p][e], RES ? (float)vr[p][e] : 0.f);
-                __builtin_nontemporal_store(out, reinterpret_cast<V*>(y) + p);
+                __builtin_nontemporal_store(out, reinterpret_cast<A*>(y) + p);
             }
         } else {
 #pragma unroll

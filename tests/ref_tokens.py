@@ -68,8 +68,9 @@ def loss_reference(kind, X, W, labels, mean, scale):
     dp = p * (dl + worst[:, None] + ds + 4 * U * (1 + span) + 4 * U)
     P = p.clone()
     P[rows, y] -= 1
+    # (in 16 bits up to two roundings: of the exponential that is held, then of the gradient made of it)
     unit = 2.0 ** -15 if kind == pkg.TYPE_F16 else 1.0
-    dP = dp + (P.abs() + dp) * (half_step(kind) + 2 * U) + unit * least(kind) + (2.0 ** -126 if kind != pkg.TYPE_F32 else 0)
+    dP = dp + SAFE * (P.abs() + dp) * (2 * half_step(kind) + 4 * U) + 2 * unit * least(kind) + (2.0 ** -125 if kind != pkg.TYPE_F32 else 0)
     dx = (P @ w) * g
     ddx = abs(g) * (dP @ w.abs() + 2 * (V + 64) * U * ((P.abs() + dP) @ w.abs())) + 4 * U * dx.abs()
     a, b = X.new_zeros((n, D), dtype=f64), X.new_zeros((n, D), dtype=f64)
