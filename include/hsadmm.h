@@ -980,7 +980,7 @@ int hsadmm_dropout(const hsadmm_plan_t* plan, const void* X, int64_t x_stride, c
  *     dX = f P W;   the layer's rows of G = f P^T X (with `accumulate` added to what G holds)
  * `scale` multiplies the gradients alone (a loss scale of fp16 training).  Rows without a target cost nothing, and what X holds there
  * is not looked at.  Logits are formed in fp32; P is rounded to `type` (half precision: 2^15 P) for the products that follow, some of it
- * from exponentials that were rounded to `type` before.  At most 2^30 bytes of either are held, a piece of the vocabulary: where it
+ * from exponentials that were rounded to `type` before.  At most 2^31 bytes of either are held, a piece of the vocabulary: where it
  * takes several, the logits of all but the last are formed twice.
  * Fill a zeroed hsadmm_softmax_loss_args_t; a NULL field means "not wanted"; at least one output is.
  *   struct_bytes  sizeof(hsadmm_softmax_loss_args_t) as the caller was compiled (INVALID_ARGUMENT if it differs)
@@ -1088,7 +1088,7 @@ int hsadmm_kernel_grid(const hsadmm_plan_t* plan, int kernel_id);
  * selection in the one launch, in ticks of 10 ns (30000 without it; for tests); rows that have waited so long are written in
  * a form that is finished once the selection is there, within the same launch.  HSADMM_GRID_MOST: workgroups that one launch of
  * hsadmm_adamw or hsadmm_expand_mx takes (16777215 without it, what a grid holds; for tests); more work takes several launches.
- * HSADMM_LOSS_HELD: bytes of logits that hsadmm_softmax_loss holds at once (2^30 without it; for tests: small vocabularies then take
+ * HSADMM_LOSS_HELD: bytes of logits that hsadmm_softmax_loss holds at once (2^31 without it; for tests: small vocabularies then take
  * several pieces).
  */
 int hsadmm_plan_estimates(const hsadmm_plan_t* plan);

@@ -122,7 +122,7 @@ constexpr size_t kTimingPairs = 8192;
 // Workgroups of one launch: a grid has fewer than 2^32 threads.  The update and the expansion of quantised buffers take several launches for
 // arenas of more than 17 G elements (or fewer, of several replicas).
 constexpr int64_t kGridMost = (1ll << 32) / kBlock - 1;
-constexpr int64_t kLossHeld = 1ll << 30;   // bytes of logits, and then their gradients, that hsadmm_softmax_loss holds at once
+constexpr int64_t kLossHeld = 1ll << 31;   // bytes of logits, and then their gradients, that hsadmm_softmax_loss holds at once
 constexpr size_t kRepairGrid = 2048;       // workgroups of the repair pass under a prediction: 8 per compute unit
 
 // Scratch of the entry point that takes no workspace argument (hsadmm_project_compact_static): one array per
@@ -2468,6 +2468,7 @@ static EmbedScratch embed_scratch(int32_t V, int32_t D, int64_t n)
     s.passes = (width + kDigitBits - 1) / kDigitBits;
     s.bits = (width + s.passes - 1) / s.passes;
     s.tile = n <= kSortMost ? kSortMost : kSortTile;
+    while ((n + s.tile - 1) / s.tile > kSortTiles) s.tile *= 2;
     s.tiles = (int)((n + s.tile - 1) / s.tile);
     // Stretches about as long as there are stretches, so that no row is a chain of more than some of either.
     s.part = 64;
@@ -2535,7 +2536,7 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     } else {
         for (int pass = 0; pass < a.passes && ws.tiles > 1 && e == hipSuccess; ++pass) {
             e = launch(p, kTokenCount, token_count, (unsigned)ws.tiles, kScanBlock, s, a, pass);
-            if (e == hipSuccess) e = launch(p, kTokenScan, token_scan, 1u, kScanBlock, s, a.counts, ((int64_t)1 << a.bits) * ws.tiles);
+            if (e == hipSuccess) e = launch(p, kTokenScan, token_scan, 1u, kScanBlock, s, a.counts, (1 << a.bits) * ws.tiles);
             if (e == hipSuccess) e = launch(p, kTokenMove, token_move, (unsigned)ws.tiles, kScanBlock, s, a, pass);
         }
     }

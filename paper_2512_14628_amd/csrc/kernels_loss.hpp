@@ -467,6 +467,23 @@ struct SoftmaxArgs {
     int32_t v0, V;
 };
 
+// Four adjacent sums, over their parts in order, eight parts in flight.
+__device__ __forceinline__ v4f add_parts(const float* p, int parts, int64_t part)
+{
+    v4f x = {0.f, 0.f, 0.f, 0.f};
+    constexpr int kAtOnce = 8;
+    int i = 0;
+    for (; i + kAtOnce <= parts; i += kAtOnce) {
+        v4f y[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) y[u] = *reinterpret_cast<const v4f*>(p + (i + u) * part);
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) x += y[u];
+    }
+    for (; i < parts; ++i) x += *reinterpret_cast<const v4f*>(p + i * part);
+    return x;
+}
+
 __device__ __forceinline__ float2 join(float2 a, float2 b)
 {
     // (a side without any value has the sum 0 and the largest value -inf; NaN in a sum stays)
@@ -495,8 +512,7 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
         for (int i = tid; i < a.slabs; i += threads) s = join(s, row[i]);
     } else {
         for (int c = tid * 4; c < a.V; c += threads * 4) {
-            v4f x = *reinterpret_cast<const v4f*>(sum_row + c);
-            for (int p = 1; p < a.parts; ++p) x += *reinterpret_cast<const v4f*>(sum_row + p * a.sum_part + c);
+            const v4f x = add_parts(sum_row + c, a.parts, a.sum_part);
             if (a.parts > 1) *reinterpret_cast<v4f*>(sum_row + c) = x;      // (read again by this thread, and for the label below)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
@@ -576,9 +592,8 @@ __global__ __launch_bounds__(kBlock) void loss_inputs(const float* __restrict__ 
     for (int c = (threadIdx.x % kWave) * m; c < cols; c += kWave * m) {
         v4f x[m / 4] = {};
         if (q >= 0)
-            for (int s = 0; s < splits; ++s)
 #pragma unroll
-                for (int h = 0; h < m / 4; ++h) x[h] += *reinterpret_cast<const v4f*>(sums + s * part + q * sum_ld + c + 4 * h);
+            for (int h = 0; h < m / 4; ++h) x[h] = add_parts(sums + q * sum_ld + c + 4 * h, splits, part);
         typename Wide<T>::vec y;
 #pragma unroll
         for (int e = 0; e < m; ++e) y[e] = (typename ElemOf<T>::type)(x[e / 4][e % 4] * f);

@@ -43,8 +43,9 @@ __global__ __launch_bounds__(kBlock) void embedding_rows(const typename ElemOf<T
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortAtOnce = 8;
-constexpr int kSortMost = 32768;        // positions that one workgroup sorts in one launch; more: tiles of kSortTile
-constexpr int kSortTile = 8192;
+constexpr int kSortMost = 4096;         // positions that one workgroup sorts in one launch; more: tiles of kSortTile or, of more
+constexpr int kSortTile = 2048;         // than kSortTiles of them, of as many powers of two as make that many
+constexpr int kSortTiles = 64;
 
 struct SortArgs {
     const void* ids;
@@ -57,15 +58,18 @@ struct SortArgs {
     int bits, passes;
 };
 
-// The lanes (of those that are active) with this lane's digit.
+// The lanes (of those that are active) with this lane's digit: for each bit those that agree in it.
 __device__ __forceinline__ unsigned long long same_digit(int digit, int bits, bool active)
 {
-    unsigned long long same = __ballot(active);
+    const unsigned long long all = __ballot(active);
+    uint32_t lo = (uint32_t)all, hi = (uint32_t)(all >> 32);
     for (int b = 0; b < bits; ++b) {
         const unsigned long long set = __ballot((digit >> b) & 1);
-        same &= (digit >> b) & 1 ? set : ~set;
+        const uint32_t own = (uint32_t)-((digit >> b) & 1);
+        lo &= ~((uint32_t)set ^ own);
+        hi &= ~((uint32_t)(set >> 32) ^ own);
     }
-    return same;
+    return (unsigned long long)hi << 32 | lo;
 }
 
 __device__ __forceinline__ int32_t sort_key(const SortArgs& a, int pass, int64_t i)
@@ -105,10 +109,7 @@ __device__ void sort_count(const SortArgs& a, int pass, int tile, SortShared& s)
         for (int u = 0; u < kSortAtOnce; ++u) key[u] = i0 + u * kWave < part.to ? sort_key(a, pass, i0 + u * kWave) : 0;
 #pragma unroll
         for (int u = 0; u < kSortAtOnce; ++u) {
-            const bool active = i0 + u * kWave < part.to;
-            const int d = (key[u] >> shift) & mask;
-            const unsigned long long same = same_digit(d, a.bits, active);
-            if (active && __ffsll((long long)same) - 1 == lane) atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
+            if (i0 + u * kWave < part.to) atomicAdd(&s.count[wave][(key[u] >> shift) & mask], 1u);
         }
     }
     __syncthreads();
@@ -202,28 +203,32 @@ __global__ __launch_bounds__(kScanBlock) void token_count(SortArgs a, int pass)
     }
 }
 
-__global__ __launch_bounds__(kScanBlock) void token_scan(uint32_t* __restrict__ counts, int64_t n)
+// (a thread takes adjacent counts, all of them at once)
+__global__ __launch_bounds__(kScanBlock) void token_scan(uint32_t* __restrict__ counts, int n)
 {
-    __shared__ uint32_t sums[2][kScanWaves];
+    constexpr int kMost = kDigits * kSortTiles / kScanBlock;
+    __shared__ uint32_t sums[kScanWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    uint32_t before = 0;
-    int turn = 0;
-    for (int64_t i0 = 0; i0 < n; i0 += kScanBlock, turn ^= 1) {
-        const int64_t i = i0 + threadIdx.x;
-        const uint32_t own = i < n ? counts[i] : 0;
-        uint32_t upto = own;
-        for (int o = 1; o < kWave; o <<= 1) {
-            const uint32_t x = __shfl_up(upto, o, kWave);
-            if (lane >= o) upto += x;
-        }
-        if (lane == kWave - 1) sums[turn][wave] = upto;
-        __syncthreads();
-        uint32_t at = before + upto - own;
-        for (int w = 0; w < kScanWaves; ++w) {
-            before += sums[turn][w];
-            if (w < wave) at += sums[turn][w];
-        }
-        if (i < n) counts[i] = at;
+    const int each = (n + kScanBlock - 1) / kScanBlock, first = threadIdx.x * each;
+    uint32_t own[kMost], all = 0;
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        own[i] = i < each && first + i < n ? counts[first + i] : 0;
+        all += own[i];
+    }
+    uint32_t upto = all;
+    for (int o = 1; o < kWave; o <<= 1) {
+        const uint32_t x = __shfl_up(upto, o, kWave);
+        if (lane >= o) upto += x;
+    }
+    if (lane == kWave - 1) sums[wave] = upto;
+    __syncthreads();
+    uint32_t at = upto - all;
+    for (int w = 0; w < wave; ++w) at += sums[w];
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+        if (i < each && first + i < n) counts[first + i] = at;
+        at += own[i];
     }
 }
 
@@ -269,25 +274,57 @@ __device__ __forceinline__ int lower_bound(const int32_t* __restrict__ key, int 
     return lo;
 }
 
-// x += dY rows of the sorted places [from, to), a piece of 16 bytes of each at column c.
-template <int T>
-__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, int c, float (&x)[Wide<T>::n])
+// x += dY rows of the sorted places [from, to), K pieces of 16 bytes at the columns c[0 .. K) of which `on` says which are wanted;
+// AT_ONCE rows in flight.  (The pieces are whole: a branch for the end of a row would have every load waited for where it stands.)
+template <int T, int K, int AT_ONCE>
+__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, const int (&c)[K], const bool (&on)[K],
+                                         float (&x)[K][Wide<T>::n])
 {
-    const typename ElemOf<T>::type* dY = static_cast<const typename ElemOf<T>::type*>(a.dY);
-    constexpr int kAtOnce = 16;
-    for (int i = from; i < to; i += kAtOnce) {
-        typename Wide<T>::vec y[kAtOnce];
-        // (places behind the last are read again and not added: the loads stay in flight together)
+    typedef typename ElemOf<T>::type E;
+    typedef typename Wide<T>::vec V;
+    const E* dY = static_cast<const E*>(a.dY);
+    const int lane = threadIdx.x & (kWave - 1);
+    const auto add = [&](auto count, int at, int32_t pos) {
+        constexpr int kCount = decltype(count)::value;
+        V y[kCount][K];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) y[u] = load_piece<T>(dY + (int64_t)a.pos[min(i + u, to - 1)] * a.ld + c, a.cols - c);
+        for (int u = 0; u < kCount; ++u) {
+            const E* row = dY + (int64_t)__builtin_amdgcn_readlane(pos, at + u) * a.ld;
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u)
-            if (i + u < to)
+            for (int k = 0; k < K; ++k)
+                if (on[k]) y[u][k] = *reinterpret_cast<const typename Wide<T>::any*>(row + c[k]);
+        }
 #pragma unroll
-                for (int e = 0; e < Wide<T>::n; ++e) x[e] += (float)y[u][e];
+        for (int u = 0; u < kCount; ++u)
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (on[k])
+#pragma unroll
+                    for (int e = 0; e < Wide<T>::n; ++e) x[k][e] += (float)y[u][k][e];
+    };
+    for (int t = from; t < to; t += kWave) {
+        const int n = min(kWave, to - t);
+        const int32_t pos = a.pos[t + min(lane, n - 1)];
+        int u = 0;
+        for (; u + AT_ONCE <= n; u += AT_ONCE) add(std::integral_constant<int, AT_ONCE>{}, u, pos);
+        if constexpr (AT_ONCE > 4)
+            for (; u + 4 <= n; u += 4) add(std::integral_constant<int, 4>{}, u, pos);
+        if (u + 2 <= n) { add(std::integral_constant<int, 2>{}, u, pos); u += 2; }
+        if (u < n) add(std::integral_constant<int, 1>{}, u, pos);
     }
 }
 
+// Sums over rows that are shorter than a piece: one column of the places [from, to).
+template <int T>
+__device__ __forceinline__ float add_column(const EmbedGradArgs& a, int from, int to, int c)
+{
+    float x = 0.f;
+    for (int t = from; t < to; ++t) x += (float)static_cast<const typename ElemOf<T>::type*>(a.dY)[(int64_t)a.pos[t] * a.ld + c];
+    return x;
+}
+
+// The stretches' sums.  Rows of at least a piece: a lane whose piece would pass the end of the row takes the row's last one instead
+// and forms some columns a second time, from the same terms in the same order.
 template <int T>
 __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
 {
@@ -304,12 +341,20 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
     for (int which = 0; which < 2; ++which) {
         if (!(which ? last : first)) continue;
         const int f = which ? bound[2] : from, t = which ? to : min(to, bound[1]);
-        for (int c = threadIdx.x * m; c < a.cols; c += kBlock * m) {
-            float x[m] = {};
-            add_rows<T>(a, f, t, c, x);
-            float* to_sums = a.sums + (2 * b + which) * a.pitch + c;
+        float* sums = a.sums + (2 * b + which) * a.pitch;
+        if (a.cols < m) {
+            if ((int)threadIdx.x < a.cols) sums[threadIdx.x] = add_column<T>(a, f, t, threadIdx.x);
+            continue;
+        }
+        for (int c0 = threadIdx.x / kWave * kWave * m; c0 < a.cols; c0 += kBlock * m) {
+            const int at = c0 + (threadIdx.x & (kWave - 1)) * m;
+            const int c[1] = {min(at, a.cols - m)};
+            const bool on[1] = {at < a.cols};
+            float x[1][m] = {};
+            add_rows<T, 1, 16>(a, f, t, c, on, x);
+            if (on[0])
 #pragma unroll
-            for (int e = 0; e < m; e += 4) *reinterpret_cast<v4f*>(to_sums + e) = v4f{x[e], x[e + 1], x[e + 2], x[e + 3]};
+                for (int e = 0; e < m; ++e) sums[c[0] + e] = x[0][e];
         }
     }
 }
@@ -325,6 +370,7 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
 {
     typedef typename ElemOf<T>::type E;
     typedef typename Wide<T>::vec V;
+    typedef typename Wide<T>::any A;
     constexpr int m = Wide<T>::n;
     __shared__ int bound[kGradRows][2];
     const auto row_of = [&](int i) { return ((int64_t)(i / a.run) * gridDim.x + blockIdx.x) * a.run + i % a.run; };
@@ -334,72 +380,72 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
     }
     __syncthreads();
     const int lane = threadIdx.x & (kWave - 1);
-    const E* dY = static_cast<const E*>(a.dY);
     for (int i = threadIdx.x / kWave; i < a.rows; i += kWaves) {
         const int64_t v = row_of(i);
         if (v >= a.V) continue;
         const int from = __builtin_amdgcn_readfirstlane(bound[i][0]), to = __builtin_amdgcn_readfirstlane(bound[i][1]);
         if (from == to && a.add) continue;
         E* row = static_cast<E*>(a.G) + v * a.cols;
-        for (int c0 = lane * m; c0 - lane * m < a.cols; c0 += kAcross * kWave * m) {
-            float x[kAcross][m] = {};
-            // `count` tokens' rows, all their pieces at once
-            const auto add = [&](auto count, int at, int32_t pos) {
-                constexpr int kCount = decltype(count)::value;
-                V y[kCount][kAcross];
-#pragma unroll
-                for (int u = 0; u < kCount; ++u) {
-                    const E* from_row = dY + (int64_t)__builtin_amdgcn_readlane(pos, at + u) * a.ld;
-#pragma unroll
-                    for (int k = 0; k < kAcross; ++k) {
-                        const int c = c0 + k * kWave * m;
-                        if (c < a.cols) y[u][k] = load_piece<T>(from_row + c, a.cols - c);
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < kCount; ++u)
-#pragma unroll
-                    for (int k = 0; k < kAcross; ++k)
-                        if (c0 + k * kWave * m < a.cols)
-#pragma unroll
-                            for (int e = 0; e < m; ++e) x[k][e] += (float)y[u][k][e];
-            };
-            if (to - from <= a.part) {
-                for (int t = from; t < to; t += kWave) {
-                    const int n = min(kWave, to - t);
-                    const int32_t pos = a.pos[t + min(lane, n - 1)];
-                    int u = 0;
-                    for (; u + 4 <= n; u += 4) add(std::integral_constant<int, 4>{}, u, pos);
-                    if (u + 2 <= n) { add(std::integral_constant<int, 2>{}, u, pos); u += 2; }
-                    if (u < n) add(std::integral_constant<int, 1>{}, u, pos);
-                }
-            } else {
-                const int64_t b0 = from / a.part, b1 = (to - 1) / a.part;
-                for (int64_t b = b0; b <= b1; ++b) {
-                    // (the token's first stretch holds it as the second one if it begins inside)
-                    const float* sums = a.sums + (2 * b + (b == b0 && b0 * a.part != from ? 1 : 0)) * a.pitch;
-#pragma unroll
-                    for (int k = 0; k < kAcross; ++k) {
-                        const int c = c0 + k * kWave * m;
-                        if (c < a.cols)
-#pragma unroll
-                            for (int e = 0; e < m; e += 4) {
-                                const v4f y = *reinterpret_cast<const v4f*>(sums + c + e);
-                                x[k][e] += y.x; x[k][e + 1] += y.y; x[k][e + 2] += y.z; x[k][e + 3] += y.w;
-                            }
-                    }
-                }
+        // a token with many positions: its stretches, of which the first holds it as the second one if it begins inside
+        const bool many = to - from > a.part;
+        const int64_t b0 = from / a.part, b1 = (to - 1) / a.part;
+        const int64_t begins = b0 * a.part != from ? 1 : 0;
+        if (a.cols < m) {
+            if (lane < a.cols) {
+                float x = 0.f;
+                if (!many) x = add_column<T>(a, from, to, lane);
+                else
+                    for (int64_t b = b0; b <= b1; ++b) x += a.sums[(2 * b + (b == b0 ? begins : 0)) * a.pitch + lane];
+                row[lane] = (E)(a.add ? x * a.scale + (float)row[lane] : x * a.scale);
             }
+            continue;
+        }
+        for (int c0 = 0; c0 < a.cols; c0 += kAcross * kWave * m) {
+            float x[kAcross][m] = {};
+            int c[kAcross];
+            bool on[kAcross];
+            V g[kAcross];
 #pragma unroll
             for (int k = 0; k < kAcross; ++k) {
-                const int c = c0 + k * kWave * m;
-                if (c >= a.cols) break;
-                V g = {};
-                if (a.add) g = load_piece<T>(row + c, a.cols - c);
-#pragma unroll
-                for (int e = 0; e < m; ++e) g[e] = (E)(a.add ? x[k][e] * a.scale + (float)g[e] : x[k][e] * a.scale);
-                store_piece<T>(row + c, g, a.cols - c);
+                const int at = c0 + (k * kWave + lane) * m;
+                on[k] = at < a.cols;
+                c[k] = min(at, a.cols - m);
             }
+            if (a.add)
+#pragma unroll
+                for (int k = 0; k < kAcross; ++k)
+                    if (on[k]) g[k] = *reinterpret_cast<const A*>(row + c[k]);
+            if (!many) {
+                add_rows<T, kAcross, 4>(a, from, to, c, on, x);
+            } else {
+                for (int64_t b = b0; b <= b1; ++b) {
+                    const float* sums = a.sums + (2 * b + (b == b0 ? begins : 0)) * a.pitch;
+#pragma unroll
+                    for (int k = 0; k < kAcross; ++k)
+                        if (on[k])
+#pragma unroll
+                            for (int e = 0; e < m; e += 4) {
+                                const v4f y = ld4u(sums + c[k] + e);
+                                x[k][e] += y.x; x[k][e + 1] += y.y; x[k][e + 2] += y.z; x[k][e + 3] += y.w;
+                            }
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kAcross; ++k)
+                if (on[k]) {
+                    V y;
+#pragma unroll
+                    for (int e = 0; e < m; ++e) y[e] = (E)(a.add ? x[k][e] * a.scale + (float)g[k][e] : x[k][e] * a.scale);
+                    const int skip = c0 + (k * kWave + lane) * m - c[k];
+                    if (!a.add || skip == 0) {
+                        *reinterpret_cast<A*>(row + c[k]) = y;
+                    } else {
+                        // (columns that another piece adds to as well: their sums may have been written already when g was read)
+#pragma unroll
+                        for (int e = 1; e < m; ++e)
+                            if (e >= skip) row[c[k] + e] = y[e];
+                    }
+                }
         }
     }
 }

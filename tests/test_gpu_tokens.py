@@ -134,6 +134,14 @@ def test_tokens_of_all_frequencies(spread, n):
     check_gradient(F32, n, 12, 777, spread)
 
 
+@pytest.mark.parametrize("kind,D", [(F32, 1023), (F32, 1025), (F32, 1027), (F32, 2049), (BF16, 2047), (BF16, 2049), (F16, 2055), (BF16, 4099), (F32, 259),
+                                    (BF16, 515), (F16, 7), (F16, 9)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_rows_that_end_inside_a_piece(kind, D, accumulate):
+    """Ends next to a wave's pieces: the last piece is moved back and shares columns with the one before it."""
+    check_gradient(kind, 500, D, 30, "common", accumulate=accumulate)
+
+
 @pytest.mark.parametrize("V", [1, 2, 511, 512, 513, 262143, 262144])
 def test_vocabularies_around_whole_digits(V):
     check_gradient(BF16, 3000, 8, V, "spread")
