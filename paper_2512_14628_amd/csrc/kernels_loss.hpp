@@ -196,25 +196,54 @@ template <int T, int B, bool KMAJOR> struct TilePart {
     }
 };
 
-template <int T, int B, bool KMAJOR, int THREADS>
-__device__ __forceinline__ void load_tile(const Operand& o, int64_t mn0, int64_t k0, const unsigned char* zeros, char* lds)
+// 16 bytes from each lane's address to LDS, the wave's pieces one behind the other from `to` on.  Written out, since the compiler has
+// every transposing read of LDS wait for all loads to LDS that it knows of, also those to places that are not read: whoever uses
+// this waits by itself (tile_barrier), and once more before the workgroup ends.
+__device__ __forceinline__ void load_to_lds(const void* from, const char* to)
 {
+    const uint32_t at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "m0");
+}
+
+// Where a lane's pieces of an operand's tiles come from.  Rows (or pieces) behind the operand's last one are read from a valid place
+// instead: whatever they hold goes to outputs that nobody stores.  What lies behind the end of k comes from the page of zeros.
+template <int T, int B, bool KMAJOR, int THREADS>
+struct TileSource {
     typedef TilePart<T, B, KMAJOR> L;
-    typedef typename L::E E;
-    constexpr int kLoads = L::kPieces / THREADS;
-    static_assert(L::kPieces % THREADS == 0, "whole loads");
-    const int tid = threadIdx.x;
+    static constexpr int kLoads = L::kPieces / THREADS;
+    static_assert(L::kPieces % THREADS == 0 && (THREADS / L::kRow) % 16 == 0 || KMAJOR, "whole loads; every load of a lane the same piece of its row");
+    const char* from[kLoads];
+    int64_t step;               // bytes from a tile to the next one
+    int k;                      // of the lane's first element, in the tile
+    __device__ __forceinline__ TileSource(const Operand& o, int64_t mn0, int64_t k0)
+    {
+        constexpr int size = sizeof(typename L::E);
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-        const int slot = i * THREADS + tid;
-        const int row = slot / L::kRow, piece = (slot % L::kRow) ^ L::turn(row);
-        const int64_t mn = KMAJOR ? mn0 + piece * L::kPiece : mn0 + row;
-        const int64_t k = KMAJOR ? k0 + row : k0 + piece * L::kPiece;
-        const void* from = zeros;
-        if (mn < o.mn && k < o.k) from = static_cast<const E*>(o.at) + (KMAJOR ? k * o.ld + mn : mn * o.ld + k);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                         (__attribute__((address_space(3))) void*)(lds + (i * THREADS + (tid & ~(kWave - 1))) * 16), 16, 0, 0);
+        for (int i = 0; i < kLoads; ++i) {
+            const int slot = i * THREADS + threadIdx.x;
+            const int row = slot / L::kRow, piece = (slot % L::kRow) ^ L::turn(row);
+            const int64_t mn = KMAJOR ? mn0 + piece * L::kPiece : min(mn0 + row, o.mn - 1);
+            const int64_t at = KMAJOR ? (k0 + row) * o.ld + (mn < o.mn ? mn : 0) : mn * o.ld + k0 + piece * L::kPiece;
+            from[i] = static_cast<const char*>(o.at) + at * size;
+            if (i == 0) k = KMAJOR ? row : piece * L::kPiece;
+        }
+        step = KMAJOR ? (int64_t)L::kK * o.ld * size : kTileK;
     }
+    // Load i of the tile that has `left` of k left, to its place in LDS.
+    __device__ __forceinline__ void load(int i, int turn, int64_t left, const unsigned char* zeros, char* lds) const
+    {
+        const void* at = (KMAJOR ? k + i * (THREADS / L::kRow) : k) < left ? static_cast<const void*>(from[i] + turn * step) : zeros;
+        load_to_lds(at, lds + (i * THREADS + (threadIdx.x & ~(kWave - 1))) * 16);
+    }
+};
+
+// Waits until no more than N loads of this wave are on their way and its LDS reads are back, then for the other waves.
+template <int N>
+__device__ __forceinline__ void tile_barrier()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 // What a lane feeds the matrix unit with for 32 rows of mn and one step of k (two pieces): its row is lane % 32, its k are
@@ -265,24 +294,11 @@ __device__ __forceinline__ v16f multiply(typename Wide<T>::vec a, typename Wide<
     }
 }
 
-// Four adjacent elements of an output row, the first nv of them; rows may start at any element.
-template <int T>
-__device__ __forceinline__ void put4(typename ElemOf<T>::type* p, v4f v, int nv, bool whole, bool add)
-{
-    typedef typename ElemOf<T>::type E;
-    typedef typename ElemOf<T>::vec V4;
-    if (whole && nv == 4) {
-        if (add) v += __builtin_convertvector(*reinterpret_cast<const V4*>(p), v4f);
-        *reinterpret_cast<V4*>(p) = __builtin_convertvector(v, V4);
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < nv) p[i] = (E)(add ? v[i] + (float)p[i] : v[i]);
-}
-
-// A tile of BP by BQ of one product per workgroup of WP by WQ waves, two tiles of k in LDS: while the matrix units work on one the
-// other is loaded, one barrier a tile.  Lane l of a wave holds, of every 32 by 32 of its part, row q = l % 32 and 16 of the p.
+// A tile of BP by BQ of one product per workgroup of WP by WQ waves.  Lane l of a wave holds, of every 32 by 32 of its part, row
+// q = l % 32 and 16 of the p.  A turn is a tile of k, four steps of the matrix units; while a step is multiplied the next one's operands
+// are read from LDS.  LDS has five places for operands' tiles, taken in the order p, q, p, q, ...: two are read, three are on
+// their way.  One barrier a turn, before its last step: the next turn's tiles have arrived, and this turn's are read, so their
+// places take the q of the turn after the next and the p of the one behind that.
 template <int T, int BP, int BQ, int WP, int WQ, bool PMAJOR, bool QMAJOR, int WHAT>
 __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
 {
@@ -290,7 +306,8 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     typedef TilePart<T, BP, PMAJOR> LP;
     typedef TilePart<T, BQ, QMAJOR> LQ;
     constexpr int kThreads = WP * WQ * kWave, TP = BP / WP / 32, TQ = BQ / WQ / 32, kSteps = 4;
-    __shared__ __align__(16) char lds[2][LP::kBytes + LQ::kBytes];
+    constexpr int kPlaces = 5, kPlace = LP::kBytes > LQ::kBytes ? LP::kBytes : LQ::kBytes;
+    __shared__ __align__(16) char lds[kPlaces * kPlace];
 
     // Workgroups go round the eight dies; a die takes adjacent tiles, 8 of q by as many p, so its cache holds what they share.
     const int64_t tiles = (int64_t)a.tiles_p * a.tiles_q;
@@ -325,49 +342,127 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
         for (int j = 0; j < TQ; ++j) acc[i][j] = v16f{};
 
     const int turns = (int)((k_end - k_begin + LP::kK - 1) / LP::kK);
-    const auto load = [&](int turn) {
-        const int64_t k0 = k_begin + (int64_t)turn * LP::kK;
-        char* to = lds[turn & 1];
-        load_tile<T, BP, PMAJOR, kThreads>(a.p, p0, k0, a.head->zeros, to);
-        load_tile<T, BQ, QMAJOR, kThreads>(a.q, q0, k0, a.head->zeros, to + LP::kBytes);
+    const TileSource<T, BP, PMAJOR, kThreads> from_p(a.p, p0, k_begin);
+    const TileSource<T, BQ, QMAJOR, kThreads> from_q(a.q, q0, k_begin);
+    constexpr int kLoadsP = from_p.kLoads, kLoadsQ = from_q.kLoads;
+    const unsigned char* zeros = a.head->zeros;
+    const auto left = [&](int turn) { return a.p.k - k_begin - (int64_t)turn * LP::kK; };
+    const auto left_q = [&](int turn) { return a.q.k - k_begin - (int64_t)turn * LP::kK; };
+    const auto place = [&](int u) { return lds + u * kPlace; };
+    typename Wide<T>::vec fp[2][TP], fq[2][TQ];
+    constexpr int kReads = TP + TQ, kProducts = TP * TQ;
+    const auto read = [&](int r, int s, const char* at_p, const char* at_q) {
+        if (r < TQ) fq[s & 1][r] = read_tile<T, BQ, QMAJOR>(at_q, wq + 32 * r, s);
+        else fp[s & 1][r - TQ] = read_tile<T, BP, PMAJOR>(at_p, wp + 32 * (r - TQ), s);
     };
-    if (turns > 0) load(0);
-    for (int turn = 0; turn < turns; ++turn) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (turn + 1 < turns) load(turn + 1);
-        const char* from = lds[turn & 1];
+    // the products of step s, `beside(n)` behind the n-th
+    const auto step = [&](int s, auto&& beside) {
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            typename Wide<T>::vec fp[TP], fq[TQ];
-#pragma unroll
-            for (int i = 0; i < TP; ++i) fp[i] = read_tile<T, BP, PMAJOR>(from, wp + 32 * i, s);
-#pragma unroll
-            for (int j = 0; j < TQ; ++j) fq[j] = read_tile<T, BQ, QMAJOR>(from + LP::kBytes, wq + 32 * j, s);
-#pragma unroll
-            for (int i = 0; i < TP; ++i)
-#pragma unroll
-                for (int j = 0; j < TQ; ++j) acc[i][j] = multiply<T>(fp[i], fq[j], acc[i][j]);
+        for (int n = 0; n < kProducts; ++n) {
+            acc[n / TQ][n % TQ] = multiply<T>(fp[s & 1][n / TQ], fq[s & 1][n % TQ], acc[n / TQ][n % TQ]);
+            beside(n);
         }
-    }
-
-    // p of element e (0..15) of acc[i][.]: 32 i + 8 (e / 4) + 4 half + e % 4 behind wp
+    };
+    // the m-th of `of` things belongs behind product n
+    const auto due = [](int n, int m, int of) { return m * kProducts / of == n; };
+    // (loads of turns behind the last one bring zeros, or another part's, that nobody reads: no branch stands between the products)
 #pragma unroll
-    for (int j = 0; j < TQ; ++j) {
-        const int64_t q = q0 + wq + 32 * j + (lane & 31);
-        if constexpr (WHAT == kLogits) {
-            const bool live = q < count;
-            const int label = live ? a.label[q] : -1;
+    for (int u = 0; u < kPlaces - 1; ++u) {
+        const int turn = u / 2;
+        if (u % 2 == 0)
+#pragma unroll
+            for (int i = 0; i < kLoadsP; ++i) from_p.load(i, turn, left(turn), zeros, place(u));
+        else
+#pragma unroll
+            for (int i = 0; i < kLoadsQ; ++i) from_q.load(i, turn, left_q(turn), zeros, place(u));
+    }
+    tile_barrier<kLoadsP + kLoadsQ>();
+#pragma unroll
+    for (int r = 0; r < kReads; ++r) read(r, 0, place(0), place(1));
+    int unit = 0;               // the place of the turn's p
+    const auto behind = [&](int n) { return lds + (unit + n >= kPlaces ? unit + n - kPlaces : unit + n) * kPlace; };
+    for (int turn = 0; turn < turns; ++turn) {
+        const char* at_p = behind(0);
+        const char* at_q = behind(1);
+#pragma unroll
+        for (int s = 0; s < kSteps - 1; ++s)
+            step(s, [&](int n) {
+#pragma unroll
+                for (int r = 0; r < kReads; ++r)
+                    if (due(n, r, kReads)) read(r, s + 1, at_p, at_q);
+                if (s == 0)
+#pragma unroll
+                    for (int i = 0; i < kLoadsP; ++i)
+                        if (due(n, i, kLoadsP)) from_p.load(i, turn + 2, left(turn + 2), zeros, behind(4));
+            });
+        tile_barrier<kLoadsP>();
+        const char* next_p = behind(2);
+        const char* next_q = behind(3);
+        step(kSteps - 1, [&](int n) {
+#pragma unroll
+            for (int r = 0; r < kReads; ++r)
+                if (due(n, r, kReads)) read(r, 0, next_p, next_q);
+#pragma unroll
+            for (int i = 0; i < kLoadsQ; ++i)
+                if (due(n, i, kLoadsQ)) from_q.load(i, turn + 2, left_q(turn + 2), zeros, behind(0));
+        });
+        unit = unit + 2 >= kPlaces ? unit + 2 - kPlaces : unit + 2;
+    }
+    tile_barrier<0>();
+
+    // p of element e (0..15) of acc[i][.]: 32 i + 8 (e / 4) + 4 half + e % 4 behind wp.  Outputs of type E pass through LDS, [q][p] with
+    // the pieces of a row turned by the row's number, and leave as whole rows: straight from the lanes, 16 bytes in each of 32 rows at
+    // a time, a tile of logits took 35 us on top of the 70 of its products (2048 inputs, bf16).
+    typedef typename ElemOf<T>::vec V4;
+    typedef typename Wide<T>::vec V;
+    constexpr int kPiece = Wide<T>::n, kRowPieces = BP / kPiece;
+    static_assert(BP * BQ * (int)sizeof(E) <= kPlaces * kPlace && (kRowPieces & (kRowPieces - 1)) == 0, "the tile fits");
+    const auto piece_at = [&](int q, int piece) { return lds + (q * kRowPieces + (piece ^ (q & (kRowPieces - 1)))) * 16; };
+    const auto stage = [&](int i, int j, int g, v4f x) {
+        const int q = wq + 32 * j + (lane & 31), p = wp + 32 * i + 8 * g + 4 * half;
+        *reinterpret_cast<V4*>(piece_at(q, p / kPiece) + p % kPiece * sizeof(E)) = __builtin_convertvector(x, V4);
+    };
+    const auto four = [&](int i, int j, int g) { return v4f{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]}; };
+    // store(q, p, piece) for every piece of the tile
+    const auto leave = [&](auto&& store) {
+        __syncthreads();
+        for (int n = threadIdx.x; n < BQ * kRowPieces; n += kThreads)
+            store(n / kRowPieces, n % kRowPieces * kPiece, *reinterpret_cast<const V*>(piece_at(n / kRowPieces, n % kRowPieces)));
+    };
+    if constexpr (WHAT == kLogits) {
+        const int first = a.v0 + (int)p0 + wp + 4 * half;               // the class of the lane's first element
+        if (a.v0 + p0 + BP > a.V) {
+#pragma unroll
+            for (int j = 0; j < TQ; ++j)
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (first + 32 * i + 8 * (e / 4) + e % 4 >= a.V) acc[i][j][e] = -__builtin_inff();
+        }
+        const bool keep = a.held && a.v0 + p0 + BP > a.keep0;
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+            const int64_t q = q0 + wq + 32 * j + (lane & 31);
+            const int own = q < count ? a.label[q] - first : -1;        // which of the wave's classes is the label
+            if (__any(own >= 0 && own < BP / WP)) {
+                float picked = 0.f;
+                bool mine = false;
+#pragma unroll
+                for (int i = 0; i < TP; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const bool is = own == 32 * i + 8 * (e / 4) + e % 4;
+                        picked = is ? acc[i][j][e] : picked;
+                        mine |= is;
+                    }
+                if (mine) a.picked[q] = picked;
+            }
             float top = -__builtin_inff();
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int v = a.v0 + (int)p0 + wp + 32 * i + 8 * (e / 4) + 4 * half + e % 4;
-                    if (v >= a.V) acc[i][j][e] = -__builtin_inff();
-                    top = fmaxf(top, acc[i][j][e]);
-                    if (v == label) a.picked[q] = acc[i][j][e];
-                }
+                for (int e = 0; e < 16; ++e) top = fmaxf(top, acc[i][j][e]);
             top = fmaxf(top, __shfl_xor(top, 32, kWave));
             // (a slab of -inf alone has the sum 0; one with a NaN the sum NaN)
             const float from = top == -__builtin_inff() ? 0.f : top;
@@ -378,70 +473,85 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                 for (int e = 0; e < 16; ++e) {
                     const float x = exp_of(acc[i][j][e] - from);
                     sum += x;
-                    if constexpr (T != HSADMM_TYPE_F32) acc[i][j][e] = x;
+                    if constexpr (T != HSADMM_TYPE_F32) acc[i][j][e] = x * grad_unit<T>();
                 }
             sum += __shfl_xor(sum, 32, kWave);
             if (half == 0) a.slab[q * a.slabs + (a.v0 + p0 + wp) / (BP / WP)] = make_float2(top, sum);
-            if (a.held) {
-                typedef typename ElemOf<T>::vec V4;
-                E* row = static_cast<E*>(a.held) + q * a.ld;
+            if (keep)
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) {
-                        const int64_t c = a.v0 + p0 + wp + 32 * i + 8 * g + 4 * half - a.keep0;
-                        v4f x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                        if constexpr (T != HSADMM_TYPE_F32) x *= grad_unit<T>();
-                        if (c >= 0 && c < a.ld) *reinterpret_cast<V4*>(row + c) = __builtin_convertvector(x, V4);
-                    }
-            }
-        } else if constexpr (WHAT == kLogitGrads) {
-            const bool live = q < count;
-            const int label = live ? a.label[q] : -1;
-            const float2 stat = live ? a.stat[q] : make_float2(0.f, 0.f);
-            E* row = static_cast<E*>(a.held) + q * a.ld;
+                    for (int g = 0; g < 4; ++g) stage(i, j, g, four(i, j, g));
+        }
+        if (keep)
+            leave([&](int q, int p, V x) {
+                const int64_t c = a.v0 + p0 + p - a.keep0;
+                if (q0 + q < count && c >= 0 && c < a.ld) *reinterpret_cast<V*>(static_cast<E*>(a.held) + (q0 + q) * a.ld + c) = x;
+            });
+    } else if constexpr (WHAT == kLogitGrads) {
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+            const int64_t q = q0 + wq + 32 * j + (lane & 31);
+            const int label = q < count ? a.label[q] : -1;
+            const float2 stat = q < count ? a.stat[q] : make_float2(0.f, 0.f);
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int64_t c = p0 + wp + 32 * i + 8 * g + 4 * half;
-                    v4f x;
+                    const int v = a.v0 + (int)p0 + wp + 32 * i + 8 * g + 4 * half;
+                    v4f x = four(i, j, g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int v = a.v0 + (int)c + e;
-                        const float y = (exp_of(acc[i][j][4 * g + e] - stat.x) * stat.y - (v == label ? 1.f : 0.f)) * grad_unit<T>();
-                        x[e] = live && v < a.V ? y : 0.f;
+                        const float y = (exp_of(x[e] - stat.x) * stat.y - (v + e == label ? 1.f : 0.f)) * grad_unit<T>();
+                        x[e] = v + e < a.V ? y : 0.f;
                     }
-                    if (c < a.ld) *reinterpret_cast<typename ElemOf<T>::vec*>(row + c) = __builtin_convertvector(x, typename ElemOf<T>::vec);
+                    stage(i, j, g, x);
                 }
-        } else if constexpr (WHAT == kSums) {
-            float* row = a.sums + part * a.sum_part + q * a.ld;
+        }
+        leave([&](int q, int p, V x) {
+            if (q0 + q < count && p0 + p < a.ld) *reinterpret_cast<V*>(static_cast<E*>(a.held) + (q0 + q) * a.ld + p0 + p) = x;
+        });
+    } else if constexpr (WHAT == kSums) {
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+            float* row = a.sums + part * a.sum_part + (q0 + wq + 32 * j + (lane & 31)) * a.ld;
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int64_t c = p0 + wp + 32 * i + 8 * g + 4 * half;
-                    v4f x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+                    v4f x = four(i, j, g);
                     if (c < a.ld) {
                         if (a.add) x += *reinterpret_cast<const v4f*>(row + c);
                         *reinterpret_cast<v4f*>(row + c) = x;
                     }
                 }
-        } else {
-            if (q >= a.q.mn) continue;
-            const float f = a.head->factor * (1.f / grad_unit<T>());
-            E* row = static_cast<E*>(a.out) + q * a.ld;
-            const bool whole = a.ld % 4 == 0;       // (an arena's layers start at multiples of four elements)
+        }
+    } else {
+        const float f = a.head->factor * (1.f / grad_unit<T>());
+        E* out = static_cast<E*>(a.out);
+#pragma unroll
+        for (int j = 0; j < TQ; ++j) {
+            const int64_t q = q0 + wq + 32 * j + (lane & 31);
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const int64_t c = p0 + wp + 32 * i + 8 * g + 4 * half;
-                    const v4f x = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-                    const int nv = (int)min((int64_t)4, a.ld - c);
-                    if (nv > 0) put4<T>(row + c, x * f, nv, whole, a.add != 0);
+                    v4f x = four(i, j, g) * f;
+                    if (a.add) {
+                        // (added to before it is rounded)
+                        const int64_t c = p0 + wp + 32 * i + 8 * g + 4 * half;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (q < a.q.mn && c + e < a.ld) x[e] += (float)out[q * a.ld + c + e];
+                    }
+                    stage(i, j, g, x);
                 }
         }
+        leave([&](int q, int p, V x) {
+            const int64_t left = a.ld - p0 - p;
+            if (q0 + q < a.q.mn && left > 0) store_piece<T>(out + (q0 + q) * a.ld + p0 + p, x, (int)min(left, (int64_t)kPiece));
+        });
     }
 }
 
