@@ -2470,9 +2470,9 @@ static EmbedScratch embed_scratch(int32_t V, int32_t D, int64_t n)
     s.tile = n <= kSortMost ? kSortMost : kSortTile;
     while ((n + s.tile - 1) / s.tile > kSortTiles) s.tile *= 2;
     s.tiles = (int)((n + s.tile - 1) / s.tile);
-    // Stretches about as long as there are stretches, so that no row is a chain of more than some of either.
-    s.part = 64;
-    while ((int64_t)s.part * s.part * 4 < n) s.part *= 2;
+    // A row is a chain of at most `part` positions or of all stretches: of both some, whatever the tokens are.
+    s.part = 32;
+    while ((int64_t)s.part * s.part * 32 < n) s.part *= 2;
     s.stretches = (n + s.part - 1) / s.part;
     s.pitch = ((int64_t)D + 7) / 8 * 8;
     size_t at = 0;
@@ -2549,9 +2549,7 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     g.G = const_cast<void*>(at_elem(G, off, size));
     g.scale = scale; g.add = accumulate != 0;
     g.rows = 4;
-    while (g.rows < kGradRows && V / g.rows > 2048) g.rows *= 2;
-    g.run = 1;
-    while (g.run < g.rows && g.run * D < 2048) g.run *= 2;
+    while (g.rows < kGradRows && V / g.rows > 8192) g.rows *= 2;
     e = for_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
         hipError_t r = hipSuccess;
@@ -2625,7 +2623,7 @@ static ProductPlan plan_product(int64_t out_p, int64_t out_q, int64_t k, bool si
     r.fills = n >= kUnits;
     r.splits = 1;
     if (parts && k > 0) {
-        const int64_t at_once = kUnits * (r.b == 256 ? 1 : r.b == 128 ? 2 : 4);        // workgroups that share the chip
+        const int64_t at_once = kUnits * (r.b == 256 ? 1 : r.b == 128 || !sixteen ? 2 : 4);        // workgroups that share the chip
         const int64_t most = std::min<int64_t>({r.b >= 128 ? most_parts(r.b) : std::max<int64_t>(1, k / 128), std::max<int64_t>(1, 2 * at_once / n), 64});
         double best = 0.0;
         for (int64_t s = 1; s <= most; ++s) {
@@ -2702,6 +2700,10 @@ int hsadmm_softmax_loss_workspace(const hsadmm_plan_t* p, int32_t layer, int64_t
     return HSADMM_OK;
 }
 
+// Threads that share a row of so many bytes, a piece of 16 each at a time, and the workgroups of so many rows.
+static int row_lanes(int64_t bytes) { return bytes > 16 * kWave ? kBlock : kWave; }
+static unsigned row_grid(int64_t rows, int64_t bytes) { return (unsigned)((rows + kBlock / row_lanes(bytes) - 1) / (kBlock / row_lanes(bytes))); }
+
 // One product over all tiles of its output.
 template <int T, bool PMAJOR, bool QMAJOR, int WHAT>
 static hipError_t launch_product(const hsadmm_plan* p, KernelId kid, const ProductPlan& how, int64_t out_p, int64_t out_q, ProductArgs a,
@@ -2743,8 +2745,8 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
     hipError_t e = launch(p, kLossTargets, loss_targets, 1u, kScanBlock, s, x->labels, (int)(x->index_bits == 64), n, V, x->scale,
                           (int)(x->mean != 0), r, x->loss, x->lse);
     if (e == hipSuccess && n > 0)
-        e = launch(p, kLossRows, loss_rows<T, true>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s, static_cast<const E*>(x->X), x->x_stride,
-                   n, (int)D, r, rows, (int)ws.Dp);
+        e = launch(p, kLossRows, loss_rows<T, true>, row_grid(n, ws.Dp * size), kBlock, s, static_cast<const E*>(x->X), x->x_stride, n, (int)D, r,
+                   rows, (int)ws.Dp, row_lanes(ws.Dp * size));
     ProductArgs a{};
     a.head = r.head;
     a.V = V;
@@ -2763,8 +2765,8 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
             return hipSuccess;
         }
         *o = Operand{packed, ws.Dp, classes, ws.Dp};
-        return launch(p, kLossRows, loss_rows<T, false>, (unsigned)((classes + kWaves - 1) / kWaves), kBlock, s, W + (int64_t)v0 * D,
-                      (int64_t)D, classes, (int)D, r, packed, (int)ws.Dp);
+        return launch(p, kLossRows, loss_rows<T, false>, row_grid(classes, ws.Dp * size), kBlock, s, W + (int64_t)v0 * D, (int64_t)D, classes,
+                      (int)D, r, packed, (int)ws.Dp, row_lanes(ws.Dp * size));
     };
     const int32_t last = (int32_t)((ws.pieces - 1) * ws.Vc);
     if (n > 0) {
@@ -2850,8 +2852,8 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
         }
     }
     if (e == hipSuccess && x->dX && n > 0)
-        e = launch(p, kLossInputs, loss_inputs<T>, (unsigned)((n + kWaves - 1) / kWaves), kBlock, s, (const float*)(w + ws.sums), ws.inputs.splits,
-                   ws.Np * ws.Dp, ws.Dp, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D);
+        e = launch(p, kLossInputs, loss_inputs<T>, row_grid(n, D * size), kBlock, s, (const float*)(w + ws.sums), ws.inputs.splits, ws.Np * ws.Dp,
+                   ws.Dp, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D, row_lanes(D * size));
     return e;
 }
 

@@ -116,16 +116,16 @@ __global__ __launch_bounds__(kScanBlock) void loss_targets(const void* __restric
 
 // Copies rows of `cols` elements that lie ld apart to rows of `pitch` (a multiple of kInputCols), zeros behind the last column.  LIST:
 // the rows of the list (those that have a target: what the others hold, NaN included, is not looked at again).  The products then
-// load whole 16-byte pieces and know no strides.  A wave takes a row.
+// load whole 16-byte pieces and know no strides.  `lanes` threads (a wave or four) share a row.
 template <int T, bool LIST>
 __global__ __launch_bounds__(kBlock) void loss_rows(const typename ElemOf<T>::type* __restrict__ src, int64_t ld, int64_t rows, int cols,
-                                                    LossRows r, typename ElemOf<T>::type* __restrict__ dst, int pitch)
+                                                    LossRows r, typename ElemOf<T>::type* __restrict__ dst, int pitch, int lanes)
 {
     constexpr int n = Wide<T>::n;
-    const int64_t j = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+    const int64_t j = (int64_t)blockIdx.x * (kBlock / lanes) + threadIdx.x / lanes;
     if (j >= (LIST ? (int64_t)r.head->count : rows)) return;
     const typename ElemOf<T>::type* from = src + (LIST ? (int64_t)r.row[j] : j) * ld;
-    for (int c = (threadIdx.x % kWave) * n; c < pitch; c += kWave * n)
+    for (int c = (threadIdx.x & (lanes - 1)) * n; c < pitch; c += lanes * n)
         *reinterpret_cast<typename Wide<T>::vec*>(dst + j * pitch + c) = load_piece<T>(from + c, cols - c);
 }
 
@@ -346,6 +346,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     const TileSource<T, BQ, QMAJOR, kThreads> from_q(a.q, q0, k_begin);
     constexpr int kLoadsP = from_p.kLoads, kLoadsQ = from_q.kLoads;
     const unsigned char* zeros = a.head->zeros;
+    // Where a call streams its weights past a few rows (BQ = 32), workgroups begin at different turns: rows of a power of two of bytes
+    // that all workgroups read at the same column keep a few of the memory's channels busy.
+    const int begin = BQ < 64 && turns > 0 ? (int)(p0 / BP % turns) : 0;
+    const auto at_turn = [&](int turn) { return BQ < 64 ? (turn + begin < turns ? turn + begin : turn + begin - turns) : turn; };
     const auto left = [&](int turn) { return a.p.k - k_begin - (int64_t)turn * LP::kK; };
     const auto left_q = [&](int turn) { return a.q.k - k_begin - (int64_t)turn * LP::kK; };
     const auto place = [&](int u) { return lds + u * kPlace; };
@@ -371,10 +375,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
         const int turn = u / 2;
         if (u % 2 == 0)
 #pragma unroll
-            for (int i = 0; i < kLoadsP; ++i) from_p.load(i, turn, left(turn), zeros, place(u));
+            for (int i = 0; i < kLoadsP; ++i) from_p.load(i, at_turn(turn), left(at_turn(turn)), zeros, place(u));
         else
 #pragma unroll
-            for (int i = 0; i < kLoadsQ; ++i) from_q.load(i, turn, left_q(turn), zeros, place(u));
+            for (int i = 0; i < kLoadsQ; ++i) from_q.load(i, at_turn(turn), left_q(at_turn(turn)), zeros, place(u));
     }
     tile_barrier<kLoadsP + kLoadsQ>();
 #pragma unroll
@@ -393,7 +397,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                 if (s == 0)
 #pragma unroll
                     for (int i = 0; i < kLoadsP; ++i)
-                        if (due(n, i, kLoadsP)) from_p.load(i, turn + 2, left(turn + 2), zeros, behind(4));
+                        if (due(n, i, kLoadsP)) from_p.load(i, at_turn(turn + 2), left(at_turn(turn + 2)), zeros, behind(4));
             });
         tile_barrier<kLoadsP>();
         const char* next_p = behind(2);
@@ -404,7 +408,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                 if (due(n, r, kReads)) read(r, 0, next_p, next_q);
 #pragma unroll
             for (int i = 0; i < kLoadsQ; ++i)
-                if (due(n, i, kLoadsQ)) from_q.load(i, turn + 2, left_q(turn + 2), zeros, behind(0));
+                if (due(n, i, kLoadsQ)) from_q.load(i, at_turn(turn + 2), left_q(at_turn(turn + 2)), zeros, behind(0));
         });
         unit = unit + 2 >= kPlaces ? unit + 2 - kPlaces : unit + 2;
     }
@@ -692,14 +696,14 @@ __global__ __launch_bounds__(kBlock) void loss_total(const LossHead* __restrict_
 // The gradients of the inputs: the parts' sums in order, times the factor, to the rows they belong to; zeros where there is no target.
 template <int T>
 __global__ __launch_bounds__(kBlock) void loss_inputs(const float* __restrict__ sums, int splits, int64_t part, int64_t sum_ld, LossRows r,
-                                                      typename ElemOf<T>::type* __restrict__ dX, int64_t ld, int64_t n, int cols)
+                                                      typename ElemOf<T>::type* __restrict__ dX, int64_t ld, int64_t n, int cols, int lanes)
 {
     constexpr int m = Wide<T>::n;
-    const int64_t i = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+    const int64_t i = (int64_t)blockIdx.x * (kBlock / lanes) + threadIdx.x / lanes;
     if (i >= n) return;
     const int64_t q = r.place[i];
     const float f = r.head->factor * (1.f / grad_unit<T>());
-    for (int c = (threadIdx.x % kWave) * m; c < cols; c += kWave * m) {
+    for (int c = (threadIdx.x & (lanes - 1)) * m; c < cols; c += lanes * m) {
         v4f x[m / 4] = {};
         if (q >= 0)
 #pragma unroll

@@ -259,17 +259,32 @@ struct EmbedGradArgs {
     void* G;
     float scale;
     int add;
-    int rows, run;      // of a workgroup (see embedding_gradient), powers of two
+    int rows;           // of a workgroup of embedding_gradient
 };
 
-// First place in the sorted list whose token is at least v.
-__device__ __forceinline__ int lower_bound(const int32_t* __restrict__ key, int n, int32_t v)
+// First place of [lo, hi) in the sorted list whose token is at least v.
+__device__ __forceinline__ int lower_bound(const int32_t* __restrict__ key, int lo, int hi, int32_t v)
 {
-    int lo = 0, hi = n;
     while (lo < hi) {
         const int mid = lo + (hi - lo) / 2;
         if (key[mid] < v) lo = mid + 1;
         else hi = mid;
+    }
+    return lo;
+}
+
+// The same by a whole wave, which looks at 64 places at a time.
+__device__ __forceinline__ int lower_bound_wave(const int32_t* __restrict__ key, int n, int32_t v)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int step = (hi - lo + kWave - 1) / kWave;
+        const int64_t at = lo + (int64_t)(lane + 1) * step - 1;        // (the last one is hi - 1 or behind it)
+        const int below = __popcll(__ballot(at < hi && key[at < hi ? at : hi - 1] < v));
+        const int64_t end = lo + (int64_t)(below + 1) * step - 1;
+        lo = (int)min((int64_t)hi, lo + (int64_t)below * step);
+        hi = (int)min((int64_t)hi, end);
     }
     return lo;
 }
@@ -333,7 +348,7 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
     const int64_t b = blockIdx.x;
     const int from = (int)(b * a.part), to = (int)min((int64_t)a.n, (b + 1) * a.part);
     // the extent of the tokens of the first and the last position
-    if (threadIdx.x < 4) bound[threadIdx.x] = lower_bound(a.key, a.n, a.key[threadIdx.x < 2 ? from : to - 1] + (threadIdx.x & 1));
+    if (threadIdx.x < 4) bound[threadIdx.x] = lower_bound(a.key, 0, a.n, a.key[threadIdx.x < 2 ? from : to - 1] + (threadIdx.x & 1));
     __syncthreads();
     const bool first = a.key[from] < a.V && bound[1] - bound[0] > a.part;
     const bool last = a.key[to - 1] < a.V && bound[3] - bound[2] > a.part && bound[2] != bound[0];
@@ -359,11 +374,11 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
     }
 }
 
-// The rows of dW: a workgroup takes `rows` of them, a wave one after the other; runs of `run` adjacent rows, the runs of a workgroup
-// as far apart as the grid is wide, as the frequent tokens often are the first ones.  A wave has kAcross pieces of 16 bytes a lane of
-// one or a few tokens' rows in flight at once.
+// The rows of dW: a workgroup takes `rows` adjacent ones, a wave one after the other; where their tokens lie in the list is found by
+// whole waves for all of them and then between those places for each.  A wave has kAcross pieces of 16 bytes a lane of one or a few
+// tokens' rows in flight at once.
 constexpr int kGradRows = 64;           // at most
-constexpr int kAcross = 4;
+constexpr int kAcross = 2;
 
 template <int T>
 __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
@@ -372,18 +387,19 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
     typedef typename Wide<T>::vec V;
     typedef typename Wide<T>::any A;
     constexpr int m = Wide<T>::n;
-    __shared__ int bound[kGradRows][2];
-    const auto row_of = [&](int i) { return ((int64_t)(i / a.run) * gridDim.x + blockIdx.x) * a.run + i % a.run; };
-    if (threadIdx.x < 2 * a.rows) {
-        const int64_t v = row_of(threadIdx.x >> 1);
-        bound[threadIdx.x >> 1][threadIdx.x & 1] = v < a.V ? lower_bound(a.key, a.n, (int32_t)v + (int)(threadIdx.x & 1)) : 0;
+    __shared__ int ends[2], bound[kGradRows + 1];
+    const int64_t v0 = (int64_t)blockIdx.x * a.rows;
+    const int rows = (int)min((int64_t)a.rows, a.V - v0), wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
+    if (wave < 2) {
+        const int at = lower_bound_wave(a.key, a.n, (int32_t)v0 + (wave ? rows : 0));
+        if (lane == 0) ends[wave] = at;
     }
     __syncthreads();
-    const int lane = threadIdx.x & (kWave - 1);
-    for (int i = threadIdx.x / kWave; i < a.rows; i += kWaves) {
-        const int64_t v = row_of(i);
-        if (v >= a.V) continue;
-        const int from = __builtin_amdgcn_readfirstlane(bound[i][0]), to = __builtin_amdgcn_readfirstlane(bound[i][1]);
+    if ((int)threadIdx.x <= rows) bound[threadIdx.x] = lower_bound(a.key, ends[0], ends[1], (int32_t)v0 + threadIdx.x);
+    __syncthreads();
+    for (int i = wave; i < rows; i += kWaves) {
+        const int64_t v = v0 + i;
+        const int from = __builtin_amdgcn_readfirstlane(bound[i]), to = __builtin_amdgcn_readfirstlane(bound[i + 1]);
         if (from == to && a.add) continue;
         E* row = static_cast<E*>(a.G) + v * a.cols;
         // a token with many positions: its stretches, of which the first holds it as the second one if it begins inside
@@ -416,18 +432,29 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
                 for (int k = 0; k < kAcross; ++k)
                     if (on[k]) g[k] = *reinterpret_cast<const A*>(row + c[k]);
             if (!many) {
-                add_rows<T, kAcross, 4>(a, from, to, c, on, x);
+                add_rows<T, kAcross, 8>(a, from, to, c, on, x);
             } else {
-                for (int64_t b = b0; b <= b1; ++b) {
-                    const float* sums = a.sums + (2 * b + (b == b0 ? begins : 0)) * a.pitch;
+                constexpr int kAtOnce = 4;
+                for (int64_t b = b0; b <= b1; b += kAtOnce) {
+                    v4f y[kAtOnce][kAcross][m / 4];
 #pragma unroll
-                    for (int k = 0; k < kAcross; ++k)
-                        if (on[k])
+                    for (int u = 0; u < kAtOnce; ++u) {
+                        const int64_t at = min(b + u, b1);
+                        const float* sums = a.sums + (2 * at + (at == b0 ? begins : 0)) * a.pitch;
 #pragma unroll
-                            for (int e = 0; e < m; e += 4) {
-                                const v4f y = ld4u(sums + c[k] + e);
-                                x[k][e] += y.x; x[k][e + 1] += y.y; x[k][e + 2] += y.z; x[k][e + 3] += y.w;
-                            }
+                        for (int k = 0; k < kAcross; ++k)
+                            if (on[k])
+#pragma unroll
+                                for (int e = 0; e < m / 4; ++e) y[u][k][e] = ld4u(sums + c[k] + 4 * e);
+                    }
+#pragma unroll
+                    for (int u = 0; u < kAtOnce; ++u)
+                        if (b + u <= b1)
+#pragma unroll
+                            for (int k = 0; k < kAcross; ++k)
+                                if (on[k])
+#pragma unroll
+                                    for (int e = 0; e < m; ++e) x[k][e] += y[u][k][e / 4][e % 4];
                 }
             }
 #pragma unroll
