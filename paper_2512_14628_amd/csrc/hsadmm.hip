@@ -2637,6 +2637,8 @@ static ProductPlan plan_product(int64_t out_p, int64_t out_q, int64_t k, bool si
     return r;
 }
 
+constexpr int64_t kFewTerms = 256;
+
 // How hsadmm_softmax_loss cuts its products, and where its scratch lies in the workspace.
 struct LossScratch {
     size_t head, row, label, place, held_loss, picked, stat, slab, rows, packed, parts, grads, sums, total;
@@ -2644,7 +2646,8 @@ struct LossScratch {
     int64_t Vc;                 // classes of a piece, a multiple of 256
     int pieces;
     bool pack;                  // W's rows are copied before they are used (not whole pieces of 16 bytes)
-    bool small;                 // logits in parts, joined by rows
+    bool small;                 // logits in fp32 and in parts, joined by rows
+    bool rest_inputs, rest_weights;     // the products with what the rounding of the logits' gradients leaves are added
     ProductPlan logits, inputs, weights;
     int slab_elems;
     int64_t slabs;
@@ -2663,7 +2666,13 @@ static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int6
     s.Vc = ((V + s.pieces - 1) / s.pieces + 255) / 256 * 256;
     s.pieces = (int)((V + s.Vc - 1) / s.Vc);
     s.logits = plan_product(V, n, s.Dp, sixteen, narrow, false);
-    s.small = !s.logits.fills && s.pieces == 1;
+    // Rounding the gradients of the logits to 16 bits is lost among the terms of a long sum.  In a short one (a vocabulary of a few
+    // classes for the inputs' gradient, a few rows for the weights') it would add half as much again to the rounding of the output:
+    // there what is left of the rounding is multiplied too, twice the time of a product that is short.
+    const bool fits = s.pieces == 1 && 4 * s.Np * s.Vc <= p->loss_held;
+    s.rest_inputs = gradients && sixteen && fits && V <= kFewTerms;
+    s.rest_weights = gradients && sixteen && fits && n <= kFewTerms;
+    s.small = (!s.logits.fills && s.pieces == 1) || s.rest_inputs || s.rest_weights;
     if (s.small) s.logits = plan_product(V, n, s.Dp, sixteen, narrow, true);
     else if (!narrow && s.logits.b == 64) s.logits.b = 128;
     s.inputs = plan_product(D, n, s.Vc, sixteen, narrow, true);
@@ -2683,7 +2692,7 @@ static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int6
     s.rows = take(size * s.Np * s.Dp);
     s.packed = take(s.pack ? size * s.Vc * s.Dp : 0);
     s.parts = take(s.small ? 4 * (int64_t)s.logits.splits * s.Np * s.Vc : 0);
-    s.grads = take(gradients ? size * s.Np * s.Vc : 0);
+    s.grads = take(gradients ? size * s.Np * s.Vc * (s.rest_inputs || s.rest_weights ? 2 : 1) : 0);
     s.sums = take(gradients ? 4 * (int64_t)s.inputs.splits * s.Np * s.Dp : 0);
     s.total = at;
     return s;
@@ -2804,6 +2813,7 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
         m.loss = x->loss; m.lse = x->lse;
         m.held = w + ws.grads;
         m.grads = gradients ? w + ws.grads : nullptr;
+        m.rest = ws.rest_inputs || ws.rest_weights ? size * ws.Np * ws.Vc : 0;
         m.ld = ws.Vc;
         m.v0 = last; m.V = V;
         // (a row of few elements keeps a small workgroup busy; few rows have to share the chip by themselves)
@@ -2837,6 +2847,7 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
             f.sum_part = ws.Np * ws.Dp;
             f.ld = ws.Dp;
             f.add = v0 != last;
+            f.rest = ws.rest_inputs ? size * ws.Np * ws.Vc : 0;
             e = launch_product<T, true, false, kSums>(p, kLossInputGrads, ws.inputs, D, n, f, s);
         }
         if (e == hipSuccess && x->G) {
@@ -2846,6 +2857,7 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
             f.out = static_cast<E*>(x->G) + off + (int64_t)v0 * D;
             f.ld = D;
             f.add = x->accumulate != 0;
+            f.rest = ws.rest_weights ? size * ws.Np * ws.Vc : 0;
             ProductPlan how = ws.weights;
             how.k_part = INT64_MAX / 2;
             e = launch_product<T, true, true, kWeightGrads>(p, kLossWeightGrads, how, D, classes, f, s);

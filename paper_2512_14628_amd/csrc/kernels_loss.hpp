@@ -148,6 +148,7 @@ struct ProductArgs {
     int tiles_p, tiles_q;       // tiles of the output
     int splits;                 // parts of the k axis (kSums)
     int64_t k_part;             // length of a part, a multiple of the tile's
+    int64_t rest;               // 0, or bytes from q to what its rounding has left, which is multiplied as well
     // kLogits, kLogitGrads
     int32_t v0, V;              // first class of the piece, all classes
     const int32_t* label;
@@ -230,9 +231,9 @@ struct TileSource {
         step = KMAJOR ? (int64_t)L::kK * o.ld * size : kTileK;
     }
     // Load i of the tile that has `left` of k left, to its place in LDS.
-    __device__ __forceinline__ void load(int i, int turn, int64_t left, const unsigned char* zeros, char* lds) const
+    __device__ __forceinline__ void load(int i, int turn, int64_t left, const unsigned char* zeros, char* lds, int64_t skip = 0) const
     {
-        const void* at = (KMAJOR ? k + i * (THREADS / L::kRow) : k) < left ? static_cast<const void*>(from[i] + turn * step) : zeros;
+        const void* at = (KMAJOR ? k + i * (THREADS / L::kRow) : k) < left ? static_cast<const void*>(from[i] + turn * step + skip) : zeros;
         load_to_lds(at, lds + (i * THREADS + (threadIdx.x & ~(kWave - 1))) * 16);
     }
 };
@@ -341,15 +342,19 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
 #pragma unroll
         for (int j = 0; j < TQ; ++j) acc[i][j] = v16f{};
 
-    const int turns = (int)((k_end - k_begin + LP::kK - 1) / LP::kK);
+    const int once = max(0, (int)((k_end - k_begin + LP::kK - 1) / LP::kK)), turns = a.rest ? 2 * once : once;
     const TileSource<T, BP, PMAJOR, kThreads> from_p(a.p, p0, k_begin);
     const TileSource<T, BQ, QMAJOR, kThreads> from_q(a.q, q0, k_begin);
     constexpr int kLoadsP = from_p.kLoads, kLoadsQ = from_q.kLoads;
     const unsigned char* zeros = a.head->zeros;
     // Where a call streams its weights past a few rows (BQ = 32), workgroups begin at different turns: rows of a power of two of bytes
     // that all workgroups read at the same column keep a few of the memory's channels busy.
-    const int begin = BQ < 64 && turns > 0 ? (int)(p0 / BP % turns) : 0;
-    const auto at_turn = [&](int turn) { return BQ < 64 ? (turn + begin < turns ? turn + begin : turn + begin - turns) : turn; };
+    const int begin = BQ < 64 && once > 0 ? (int)(p0 / BP % once) : 0;
+    const auto at_turn = [&](int turn) {
+        const int u = turn >= once && a.rest ? turn - once : turn;
+        return BQ < 64 ? (u + begin < once ? u + begin : u + begin - once) : u;
+    };
+    const auto skip = [&](int turn) { return turn >= once ? a.rest : 0; };
     const auto left = [&](int turn) { return a.p.k - k_begin - (int64_t)turn * LP::kK; };
     const auto left_q = [&](int turn) { return a.q.k - k_begin - (int64_t)turn * LP::kK; };
     const auto place = [&](int u) { return lds + u * kPlace; };
@@ -378,7 +383,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
             for (int i = 0; i < kLoadsP; ++i) from_p.load(i, at_turn(turn), left(at_turn(turn)), zeros, place(u));
         else
 #pragma unroll
-            for (int i = 0; i < kLoadsQ; ++i) from_q.load(i, at_turn(turn), left_q(at_turn(turn)), zeros, place(u));
+            for (int i = 0; i < kLoadsQ; ++i) from_q.load(i, at_turn(turn), left_q(at_turn(turn)), zeros, place(u), skip(turn));
     }
     tile_barrier<kLoadsP + kLoadsQ>();
 #pragma unroll
@@ -408,7 +413,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                 if (due(n, r, kReads)) read(r, 0, next_p, next_q);
 #pragma unroll
             for (int i = 0; i < kLoadsQ; ++i)
-                if (due(n, i, kLoadsQ)) from_q.load(i, at_turn(turn + 2), left_q(at_turn(turn + 2)), zeros, behind(0));
+                if (due(n, i, kLoadsQ)) from_q.load(i, at_turn(turn + 2), left_q(at_turn(turn + 2)), zeros, behind(0), skip(turn + 2));
         });
         unit = unit + 2 >= kPlaces ? unit + 2 - kPlaces : unit + 2;
     }
@@ -577,6 +582,7 @@ struct SoftmaxArgs {
     float* lse;
     const void* held;           // with slabs: of the classes from v0 on, as kLogits wrote them
     void* grads;                // [rows][ld] gradients of the logits, may be null; with slabs held itself
+    int64_t rest;               // 0, or (16 bits, without slabs) bytes from grads to what their rounding leaves
     int64_t ld;
     int32_t v0, V;
 };
@@ -608,6 +614,7 @@ __device__ __forceinline__ float2 join(float2 a, float2 b)
 // A row per workgroup: largest logit, sum, loss, and the gradients of the logits that are held (softmax minus the label's one).  The order
 // of the additions depends on the sizes alone.  16 bits: what kLogits held is rounded already, so a gradient here carries two
 // roundings; the label's own comes from its logit in fp32, as softmax - 1 of a confident row has far fewer digits than either.
+// Without slabs what the rounding leaves is written as well where the call is one of few terms (a.rest).
 template <int T>
 __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
 {
@@ -650,10 +657,11 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
     if (!a.grads) return;
     const float own = (exp_of(picked - s.x) * inv - 1.f) * grad_unit<T>();
     E* to = static_cast<E*>(a.grads) + q * a.ld;
+    E* to_rest = reinterpret_cast<E*>(reinterpret_cast<char*>(to) + a.rest);
     const E* held = static_cast<const E*>(a.held) + q * a.ld;
     for (int64_t c = (int64_t)tid * n; c < a.ld; c += threads * n) {
         const int64_t v = a.v0 + c;
-        V x = {};
+        V x = {}, rest = {};
         if (v < a.V) {
             if (T != HSADMM_TYPE_F32 && a.slab) {
                 const float f = exp_of(a.slab[q * a.pitch + v / a.slab_elems].x - s.x) * inv;
@@ -663,7 +671,12 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
             } else {
                 const float* from = a.slab ? reinterpret_cast<const float*>(held) : sum_row;
 #pragma unroll
-                for (int e = 0; e < n; ++e) x[e] = (E)(exp_of(from[c + e] - s.x) * inv * grad_unit<T>());
+                for (int e = 0; e < n; ++e) {
+                    float y = exp_of(from[c + e] - s.x) * inv * grad_unit<T>();
+                    if (v + e == label) y = own;
+                    x[e] = (E)y;
+                    rest[e] = (E)(v + e < a.V ? y - (float)x[e] : 0.f);
+                }
             }
 #pragma unroll
             for (int e = 0; e < n; ++e) {
@@ -671,6 +684,7 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
                 if (v + e >= a.V) x[e] = (E)0.f;
             }
         }
+        if (a.rest) *reinterpret_cast<V*>(to_rest + c) = rest;
         *reinterpret_cast<V*>(to + c) = x;
     }
 }

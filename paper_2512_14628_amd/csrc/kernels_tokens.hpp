@@ -157,26 +157,31 @@ __device__ void sort_move(const SortArgs& a, int pass, int tile, SortShared& s)
 __device__ void sort_places(SortShared& s, const uint32_t* start, int stride)
 {
     const int d = threadIdx.x, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-    uint32_t all = 0;
-    if (d < kDigits)
-        for (int w = 0; w < kScanWaves; ++w) all += s.count[w][d];
-    uint32_t upto = all;
-    for (int o = 1; o < kWave; o <<= 1) {
-        const uint32_t x = __shfl_up(upto, o, kWave);
-        if (lane >= o) upto += x;
+    uint32_t own[kScanWaves], all = 0;
+    const uint32_t begin = start && d < kDigits ? start[(int64_t)d * stride] : 0;
+#pragma unroll
+    for (int w = 0; w < kScanWaves; ++w) {
+        own[w] = d < kDigits ? s.count[w][d] : 0;
+        all += own[w];
     }
-    if (lane == kWave - 1) s.sums[wave] = upto;
-    __syncthreads();
-    uint32_t at = upto - all;
-    for (int w = 0; w < wave; ++w) at += s.sums[w];
-    if (d < kDigits) {
-        if (start) at = start[(int64_t)d * stride];
-        for (int w = 0; w < kScanWaves; ++w) {
-            const uint32_t c = s.count[w][d];
-            s.count[w][d] = at;
-            at += c;
+    uint32_t at = begin;
+    if (!start) {
+        uint32_t upto = all;
+        for (int o = 1; o < kWave; o <<= 1) {
+            const uint32_t x = __shfl_up(upto, o, kWave);
+            if (lane >= o) upto += x;
         }
+        if (lane == kWave - 1) s.sums[wave] = upto;
+        __syncthreads();
+        at = upto - all;
+        for (int w = 0; w < wave; ++w) at += s.sums[w];
     }
+    if (d < kDigits)
+#pragma unroll
+        for (int w = 0; w < kScanWaves; ++w) {
+            s.count[w][d] = at;
+            at += own[w];
+        }
     __syncthreads();
 }
 
@@ -213,7 +218,9 @@ __global__ __launch_bounds__(kScanBlock) void token_scan(uint32_t* __restrict__ 
     uint32_t own[kMost], all = 0;
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
-        own[i] = i < each && first + i < n ? counts[first + i] : 0;
+        if (i >= each) { own[i] = 0; continue; }        // (the same for all threads)
+        const uint32_t c = counts[min(first + i, n - 1)];
+        own[i] = first + i < n ? c : 0;
         all += own[i];
     }
     uint32_t upto = all;
@@ -289,11 +296,10 @@ __device__ __forceinline__ int lower_bound_wave(const int32_t* __restrict__ key,
     return lo;
 }
 
-// x += dY rows of the sorted places [from, to), K pieces of 16 bytes at the columns c[0 .. K) of which `on` says which are wanted;
-// AT_ONCE rows in flight.  (The pieces are whole: a branch for the end of a row would have every load waited for where it stands.)
+// x += dY rows of the sorted places [from, to), K pieces of 16 bytes at the columns c[0 .. K); AT_ONCE rows in flight.  (The pieces
+// are whole and all of them are read, also by lanes that have none to write: with a branch every load is waited for where it stands.)
 template <int T, int K, int AT_ONCE>
-__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, const int (&c)[K], const bool (&on)[K],
-                                         float (&x)[K][Wide<T>::n])
+__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, const int (&c)[K], float (&x)[K][Wide<T>::n])
 {
     typedef typename ElemOf<T>::type E;
     typedef typename Wide<T>::vec V;
@@ -307,15 +313,14 @@ __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int t
             const E* row = dY + (int64_t)__builtin_amdgcn_readlane(pos, at + u) * a.ld;
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (on[k]) y[u][k] = *reinterpret_cast<const typename Wide<T>::any*>(row + c[k]);
+                y[u][k] = *reinterpret_cast<const typename Wide<T>::any*>(row + c[k]);
         }
 #pragma unroll
         for (int u = 0; u < kCount; ++u)
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                if (on[k])
 #pragma unroll
-                    for (int e = 0; e < Wide<T>::n; ++e) x[k][e] += (float)y[u][k][e];
+                for (int e = 0; e < Wide<T>::n; ++e) x[k][e] += (float)y[u][k][e];
     };
     for (int t = from; t < to; t += kWave) {
         const int n = min(kWave, to - t);
@@ -364,10 +369,9 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
         for (int c0 = threadIdx.x / kWave * kWave * m; c0 < a.cols; c0 += kBlock * m) {
             const int at = c0 + (threadIdx.x & (kWave - 1)) * m;
             const int c[1] = {min(at, a.cols - m)};
-            const bool on[1] = {at < a.cols};
             float x[1][m] = {};
-            add_rows<T, 1, 16>(a, f, t, c, on, x);
-            if (on[0])
+            add_rows<T, 1, 16>(a, f, t, c, x);
+            if (at < a.cols)
 #pragma unroll
                 for (int e = 0; e < m; ++e) sums[c[0] + e] = x[0][e];
         }
@@ -397,10 +401,17 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
     __syncthreads();
     if ((int)threadIdx.x <= rows) bound[threadIdx.x] = lower_bound(a.key, ends[0], ends[1], (int32_t)v0 + threadIdx.x);
     __syncthreads();
+    // rows without a token first: nothing waits for anything
+    if (!a.add)
+        for (int i = wave; i < rows; i += kWaves) {
+            if (bound[i] != bound[i + 1]) continue;
+            E* row = static_cast<E*>(a.G) + (v0 + i) * a.cols;
+            for (int c = lane * m; c < a.cols; c += kWave * m) store_piece<T>(row + c, V{}, a.cols - c);
+        }
     for (int i = wave; i < rows; i += kWaves) {
         const int64_t v = v0 + i;
         const int from = __builtin_amdgcn_readfirstlane(bound[i]), to = __builtin_amdgcn_readfirstlane(bound[i + 1]);
-        if (from == to && a.add) continue;
+        if (from == to) continue;
         E* row = static_cast<E*>(a.G) + v * a.cols;
         // a token with many positions: its stretches, of which the first holds it as the second one if it begins inside
         const bool many = to - from > a.part;
@@ -430,11 +441,11 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
             if (a.add)
 #pragma unroll
                 for (int k = 0; k < kAcross; ++k)
-                    if (on[k]) g[k] = *reinterpret_cast<const A*>(row + c[k]);
+                    g[k] = *reinterpret_cast<const A*>(row + c[k]);
             if (!many) {
-                add_rows<T, kAcross, 8>(a, from, to, c, on, x);
+                add_rows<T, kAcross, 4>(a, from, to, c, x);
             } else {
-                constexpr int kAtOnce = 4;
+                constexpr int kAtOnce = 2;
                 for (int64_t b = b0; b <= b1; b += kAtOnce) {
                     v4f y[kAtOnce][kAcross][m / 4];
 #pragma unroll
@@ -443,18 +454,16 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
                         const float* sums = a.sums + (2 * at + (at == b0 ? begins : 0)) * a.pitch;
 #pragma unroll
                         for (int k = 0; k < kAcross; ++k)
-                            if (on[k])
 #pragma unroll
-                                for (int e = 0; e < m / 4; ++e) y[u][k][e] = ld4u(sums + c[k] + 4 * e);
+                            for (int e = 0; e < m / 4; ++e) y[u][k][e] = ld4u(sums + c[k] + 4 * e);
                     }
 #pragma unroll
                     for (int u = 0; u < kAtOnce; ++u)
                         if (b + u <= b1)
 #pragma unroll
                             for (int k = 0; k < kAcross; ++k)
-                                if (on[k])
 #pragma unroll
-                                    for (int e = 0; e < m; ++e) x[k][e] += y[u][k][e / 4][e % 4];
+                                for (int e = 0; e < m; ++e) x[k][e] += y[u][k][e / 4][e % 4];
                 }
             }
 #pragma unroll
