@@ -2453,6 +2453,9 @@ int hsadmm_embedding(const hsadmm_plan_t* p, int32_t layer, const void* W, int32
     return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;
 }
 
+// Workgroups that clear rows beside the sort: two of 1024 threads on every compute unit.
+constexpr int kClearing = 512;
+
 // Where the scratch of the embedding's gradient lies in its workspace.
 struct EmbedScratch {
     size_t key[2], pos[2], counts, sums, total;
@@ -2530,17 +2533,26 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     }
     a.counts = reinterpret_cast<uint32_t*>(w + ws.counts);
     a.tile = ws.tile; a.tiles = ws.tiles; a.bits = ws.bits; a.passes = ws.passes;
+    // rows that no token names are cleared by workgroups beside the sort's (a sort of few tiles leaves most of the chip idle)
+    int clearing = 0;
+    a.clear = const_cast<void*>(at_elem(G, off, size));
+    if (!accumulate) {
+        a.clear_pieces = (int64_t)V * D * (int64_t)size / 16;
+        a.clear_rest = (int)((int64_t)V * D * (int64_t)size % 16);
+        clearing = (int)std::max<int64_t>(1, std::min<int64_t>(kClearing, a.clear_pieces / (ws.tiles > 1 ? 3 * a.passes : 1) / kScanBlock));
+    }
     hipError_t e = hipSuccess;
-    if (ws.tiles == 1) {
-        e = launch(p, kTokenSort, token_sort, 1u, kScanBlock, s, a);
+    if (ws.tiles <= 1) {
+        if (n > 0 || clearing > 0) e = launch(p, kTokenSort, token_sort, 1u + clearing, kScanBlock, s, a);
     } else {
-        for (int pass = 0; pass < a.passes && ws.tiles > 1 && e == hipSuccess; ++pass) {
-            e = launch(p, kTokenCount, token_count, (unsigned)ws.tiles, kScanBlock, s, a, pass);
-            if (e == hipSuccess) e = launch(p, kTokenScan, token_scan, 1u, kScanBlock, s, a.counts, (1 << a.bits) * ws.tiles);
-            if (e == hipSuccess) e = launch(p, kTokenMove, token_move, (unsigned)ws.tiles, kScanBlock, s, a, pass);
+        for (int pass = 0; pass < a.passes && e == hipSuccess; ++pass) {
+            e = launch(p, kTokenCount, token_count, (unsigned)(ws.tiles + clearing), kScanBlock, s, a, pass);
+            if (e == hipSuccess) e = launch(p, kTokenScan, token_scan, 1u + clearing, kScanBlock, s, a, pass);
+            if (e == hipSuccess) e = launch(p, kTokenMove, token_move, (unsigned)(ws.tiles + clearing), kScanBlock, s, a, pass);
         }
     }
     if (e != hipSuccess) return HSADMM_ERR_HIP;
+    if (n == 0) return HSADMM_OK;
     EmbedGradArgs g{};
     g.key = a.key[(a.passes - 1) & 1]; g.pos = a.pos[(a.passes - 1) & 1];
     g.n = (int32_t)n; g.V = V; g.part = ws.part;
@@ -2548,13 +2560,12 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     g.sums = reinterpret_cast<float*>(w + ws.sums); g.pitch = ws.pitch;
     g.G = const_cast<void*>(at_elem(G, off, size));
     g.scale = scale; g.add = accumulate != 0;
-    g.rows = 4;
-    while (g.rows < kGradRows && V / g.rows > 8192) g.rows *= 2;
     e = for_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
         hipError_t r = hipSuccess;
         if (n > ws.part) r = launch(p, kEmbedParts, embedding_parts<T>, (unsigned)ws.stretches, kBlock, s, g);
-        if (r == hipSuccess) r = launch(p, kEmbedGrad, embedding_gradient<T>, (unsigned)((V + g.rows - 1) / g.rows), kBlock, s, g);
+        if (r == hipSuccess) r = launch(p, kEmbedGrad, embedding_gradient<T>, (unsigned)((n + kWaves * kPlacesOfWave - 1) / (kWaves * kPlacesOfWave)), kBlock, s,
+                                        g);
         return r;
     });
     return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;

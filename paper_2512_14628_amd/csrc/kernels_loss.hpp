@@ -230,10 +230,10 @@ struct TileSource {
         }
         step = KMAJOR ? (int64_t)L::kK * o.ld * size : kTileK;
     }
-    // Load i of the tile that has `left` of k left, to its place in LDS.
-    __device__ __forceinline__ void load(int i, int turn, int64_t left, const unsigned char* zeros, char* lds, int64_t skip = 0) const
+    // Load i of the tile that lies `offset` bytes behind the first one and has `left` of k left, to its place in LDS.
+    __device__ __forceinline__ void load(int i, int64_t offset, int left, const unsigned char* zeros, char* lds) const
     {
-        const void* at = (KMAJOR ? k + i * (THREADS / L::kRow) : k) < left ? static_cast<const void*>(from[i] + turn * step + skip) : zeros;
+        const void* at = (KMAJOR ? k + i * (THREADS / L::kRow) : k) < left ? static_cast<const void*>(from[i] + offset) : zeros;
         load_to_lds(at, lds + (i * THREADS + (threadIdx.x & ~(kWave - 1))) * 16);
     }
 };
@@ -354,9 +354,11 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
         const int u = turn >= once && a.rest ? turn - once : turn;
         return BQ < 64 ? (u + begin < once ? u + begin : u + begin - once) : u;
     };
-    const auto skip = [&](int turn) { return turn >= once ? a.rest : 0; };
-    const auto left = [&](int turn) { return a.p.k - k_begin - (int64_t)turn * LP::kK; };
-    const auto left_q = [&](int turn) { return a.q.k - k_begin - (int64_t)turn * LP::kK; };
+    const int all_p = (int)(a.p.k - k_begin), all_q = (int)(a.q.k - k_begin);
+    const auto left_p = [&](int turn) { return all_p - at_turn(turn) * LP::kK; };
+    const auto left_q = [&](int turn) { return all_q - at_turn(turn) * LP::kK; };
+    const auto offset_p = [&](int turn) { return at_turn(turn) * from_p.step; };
+    const auto offset_q = [&](int turn) { return at_turn(turn) * from_q.step + (turn >= once ? a.rest : 0); };
     const auto place = [&](int u) { return lds + u * kPlace; };
     typename Wide<T>::vec fp[2][TP], fq[2][TQ];
     constexpr int kReads = TP + TQ, kProducts = TP * TQ;
@@ -380,10 +382,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
         const int turn = u / 2;
         if (u % 2 == 0)
 #pragma unroll
-            for (int i = 0; i < kLoadsP; ++i) from_p.load(i, at_turn(turn), left(at_turn(turn)), zeros, place(u));
+            for (int i = 0; i < kLoadsP; ++i) from_p.load(i, offset_p(turn), left_p(turn), zeros, place(u));
         else
 #pragma unroll
-            for (int i = 0; i < kLoadsQ; ++i) from_q.load(i, at_turn(turn), left_q(at_turn(turn)), zeros, place(u), skip(turn));
+            for (int i = 0; i < kLoadsQ; ++i) from_q.load(i, offset_q(turn), left_q(turn), zeros, place(u));
     }
     tile_barrier<kLoadsP + kLoadsQ>();
 #pragma unroll
@@ -393,6 +395,8 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     for (int turn = 0; turn < turns; ++turn) {
         const char* at_p = behind(0);
         const char* at_q = behind(1);
+        const int64_t to_p = offset_p(turn + 2), to_q = offset_q(turn + 2);
+        const int some_p = left_p(turn + 2), some_q = left_q(turn + 2);
 #pragma unroll
         for (int s = 0; s < kSteps - 1; ++s)
             step(s, [&](int n) {
@@ -402,7 +406,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                 if (s == 0)
 #pragma unroll
                     for (int i = 0; i < kLoadsP; ++i)
-                        if (due(n, i, kLoadsP)) from_p.load(i, at_turn(turn + 2), left(at_turn(turn + 2)), zeros, behind(4));
+                        if (due(n, i, kLoadsP)) from_p.load(i, to_p, some_p, zeros, behind(4));
             });
         tile_barrier<kLoadsP>();
         const char* next_p = behind(2);
@@ -413,7 +417,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                 if (due(n, r, kReads)) read(r, 0, next_p, next_q);
 #pragma unroll
             for (int i = 0; i < kLoadsQ; ++i)
-                if (due(n, i, kLoadsQ)) from_q.load(i, at_turn(turn + 2), left_q(at_turn(turn + 2)), zeros, behind(0), skip(turn + 2));
+                if (due(n, i, kLoadsQ)) from_q.load(i, to_q, some_q, zeros, behind(0));
         });
         unit = unit + 2 >= kPlaces ? unit + 2 - kPlaces : unit + 2;
     }

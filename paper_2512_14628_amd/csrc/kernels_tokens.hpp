@@ -40,6 +40,7 @@ __global__ __launch_bounds__(kBlock) void embedding_rows(const typename ElemOf<T
 // kDigitBits bits each.  Ids outside [0, V) become V and so come last.  A workgroup takes a tile of positions, a wave of it adjacent
 // ones, kSortAtOnce for each lane at a time (their loads are in flight together: one after the other, 32768 positions took 146 us);
 // lanes with equal digits find each other by ballots, so places depend on the ids alone.
+typedef float v4f_at2 __attribute__((ext_vector_type(4), aligned(2)));
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
 constexpr int kSortAtOnce = 8;
@@ -56,7 +57,24 @@ struct SortArgs {
     uint32_t* counts;           // [digit][tile], several tiles only
     int tile, tiles;
     int bits, passes;
+    // rows without a token become zero beside the sort: workgroups behind those that sort clear `clear_pieces` pieces of 16 bytes, and
+    // the last one the elements behind them
+    void* clear;
+    int64_t clear_pieces;
+    int clear_rest;             // bytes
 };
+
+// The `which`-th of `of` workgroups' share of the `turn`-th of `turns` parts of what is cleared.
+__device__ void clear_rows(const SortArgs& a, int turn, int turns, int which, int of)
+{
+    typedef v4f_at2 A;
+    const int64_t from = a.clear_pieces * turn / turns, to = a.clear_pieces * (turn + 1) / turns;
+    char* at = static_cast<char*>(a.clear);
+    for (int64_t i = from + (int64_t)which * kScanBlock + threadIdx.x; i < to; i += (int64_t)of * kScanBlock)
+        *reinterpret_cast<A*>(at + 16 * i) = A{0.f, 0.f, 0.f, 0.f};
+    if (turn == turns - 1 && which == 0 && (int)threadIdx.x * 2 < a.clear_rest)
+        reinterpret_cast<uint16_t*>(at + 16 * a.clear_pieces)[threadIdx.x] = 0;
+}
 
 // The lanes (of those that are active) with this lane's digit: for each bit those that agree in it.
 __device__ __forceinline__ unsigned long long same_digit(int digit, int bits, bool active)
@@ -185,10 +203,11 @@ __device__ void sort_places(SortShared& s, const uint32_t* start, int stride)
     __syncthreads();
 }
 
-// A single tile: all passes in one workgroup.
+// A single tile: all passes in one workgroup, the first.
 __global__ __launch_bounds__(kScanBlock) void token_sort(SortArgs a)
 {
     __shared__ SortShared s;
+    if (blockIdx.x > 0) return clear_rows(a, 0, 1, blockIdx.x - 1, gridDim.x - 1);
     for (int pass = 0; pass < a.passes; ++pass) {
         sort_count(a, pass, 0, s);
         sort_places(s, nullptr, 0);
@@ -200,6 +219,7 @@ __global__ __launch_bounds__(kScanBlock) void token_sort(SortArgs a)
 __global__ __launch_bounds__(kScanBlock) void token_count(SortArgs a, int pass)
 {
     __shared__ SortShared s;
+    if ((int)blockIdx.x >= a.tiles) return clear_rows(a, 3 * pass, 3 * a.passes, blockIdx.x - a.tiles, gridDim.x - a.tiles);
     sort_count(a, pass, blockIdx.x, s);
     for (int d = threadIdx.x; d < kDigits; d += kScanBlock) {
         uint32_t all = 0;
@@ -209,8 +229,11 @@ __global__ __launch_bounds__(kScanBlock) void token_count(SortArgs a, int pass)
 }
 
 // (a thread takes adjacent counts, all of them at once)
-__global__ __launch_bounds__(kScanBlock) void token_scan(uint32_t* __restrict__ counts, int n)
+__global__ __launch_bounds__(kScanBlock) void token_scan(SortArgs a, int pass)
 {
+    if (blockIdx.x > 0) return clear_rows(a, 3 * pass + 1, 3 * a.passes, blockIdx.x - 1, gridDim.x - 1);
+    uint32_t* counts = a.counts;
+    const int n = a.tiles << a.bits;
     constexpr int kMost = kDigits * kSortTiles / kScanBlock;
     __shared__ uint32_t sums[kScanWaves];
     const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
@@ -242,6 +265,7 @@ __global__ __launch_bounds__(kScanBlock) void token_scan(uint32_t* __restrict__ 
 __global__ __launch_bounds__(kScanBlock) void token_move(SortArgs a, int pass)
 {
     __shared__ SortShared s;
+    if ((int)blockIdx.x >= a.tiles) return clear_rows(a, 3 * pass + 2, 3 * a.passes, blockIdx.x - a.tiles, gridDim.x - a.tiles);
     sort_count(a, pass, blockIdx.x, s);
     sort_places(s, a.counts + blockIdx.x, a.tiles);
     sort_move(a, pass, blockIdx.x, s);
@@ -249,7 +273,8 @@ __global__ __launch_bounds__(kScanBlock) void token_move(SortArgs a, int pass)
 
 // ------------------------------------------------------------------ gradient of the embedding
 
-// dW[v] = scale times the sum of dY over v's tokens, in the order of their positions; in fp32, rounded once.  A token with more than
+// dW[v] = scale times the sum of dY over v's tokens, in the order of their positions; in fp32, rounded once.  (Rows without a token
+// are cleared beside the sort.)  A token with more than
 // `part` positions is summed in parts first, those of the sorted list's stretches of `part`: a stretch holds the end of at most one
 // such token and the beginning of at most one (or the whole stretch is one's), so it has two rows of sums: [2 b] for the token of its
 // first position, [2 b + 1] for another that begins in it.
@@ -266,21 +291,9 @@ struct EmbedGradArgs {
     void* G;
     float scale;
     int add;
-    int rows;           // of a workgroup of embedding_gradient
 };
 
-// First place of [lo, hi) in the sorted list whose token is at least v.
-__device__ __forceinline__ int lower_bound(const int32_t* __restrict__ key, int lo, int hi, int32_t v)
-{
-    while (lo < hi) {
-        const int mid = lo + (hi - lo) / 2;
-        if (key[mid] < v) lo = mid + 1;
-        else hi = mid;
-    }
-    return lo;
-}
-
-// The same by a whole wave, which looks at 64 places at a time.
+// First place in the sorted list whose token is at least v, by a whole wave: it looks at 64 places at a time.
 __device__ __forceinline__ int lower_bound_wave(const int32_t* __restrict__ key, int n, int32_t v)
 {
     const int lane = threadIdx.x & (kWave - 1);
@@ -296,24 +309,22 @@ __device__ __forceinline__ int lower_bound_wave(const int32_t* __restrict__ key,
     return lo;
 }
 
-// x += dY rows of the sorted places [from, to), K pieces of 16 bytes at the columns c[0 .. K); AT_ONCE rows in flight.  (The pieces
-// are whole and all of them are read, also by lanes that have none to write: with a branch every load is waited for where it stands.)
+// x += the rows of dY whose numbers are in lanes first to first + n - 1 of pos, K pieces of 16 bytes at the columns c[0 .. K); AT_ONCE
+// rows in flight.  (The pieces are whole and all of them are read, also by lanes that have none to write: with a branch every load
+// is waited for where it stands.)
 template <int T, int K, int AT_ONCE>
-__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int to, const int (&c)[K], float (&x)[K][Wide<T>::n])
+__device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int32_t pos, int first, int n, const int (&c)[K], float (&x)[K][Wide<T>::n])
 {
     typedef typename ElemOf<T>::type E;
-    typedef typename Wide<T>::vec V;
     const E* dY = static_cast<const E*>(a.dY);
-    const int lane = threadIdx.x & (kWave - 1);
-    const auto add = [&](auto count, int at, int32_t pos) {
+    const auto add = [&](auto count, int at) {
         constexpr int kCount = decltype(count)::value;
-        V y[kCount][K];
+        typename Wide<T>::vec y[kCount][K];
 #pragma unroll
         for (int u = 0; u < kCount; ++u) {
             const E* row = dY + (int64_t)__builtin_amdgcn_readlane(pos, at + u) * a.ld;
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                y[u][k] = *reinterpret_cast<const typename Wide<T>::any*>(row + c[k]);
+            for (int k = 0; k < K; ++k) y[u][k] = *reinterpret_cast<const typename Wide<T>::any*>(row + c[k]);
         }
 #pragma unroll
         for (int u = 0; u < kCount; ++u)
@@ -322,16 +333,13 @@ __device__ __forceinline__ void add_rows(const EmbedGradArgs& a, int from, int t
 #pragma unroll
                 for (int e = 0; e < Wide<T>::n; ++e) x[k][e] += (float)y[u][k][e];
     };
-    for (int t = from; t < to; t += kWave) {
-        const int n = min(kWave, to - t);
-        const int32_t pos = a.pos[t + min(lane, n - 1)];
-        int u = 0;
-        for (; u + AT_ONCE <= n; u += AT_ONCE) add(std::integral_constant<int, AT_ONCE>{}, u, pos);
-        if constexpr (AT_ONCE > 4)
-            for (; u + 4 <= n; u += 4) add(std::integral_constant<int, 4>{}, u, pos);
-        if (u + 2 <= n) { add(std::integral_constant<int, 2>{}, u, pos); u += 2; }
-        if (u < n) add(std::integral_constant<int, 1>{}, u, pos);
-    }
+    int u = first;
+    const int end = first + n;
+    for (; u + AT_ONCE <= end; u += AT_ONCE) add(std::integral_constant<int, AT_ONCE>{}, u);
+    if constexpr (AT_ONCE > 4)
+        for (; u + 4 <= end; u += 4) add(std::integral_constant<int, 4>{}, u);
+    if (u + 2 <= end) { add(std::integral_constant<int, 2>{}, u); u += 2; }
+    if (u < end) add(std::integral_constant<int, 1>{}, u);
 }
 
 // Sums over rows that are shorter than a piece: one column of the places [from, to).
@@ -351,9 +359,12 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
     constexpr int m = Wide<T>::n;
     __shared__ int bound[4];
     const int64_t b = blockIdx.x;
-    const int from = (int)(b * a.part), to = (int)min((int64_t)a.n, (b + 1) * a.part);
+    const int from = (int)(b * a.part), to = (int)min((int64_t)a.n, (b + 1) * a.part), wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
     // the extent of the tokens of the first and the last position
-    if (threadIdx.x < 4) bound[threadIdx.x] = lower_bound(a.key, 0, a.n, a.key[threadIdx.x < 2 ? from : to - 1] + (threadIdx.x & 1));
+    {
+        const int at = lower_bound_wave(a.key, a.n, a.key[wave < 2 ? from : to - 1] + (wave & 1));
+        if (lane == 0) bound[wave] = at;
+    }
     __syncthreads();
     const bool first = a.key[from] < a.V && bound[1] - bound[0] > a.part;
     const bool last = a.key[to - 1] < a.V && bound[3] - bound[2] > a.part && bound[2] != bound[0];
@@ -366,11 +377,14 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
             if ((int)threadIdx.x < a.cols) sums[threadIdx.x] = add_column<T>(a, f, t, threadIdx.x);
             continue;
         }
-        for (int c0 = threadIdx.x / kWave * kWave * m; c0 < a.cols; c0 += kBlock * m) {
-            const int at = c0 + (threadIdx.x & (kWave - 1)) * m;
+        for (int c0 = wave * kWave * m; c0 < a.cols; c0 += kBlock * m) {
+            const int at = c0 + lane * m;
             const int c[1] = {min(at, a.cols - m)};
             float x[1][m] = {};
-            add_rows<T, 1, 16>(a, f, t, c, x);
+            for (int i = f; i < t; i += kWave) {
+                const int n = min(kWave, t - i);
+                add_rows<T, 1, 16>(a, a.pos[i + min(lane, n - 1)], 0, n, c, x);
+            }
             if (at < a.cols)
 #pragma unroll
                 for (int e = 0; e < m; ++e) sums[c[0] + e] = x[0][e];
@@ -378,10 +392,10 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
     }
 }
 
-// The rows of dW: a workgroup takes `rows` adjacent ones, a wave one after the other; where their tokens lie in the list is found by
-// whole waves for all of them and then between those places for each.  A wave has kAcross pieces of 16 bytes a lane of one or a few
-// tokens' rows in flight at once.
-constexpr int kGradRows = 64;           // at most
+// The rows of dW that have tokens.  A wave takes kPlaces places of the sorted list and the tokens whose positions begin there; it has the
+// keys and positions of the 64 places from its first on in its lanes, so most tokens' rows are loaded as soon as those are there.
+// kAcross pieces of 16 bytes a lane of up to four rows are in flight at once.
+constexpr int kPlacesOfWave = 4;
 constexpr int kAcross = 2;
 
 template <int T>
@@ -391,38 +405,33 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
     typedef typename Wide<T>::vec V;
     typedef typename Wide<T>::any A;
     constexpr int m = Wide<T>::n;
-    __shared__ int ends[2], bound[kGradRows + 1];
-    const int64_t v0 = (int64_t)blockIdx.x * a.rows;
-    const int rows = (int)min((int64_t)a.rows, a.V - v0), wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
-    if (wave < 2) {
-        const int at = lower_bound_wave(a.key, a.n, (int32_t)v0 + (wave ? rows : 0));
-        if (lane == 0) ends[wave] = at;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x <= rows) bound[threadIdx.x] = lower_bound(a.key, ends[0], ends[1], (int32_t)v0 + threadIdx.x);
-    __syncthreads();
-    // rows without a token first: nothing waits for anything
-    if (!a.add)
-        for (int i = wave; i < rows; i += kWaves) {
-            if (bound[i] != bound[i + 1]) continue;
-            E* row = static_cast<E*>(a.G) + (v0 + i) * a.cols;
-            for (int c = lane * m; c < a.cols; c += kWave * m) store_piece<T>(row + c, V{}, a.cols - c);
-        }
-    for (int i = wave; i < rows; i += kWaves) {
-        const int64_t v = v0 + i;
-        const int from = __builtin_amdgcn_readfirstlane(bound[i]), to = __builtin_amdgcn_readfirstlane(bound[i + 1]);
-        if (from == to) continue;
-        E* row = static_cast<E*>(a.G) + v * a.cols;
+    const int lane = threadIdx.x & (kWave - 1);
+    const int64_t first = ((int64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * kPlacesOfWave;
+    if (first >= a.n) return;
+    const int64_t place = min(first + lane, (int64_t)a.n - 1);
+    const int32_t key = first + lane < a.n ? a.key[place] : a.V;       // (behind the last place: no token)
+    const int32_t pos = a.pos[place];
+    const int32_t ahead = first > 0 ? a.key[first - 1] : -1, up = __shfl_up(key, 1, kWave);
+    const int32_t before = lane == 0 ? ahead : up;
+    const unsigned long long ends = __ballot(key != before), begins = ends & __ballot(key < a.V);
+    for (int i = 0; i < kPlacesOfWave; ++i) {
+        if (!((begins >> i) & 1)) continue;
+        const int32_t v = __builtin_amdgcn_readlane(key, i);
+        const unsigned long long later = i < kWave - 1 ? ends >> (i + 1) : 0;
+        // how many positions the token has (all of them among the 64, or to be looked for)
+        const int from = (int)first + i;
+        const int n = later ? __ffsll((long long)later) : lower_bound_wave(a.key, a.n, v + 1) - from;
+        const bool many = n > a.part;
         // a token with many positions: its stretches, of which the first holds it as the second one if it begins inside
-        const bool many = to - from > a.part;
-        const int64_t b0 = from / a.part, b1 = (to - 1) / a.part;
-        const int64_t begins = b0 * a.part != from ? 1 : 0;
+        const int64_t b0 = from / a.part, b1 = (from + n - 1) / a.part;
+        const int64_t inside = b0 * a.part != from ? 1 : 0;
+        E* row = static_cast<E*>(a.G) + (int64_t)v * a.cols;
         if (a.cols < m) {
             if (lane < a.cols) {
                 float x = 0.f;
-                if (!many) x = add_column<T>(a, from, to, lane);
+                if (!many) x = add_column<T>(a, from, from + n, lane);
                 else
-                    for (int64_t b = b0; b <= b1; ++b) x += a.sums[(2 * b + (b == b0 ? begins : 0)) * a.pitch + lane];
+                    for (int64_t b = b0; b <= b1; ++b) x += a.sums[(2 * b + (b == b0 ? inside : 0)) * a.pitch + lane];
                 row[lane] = (E)(a.add ? x * a.scale + (float)row[lane] : x * a.scale);
             }
             continue;
@@ -440,18 +449,15 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
             }
             if (a.add)
 #pragma unroll
-                for (int k = 0; k < kAcross; ++k)
-                    g[k] = *reinterpret_cast<const A*>(row + c[k]);
-            if (!many) {
-                add_rows<T, kAcross, 4>(a, from, to, c, x);
-            } else {
-                constexpr int kAtOnce = 2;
+                for (int k = 0; k < kAcross; ++k) g[k] = *reinterpret_cast<const A*>(row + c[k]);
+            if (many) {
+                constexpr int kAtOnce = 4;
                 for (int64_t b = b0; b <= b1; b += kAtOnce) {
                     v4f y[kAtOnce][kAcross][m / 4];
 #pragma unroll
                     for (int u = 0; u < kAtOnce; ++u) {
                         const int64_t at = min(b + u, b1);
-                        const float* sums = a.sums + (2 * at + (at == b0 ? begins : 0)) * a.pitch;
+                        const float* sums = a.sums + (2 * at + (at == b0 ? inside : 0)) * a.pitch;
 #pragma unroll
                         for (int k = 0; k < kAcross; ++k)
 #pragma unroll
@@ -464,6 +470,13 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
                             for (int k = 0; k < kAcross; ++k)
 #pragma unroll
                                 for (int e = 0; e < m; ++e) x[k][e] += y[u][k][e / 4][e % 4];
+                }
+            } else if (i + n <= kWave) {
+                add_rows<T, kAcross, 4>(a, pos, i, n, c, x);
+            } else {
+                for (int t = 0; t < n; t += kWave) {
+                    const int some = min(kWave, n - t);
+                    add_rows<T, kAcross, 4>(a, a.pos[from + t + min(lane, some - 1)], 0, some, c, x);
                 }
             }
 #pragma unroll
