@@ -935,7 +935,7 @@ int hsadmm_expand_mx(const hsadmm_plan_t* plan, const uint8_t* const* codes, con
 /*
  * out[i] = scale W[id_i] (one rounding), and zeros where id_i is no token.
  *   out   device, n rows of D elements
- * n <= 2^30 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
+ * n <= 2^27 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, UNSUPPORTED, HIP.
  */
 int hsadmm_embedding(const hsadmm_plan_t* plan, int32_t layer, const void* W, int32_t type, const void* ids, int32_t index_bits,
                      int64_t n, float scale, void* out, int64_t out_stride, void* hip_stream);
@@ -946,7 +946,7 @@ int hsadmm_embedding(const hsadmm_plan_t* plan, int32_t layer, const void* W, in
  * to what G holds (and rows without a token are left alone): several batches, or a layer that is the first and the last at once,
  * whose other gradient hsadmm_softmax_loss has written.  dY of positions that are no token is not read.
  *   workspace   device, hsadmm_embedding_workspace bytes, 256-byte aligned; nothing is kept in it between calls
- * n <= 2^30 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
+ * n <= 2^27 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
  */
 int hsadmm_embedding_workspace(const hsadmm_plan_t* plan, int32_t layer, int64_t n, size_t* bytes);
 int hsadmm_embedding_gradient(const hsadmm_plan_t* plan, int32_t layer, const void* ids, int32_t index_bits, int64_t n, const void* dY,
@@ -962,7 +962,7 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* plan, int32_t layer, const vo
  * words the halves in ascending order belong to the elements 8 (i / 8) to 8 (i / 8) + 7.
  *   residual     in, optional, rows like X's
  *   Y            out; may be X, or the residual, with the same stride
- *   rows, width  either may be 0
+ *   rows, width  either may be 0; rows * width <= 2^46 (UNSUPPORTED beyond)
  *   p            0 <= p < 1
  *   seed, call   any numbers; `call` differs from call to call (a layer's number and a step's, say)
  *   call_device  in, optional, DEVICE, 8-byte aligned: takes the place of call, read when the kernel runs (captured graphs)
@@ -992,7 +992,7 @@ int hsadmm_dropout(const hsadmm_plan_t* plan, const void* X, int64_t x_stride, c
  *   G             out (in/out with `accumulate`), optional, gradient arena
  *   workspace     device, hsadmm_softmax_loss_workspace bytes, 256-byte aligned (`gradients`: whether dX or G is wanted); nothing is
  *                 kept in it between calls.  Calls that may overlap in time need one each
- * n <= 2^23 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
+ * n <= 2^21, V <= 2^30, and fewer than 2^32 threads for the tiles of a product (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
  */
 typedef struct {
     size_t struct_bytes;

@@ -367,6 +367,7 @@ class Plan:
         self.arena_elems, self.groups_total = a.value, g.value
         self.packed_capacity_elems, self.workspace_bytes = c.value, w.value
         self.state_blocks = hsadmm_plan_state_blocks(self)
+        self.device = torch.cuda.current_device()
         self.widths = [int(c) for c in table["c_in"]]          # (columns of the layers that have one row a token)
 
     def close(self):
@@ -986,6 +987,13 @@ def _count(ids, n: Optional[int]) -> int:
     return ids.numel()
 
 
+def _here(plan: Plan, *tensors) -> None:
+    """Tensors have to lie on the plan's device (which the library compares with the current one)."""
+    for x in tensors:
+        if x is not None and not isinstance(x, int) and x.get_device() != plan.device:
+            raise _Unfit("a tensor on %s, not on the plan's device" % x.device)
+
+
 def _rows(x, name: str, dtype, n: int, width: int):
     """Device address and stride of n rows of `width` elements: a tensor of two dimensions whose rows lie in one piece, at least
     their width apart.  An integer address (the caller's word) stands for rows without gaps."""
@@ -1001,10 +1009,11 @@ def _rows(x, name: str, dtype, n: int, width: int):
 def hsadmm_embedding(plan: Plan, layer: int, W, ids, out, *, scale: float = 1.0, type: int = TYPE_F32, index_bits: int = 32,
                      n: Optional[int] = None, stream=None, check: bool = True) -> int:
     """out[i] = scale W[ids[i]], rows of the layer in the arena W; zeros where ids[i] is no token.  `n` only with addresses in the
-    place of tensors.  Tensors of other types or shapes are refused (INVALID_ARGUMENT)."""
+    place of tensors.  Tensors of other types or shapes, or on another device, are refused (INVALID_ARGUMENT)."""
     dtype, width = _GRAD_DTYPES.get(type), _width(plan, layer)
     try:
         n = _count(ids, n)
+        _here(plan, W, ids, out)
         if dtype is None or index_bits not in _INDEX_DTYPES:               # (the library refuses these as such)
             at, ids_at, out_at, stride = _ptr(W), _ptr(ids), _ptr(out), width
         else:
@@ -1033,10 +1042,11 @@ def hsadmm_embedding_gradient(plan: Plan, layer: int, ids, dY, G, workspace, *, 
                               type: int = TYPE_F32, index_bits: int = 32, n: Optional[int] = None, stream=None,
                               workspace_bytes: Optional[int] = None, check: bool = True) -> int:
     """The layer's rows of the gradient arena G: the scaled sums of their tokens' rows of dY (added to what G holds with
-    `accumulate`).  Tensors of other types or shapes are refused (INVALID_ARGUMENT)."""
+    `accumulate`).  Tensors of other types or shapes, or on another device, are refused (INVALID_ARGUMENT)."""
     dtype, width = _GRAD_DTYPES.get(type), _width(plan, layer)
     try:
         n = _count(ids, n)
+        _here(plan, ids, dY, G, workspace)
         if dtype is None or index_bits not in _INDEX_DTYPES:
             at, ids_at, dy_at, stride = _ptr(G), _ptr(ids), _ptr(dY), width
         else:
@@ -1057,13 +1067,14 @@ def hsadmm_dropout(plan: Plan, X, Y, p: float, seed: int, call: int, *, residual
                    width: Optional[int] = None, call_device=None, stream=None, check: bool = True) -> int:
     """Y = X without a share p of its elements, the others scaled up, plus the residual.  Which ones follows from seed and call (or
     the 64-bit number at call_device, read when the kernel runs): the same call on Y's gradient is X's.  Tensors of two dimensions;
-    rows and width only with addresses in their place.  Tensors of other types or shapes are refused (INVALID_ARGUMENT)."""
+    rows and width only with addresses in their place.  Tensors of other types or shapes, or on another device, are refused (INVALID_ARGUMENT)."""
     dtype = _GRAD_DTYPES.get(type)
     try:
         if X is not None and not isinstance(X, int) and X.dim() == 2:
             rows, width = X.shape[0] if rows is None else rows, X.shape[1] if width is None else width
         if rows is None or width is None:
             raise _Unfit("X: two dimensions, or rows and width")
+        _here(plan, X, residual, Y, call_device)
         if dtype is None:
             at = [(_ptr(x) or 0, width) for x in (X, residual, Y)]
         else:
@@ -1093,11 +1104,12 @@ def hsadmm_softmax_loss(plan: Plan, layer: int, W, X, labels, *, workspace, loss
                         mean: bool = True, scale: float = 1.0, accumulate: bool = False, type: int = TYPE_F32, index_bits: int = 32,
                         n: Optional[int] = None, stream=None, workspace_bytes: Optional[int] = None, check: bool = True) -> int:
     """Softmax cross entropy of X times the layer's rows of the arena W against labels, and its gradients; outputs that are None are
-    not wanted.  The other arguments are the fields of hsadmm_softmax_loss_args_t.  Tensors of other types or shapes are refused
-    (INVALID_ARGUMENT)."""
+    not wanted.  The other arguments are the fields of hsadmm_softmax_loss_args_t.  Tensors of other types or shapes, or on
+    another device, are refused (INVALID_ARGUMENT)."""
     dtype, width = _GRAD_DTYPES.get(type), _width(plan, layer)
     try:
         n = _count(labels, n)
+        _here(plan, W, X, labels, workspace, loss, lse, total, dX, G)
         if dtype is None or index_bits not in _INDEX_DTYPES:
             arenas, (x_at, x_stride), (dx_at, dx_stride), labels_at = [_ptr(W), _ptr(G) or 0], (_ptr(X), width), (_ptr(dX) or 0, width), _ptr(labels)
         else:

@@ -2398,9 +2398,8 @@ static int table_layer(const hsadmm_plan_t* p, int32_t layer, int32_t* V, int32_
 static size_t type_size(int32_t type) { return type == HSADMM_TYPE_F32 ? 4 : 2; }
 static bool known_type(int32_t type) { return type >= HSADMM_TYPE_F32 && type <= HSADMM_TYPE_F16; }
 static size_t index_size(int32_t bits) { return bits == 64 ? 8 : 4; }
-// Rows of a call: their positions are held in 32 bits.
-constexpr int64_t kMostRows = 1ll << 30;
-constexpr int64_t kMostLossRows = 1ll << 23;
+// Tokens and rows of a call, and classes of a loss: positions are held in 32 bits, and a grid has fewer than 2^32 threads.
+constexpr int64_t kMostTokens = 1ll << 27, kMostLossRows = 1ll << 21, kMostClasses = 1ll << 30;
 // Bytes from the first element of `rows` rows to the last one.
 static size_t span_of(int64_t rows, int64_t ld, int64_t cols, size_t size)
 {
@@ -2427,7 +2426,7 @@ int hsadmm_embedding(const hsadmm_plan_t* p, int32_t layer, const void* W, int32
     int64_t off;
     if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
     if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
-    if (!known_type(type) || (index_bits != 32 && index_bits != 64) || n > kMostRows) return HSADMM_ERR_UNSUPPORTED;
+    if (!known_type(type) || (index_bits != 32 && index_bits != 64) || n > kMostTokens) return HSADMM_ERR_UNSUPPORTED;
     if (n < 0 || out_stride < D || out_stride > INT32_MAX) return HSADMM_ERR_INVALID_ARGUMENT;
     if (n == 0) return HSADMM_OK;
     const size_t size = type_size(type);
@@ -2442,8 +2441,7 @@ int hsadmm_embedding(const hsadmm_plan_t* p, int32_t layer, const void* W, int32
     const int pieces = (int)((D * size + 15) / 16);
     int lanes = 1;
     while (lanes < pieces && lanes < kBlock) lanes *= 2;
-    const int64_t grid = (n + kBlock / lanes - 1) / (kBlock / lanes);
-    if (grid > kGridMost) return HSADMM_ERR_UNSUPPORTED;
+    const int64_t grid = std::min<int64_t>((n + kBlock / lanes - 1) / (kBlock / lanes), 1 << 20);
     const hipError_t e = for_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
         typedef typename ElemOf<T>::type E;
@@ -2494,7 +2492,7 @@ int hsadmm_embedding_workspace(const hsadmm_plan_t* p, int32_t layer, int64_t n,
     int64_t off;
     if (!bytes || n < 0) return HSADMM_ERR_INVALID_ARGUMENT;
     if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
-    if (n > kMostRows) return HSADMM_ERR_UNSUPPORTED;
+    if (n > kMostTokens) return HSADMM_ERR_UNSUPPORTED;
     *bytes = embed_scratch(V, D, n).total;
     return HSADMM_OK;
 }
@@ -2507,7 +2505,7 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     int64_t off;
     if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
     if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
-    if (!known_type(type) || (index_bits != 32 && index_bits != 64) || n > kMostRows) return HSADMM_ERR_UNSUPPORTED;
+    if (!known_type(type) || (index_bits != 32 && index_bits != 64) || n > kMostTokens) return HSADMM_ERR_UNSUPPORTED;
     if (n < 0 || dy_stride < D || dy_stride > INT32_MAX) return HSADMM_ERR_INVALID_ARGUMENT;
     const size_t size = type_size(type);
     if (!G || !workspace || !is_aligned(G, type == HSADMM_TYPE_F32 ? 16 : 8) || !is_aligned(workspace, 256)) return HSADMM_ERR_INVALID_ARGUMENT;
@@ -2533,13 +2531,12 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     }
     a.counts = reinterpret_cast<uint32_t*>(w + ws.counts);
     a.tile = ws.tile; a.tiles = ws.tiles; a.bits = ws.bits; a.passes = ws.passes;
-    // rows that no token names are cleared by workgroups beside the sort's (a sort of few tiles leaves most of the chip idle)
+    // rows that no token names are cleared by workgroups beside the sort's
     int clearing = 0;
-    a.clear = const_cast<void*>(at_elem(G, off, size));
     if (!accumulate) {
-        a.clear_pieces = (int64_t)V * D * (int64_t)size / 16;
-        a.clear_rest = (int)((int64_t)V * D * (int64_t)size % 16);
-        clearing = (int)std::max<int64_t>(1, std::min<int64_t>(kClearing, a.clear_pieces / (ws.tiles > 1 ? 3 * a.passes : 1) / kScanBlock));
+        const int64_t bytes = (int64_t)V * D * (int64_t)size;
+        a.clear = Clear{static_cast<char*>(const_cast<void*>(at_elem(G, off, size))), bytes / 16, (int)(bytes % 16), ws.tiles > 1 ? 3 * a.passes : 1};
+        clearing = (int)std::max<int64_t>(1, std::min<int64_t>(kClearing, a.clear.pieces / a.clear.turns / kScanBlock));
     }
     hipError_t e = hipSuccess;
     if (ws.tiles <= 1) {
@@ -2577,8 +2574,9 @@ int hsadmm_dropout(const hsadmm_plan_t* p, const void* X, int64_t x_stride, cons
 {
     if (!p || rows < 0 || width < 0 || !(prob >= 0.0 && prob < 1.0)) return HSADMM_ERR_INVALID_ARGUMENT;
     if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
-    if (!known_type(type) || rows > (1ll << 40) || width > INT32_MAX) return HSADMM_ERR_UNSUPPORTED;
+    if (!known_type(type) || width > INT32_MAX) return HSADMM_ERR_UNSUPPORTED;
     if (rows == 0 || width == 0) return HSADMM_OK;
+    if (rows > (1ll << 46) / width) return HSADMM_ERR_UNSUPPORTED;
     const size_t size = type_size(type);
     if (!X || !Y || x_stride < width || y_stride < width || (residual && residual_stride < width) || x_stride > INT32_MAX ||
         y_stride > INT32_MAX || (residual && residual_stride > INT32_MAX) || !is_aligned(X, size) || !is_aligned(Y, size) ||
@@ -2662,7 +2660,15 @@ struct LossScratch {
     ProductPlan logits, inputs, weights;
     int slab_elems;
     int64_t slabs;
+    bool launches;              // the products' tiles fit their grids
 };
+
+// Whether a product's tiles fit one launch.
+static bool launches(const ProductPlan& how, int64_t out_p, int64_t out_q)
+{
+    const int64_t bp = how.b == kNarrow ? kNarrowTile : how.b, threads = how.b == 256 ? 512 : 256;
+    return ((out_p + bp - 1) / bp) * ((out_q + how.b - 1) / how.b) * how.splits + 8 < (1ll << 32) / threads;
+}
 
 static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int64_t off, int64_t n, int32_t type, bool gradients)
 {
@@ -2690,6 +2696,7 @@ static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int6
     s.weights = plan_product(D, std::min<int64_t>(V, s.Vc), n, sixteen, false, false);
     s.slab_elems = s.logits.b == kNarrow ? 32 : s.logits.b / 2;
     s.slabs = s.small ? 0 : (V + 255) / 256 * (256 / s.slab_elems);
+    s.launches = launches(s.logits, V, n) && launches(s.inputs, D, n) && launches(s.weights, D, std::min<int64_t>(V, s.Vc));
     size_t at = 0;
     const auto take = [&](int64_t bytes) { const size_t here = at; at = align_up(at + (size_t)bytes, 256); return here; };
     s.head = take(sizeof(LossHead));
@@ -2715,8 +2722,10 @@ int hsadmm_softmax_loss_workspace(const hsadmm_plan_t* p, int32_t layer, int64_t
     int64_t off;
     if (!bytes || n < 0) return HSADMM_ERR_INVALID_ARGUMENT;
     if (const int rc = table_layer(p, layer, &V, &D, &off); rc != HSADMM_OK) return rc;
-    if (!known_type(type) || n > kMostLossRows) return HSADMM_ERR_UNSUPPORTED;
-    *bytes = loss_scratch(p, V, D, off, n, type, gradients != 0).total;
+    if (!known_type(type) || n > kMostLossRows || V > kMostClasses) return HSADMM_ERR_UNSUPPORTED;
+    const LossScratch ws = loss_scratch(p, V, D, off, n, type, gradients != 0);
+    if (!ws.launches) return HSADMM_ERR_UNSUPPORTED;
+    *bytes = ws.total;
     return HSADMM_OK;
 }
 
@@ -2887,7 +2896,7 @@ int hsadmm_softmax_loss(const hsadmm_plan_t* p, const hsadmm_softmax_loss_args_t
     int64_t off;
     if (const int rc = table_layer(p, x->layer, &V, &D, &off); rc != HSADMM_OK) return rc;
     if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
-    if (!known_type(x->type) || x->reserved != 0 || (x->index_bits != 32 && x->index_bits != 64) || x->n > kMostLossRows) return HSADMM_ERR_UNSUPPORTED;
+    if (!known_type(x->type) || x->reserved != 0 || (x->index_bits != 32 && x->index_bits != 64) || x->n > kMostLossRows || V > kMostClasses) return HSADMM_ERR_UNSUPPORTED;
     const size_t size = type_size(x->type);
     if (x->n < 0 || !x->W || !is_aligned(x->W, 16) || !x->workspace || !is_aligned(x->workspace, 256) || !(std::fabs(x->scale) <= 3e38))
         return HSADMM_ERR_INVALID_ARGUMENT;
@@ -2900,6 +2909,7 @@ int hsadmm_softmax_loss(const hsadmm_plan_t* p, const hsadmm_softmax_loss_args_t
         return HSADMM_ERR_INVALID_ARGUMENT;
     if (!x->loss && !x->lse && !x->total && !x->dX && !x->G) return HSADMM_ERR_INVALID_ARGUMENT;
     const LossScratch ws = loss_scratch(p, V, D, off, x->n, x->type, x->dX || x->G);
+    if (!ws.launches) return HSADMM_ERR_UNSUPPORTED;
     if (x->workspace_bytes < ws.total) return HSADMM_ERR_WORKSPACE;
     Stretches used;
     const size_t rows = (size_t)x->n;

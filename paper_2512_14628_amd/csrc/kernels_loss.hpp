@@ -348,7 +348,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     constexpr int kLoadsP = from_p.kLoads, kLoadsQ = from_q.kLoads;
     const unsigned char* zeros = a.head->zeros;
     // Where a call streams its weights past a few rows (BQ = 32), workgroups begin at different turns: rows of a power of two of bytes
-    // that all workgroups read at the same column keep a few of the memory's channels busy.
+    // that all workgroups read at the same column keep a few of the memory's channels busy (one row x 2048 x 131072, bf16: 121 us, so 91).
     const int begin = BQ < 64 && once > 0 ? (int)(p0 / BP % once) : 0;
     const auto at_turn = [&](int turn) {
         const int u = turn >= once && a.rest ? turn - once : turn;

@@ -319,5 +319,5 @@ def test_refusals():
     assert code(dX=c.X) == -1 and code(G=c.W) == -1 and code(loss=c.loss[:6], lse=c.loss[:6]) == -1 and code(G=c.G[:-1]) == -1
     assert code(loss=c.loss[:5]) == -1 and code(total=c.total[:1]) == -1
     assert code(labels=c.labels.data_ptr()) == -1                                  # no n
-    assert code(labels=c.labels.data_ptr(), n=-1) == -1 and code(labels=8, X=16, dX=16, loss=4, n=2 ** 23 + 1) == -4
+    assert code(labels=c.labels.data_ptr(), n=-1) == -1 and code(labels=8, X=16, dX=16, loss=4, n=2 ** 21 + 1) == -4
     torch.cuda.synchronize()

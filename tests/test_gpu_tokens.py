@@ -297,7 +297,7 @@ def test_refusals():
     assert look(out=out[:, :19]) == -1 and look(out=out[:5]) == -1 and look(out=out.half()) == -1 and look(W=W[:-1]) == -1
     assert look(W=W.data_ptr() + 4) == -1 and look(ids=ids.data_ptr()) == -1 and look(ids=ids.data_ptr() + 2, n=2) == -1
     assert look(out=W[:120].view(6, 20)) == -1                        # written and read
-    assert look(ids=ids.data_ptr(), n=-1, out=out.data_ptr()) == -1 and look(ids=16, n=2 ** 30 + 1, out=16) == -4
+    assert look(ids=ids.data_ptr(), n=-1, out=out.data_ptr()) == -1 and look(ids=16, n=2 ** 27 + 1, out=16) == -4
 
     nbytes = pkg.hsadmm_embedding_workspace(plan, 1, 6)
     ws = torch.zeros(nbytes + 256, dtype=torch.uint8, device=DEV)
@@ -326,3 +326,91 @@ def test_refusals():
     empty = torch.zeros((0, 20), device=DEV)
     assert drop_(X=empty, Y=empty) == 0
     torch.cuda.synchronize()
+
+
+def test_tensors_elsewhere_are_refused():
+    plan = table(20, 30)
+    W, ids, out = torch.zeros(plan.arena_elems, device=DEV), torch.zeros(6, dtype=torch.int32, device=DEV), torch.zeros((6, 20), device=DEV)
+    ws = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+    cpu = lambda t: t.cpu()                                           # noqa: E731
+    assert pkg.hsadmm_embedding(plan, 1, cpu(W), ids, out, check=False) == -1
+    assert pkg.hsadmm_embedding(plan, 1, W, cpu(ids), out, check=False) == -1
+    assert pkg.hsadmm_embedding_gradient(plan, 1, ids, cpu(out), W, ws, check=False) == -1
+    assert pkg.hsadmm_embedding_gradient(plan, 1, ids, out, W, cpu(ws), check=False) == -1
+    assert pkg.hsadmm_dropout(plan, out, cpu(out), 0.5, 1, 1, check=False) == -1
+    loss = torch.zeros(6, device=DEV)
+    assert pkg.hsadmm_softmax_loss(plan, 1, W, out, ids, workspace=ws, loss=cpu(loss), check=False) == -1
+    with pytest.raises(pkg.HsadmmError, match="device"):
+        pkg.hsadmm_embedding(plan, 1, W, ids, cpu(out))
+
+
+@pytest.mark.parametrize("kind,n,D,V", [(F32, 5, 3, 9), (BF16, 300, 65, 400), (F16, 5000, 24, 3000)])
+def test_addresses_stand_for_rows_without_gaps(kind, n, D, V):
+    """Integer addresses in the place of tensors give what the tensors give."""
+    gen = torch.Generator().manual_seed(5)
+    plan, dtype = table(D, V), ref.TYPES[kind]
+    W = torch.randn(plan.arena_elems, generator=gen).to(dtype).to(DEV)
+    ids, x = tokens(n, V, gen, "common", 32), torch.randn((n, D), generator=gen).to(dtype).to(DEV)
+    ws = torch.zeros(max(pkg.hsadmm_embedding_workspace(plan, 1, n), pkg.hsadmm_softmax_loss_workspace(plan, 1, n, kind)), dtype=torch.uint8, device=DEV)
+    both = []
+    for at in (lambda t: t, lambda t: t.data_ptr()):
+        y, G, dX, total = torch.zeros_like(x), torch.zeros_like(W), torch.zeros_like(x), torch.zeros(2, device=DEV)
+        pkg.hsadmm_embedding(plan, 1, at(W), at(ids), at(y), type=kind, n=n)
+        pkg.hsadmm_softmax_loss(plan, 1, at(W), at(x), at(ids), workspace=at(ws), workspace_bytes=ws.numel(), total=at(total), dX=at(dX), G=at(G),
+                                type=kind, n=n)
+        pkg.hsadmm_embedding_gradient(plan, 1, at(ids), at(x), at(G), at(ws), workspace_bytes=ws.numel(), type=kind, n=n, accumulate=True)
+        z = torch.zeros_like(x)
+        pkg.hsadmm_dropout(plan, at(x), at(z), 0.5, 1, 2, type=kind, rows=n, width=D, residual=at(y))
+        torch.cuda.synchronize()
+        both.append((y, G, dX, total, z))
+    for a, b in zip(*both):
+        assert torch.equal(a, b)
+
+
+def test_the_largest_offsets():
+    """A layer that begins behind 2^31 elements of its arena, rows whose offsets pass 32 bits in bytes and in elements."""
+    D, V, off = 2048, 3, 2 ** 31 + 8
+    plan = pkg.Plan({"elem_off": [0, off], "c_out": [1, V], "c_in": [8, D], "khw": [1, 1], "mode": [0, 0], "k": [1, V]})
+    gen = torch.Generator().manual_seed(6)
+    W = torch.zeros(plan.arena_elems, dtype=torch.bfloat16, device=DEV)
+    w = W[off:].view(V, D)
+    w.copy_(torch.randn((V, D), generator=gen).to(torch.bfloat16))
+    n, pad = 1100, 2 ** 21 - D                                # (n rows of 2^21 elements: 2.3 G elements)
+    big = torch.zeros((n, D + pad), dtype=torch.bfloat16, device=DEV)
+    ids = torch.randint(0, V, (n,), generator=gen, dtype=torch.int32).to(DEV)
+    pkg.hsadmm_embedding(plan, 1, W, ids, big[:, :D], type=BF16)
+    ref.close(big[:, :D], *ref.embedding_reference(BF16, w, ids.long(), 1.0), "rows far apart")
+    near = big[:, :D].contiguous()
+    G = torch.zeros_like(W)
+    ws = torch.zeros(max(pkg.hsadmm_embedding_workspace(plan, 1, n), pkg.hsadmm_softmax_loss_workspace(plan, 1, n, BF16)), dtype=torch.uint8, device=DEV)
+    g = G[off:].view(V, D)
+    for rows_ in (big[:, :D], near):
+        pkg.hsadmm_embedding_gradient(plan, 1, ids, rows_, G, ws, type=BF16)
+        value, bound = ref.embedding_gradient_reference(V, near, ids.long(), 1.0)
+        ref.close(g, value, ref.rounded(BF16, value, bound), "G")
+    totals = [torch.zeros(2, device=DEV) for _ in range(2)]
+    outs = []
+    # (a row of W against itself has a logit of about 2048, so its own label a softmax of 1 and no gradient at all: the next one)
+    labels = (ids + 1) % V
+    for rows_, total in zip((big[:, :D], near), totals):
+        pkg.hsadmm_softmax_loss(plan, 1, W, rows_, labels, workspace=ws, total=total, G=G, type=BF16)
+        outs.append(g.clone())
+    assert torch.equal(*totals) and torch.equal(*outs) and outs[0].abs().max() > 0
+    y = torch.zeros_like(near)
+    pkg.hsadmm_dropout(plan, big[:, :D], y, 0.5, 3, 4, type=BF16)
+    z = torch.zeros_like(near)
+    pkg.hsadmm_dropout(plan, near, z, 0.5, 3, 4, type=BF16)
+    assert torch.equal(y, z)
+
+
+def test_dropout_beyond_two_to_the_thirty_two_elements():
+    """The element's number is counted in 64 bits: its last groups against the generator."""
+    n = 2 ** 32 + 1000
+    plan, x = table(4, 4), torch.ones((1, n), dtype=torch.float16, device=DEV)
+    if n > 2 ** 31:                                           # (a row is at most 2^31 - 1 wide: as rows of a power of two)
+        x = x[:, :2 ** 32].view(2 ** 12, 2 ** 20)
+    y = x
+    drop(plan, F16, x, y, 0.5, 21, 22)
+    last = y.view(-1)[-5003:]
+    kept, factor = ref.dropout_kept(5003, 0.5, 21, 22, first=y.numel() - 5003)
+    assert torch.equal(last.cpu(), torch.from_numpy(kept * factor).half())
