@@ -310,11 +310,15 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     constexpr int kPlaces = 5, kPlace = LP::kBytes > LQ::kBytes ? LP::kBytes : LQ::kBytes;
     __shared__ __align__(16) char lds[kPlaces * kPlace];
 
-    // Workgroups go round the eight dies; a die takes adjacent tiles, 8 of q by as many p, so its cache holds what they share.
+    // Workgroups go round the eight dies; a die takes adjacent tiles, 8 of q by as many p, so its cache holds what they share.  Tiles of
+    // rows that have no target are none of them.
+    const int count = a.head->count;
+    if (WHAT != kWeightGrads) a.tiles_q = min(a.tiles_q, (count + BQ - 1) / BQ);
     const int64_t tiles = (int64_t)a.tiles_p * a.tiles_q;
     int64_t t = blockIdx.x;
     {
         const int64_t all = tiles * a.splits, each = (all + 7) / 8, die = t % 8;
+        if (t / 8 >= each) return;
         t = die * each + t / 8;
         if (t >= all) return;
     }
@@ -326,8 +330,6 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     t -= band * kBand * a.tiles_p;
     const int64_t q0 = (band * kBand + t % in_band) * BQ, p0 = t / in_band * BP;
 
-    const int count = a.head->count;
-    if (WHAT != kWeightGrads && q0 >= count) return;
     // (rows behind the last one with a target hold anything: as rows of the output nobody reads them, along k they are left out)
     if (WHAT == kWeightGrads) a.p.k = a.q.k = count;
     int64_t k_end = a.p.k;
