@@ -24,7 +24,9 @@
  * hsadmm_stopping_test (host) is the break test of Algorithm 1's Phase 5.
  * Around the outer iteration: hsadmm_gradient_norms and hsadmm_adamw train the replicas between two steps (Phase 1, Eq. (7)
  * with AdamW; optimizer states in 32 or 8 bits), and hsadmm_compact_mx / hsadmm_expand_mx write the packed buffer in 8 or 4
- * bits a value and read the nodes' buffers back.
+ * bits a value and read the nodes' buffers back.  Of a model that learns language, hsadmm_embedding and hsadmm_embedding_gradient,
+ * hsadmm_dropout and hsadmm_softmax_loss are the two ends: tokens to activations, the last layer's products to a loss, and the
+ * gradients of both that hsadmm_adamw takes.
  *
  * Data layout.  A layer is the row-major fp32 array W[c_out][c_in][khw]
  * (Section 2, first paragraph; khw = K_H*K_W, 1 for linear layers).  A

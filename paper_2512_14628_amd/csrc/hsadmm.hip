@@ -46,7 +46,12 @@
 //   gather_mx / scatter_mx   compact_gather into, and expand_scatter out of, blocks of 32 codes with a shared power of two; the second
 //                   takes the mean of several nodes' buffers and the dual update of Eq. (13) with it
 //
-// Nothing here is a dense contraction, so no MFMA is used; every kernel is bound by HBM traffic.
+//   embedding_rows, token_sort / token_count / token_scan / token_move, embedding_parts / embedding_gradient, dropout_kernel   the
+//                   tokens' way into a language model, and back (hsadmm_embedding, hsadmm_embedding_gradient, hsadmm_dropout)
+//   loss_targets / loss_rows / loss_product / loss_softmax / loss_total / loss_inputs   softmax cross entropy of a layer's products and
+//                   its gradients (hsadmm_softmax_loss)
+//
+// loss_product is the one dense contraction: tiles on the matrix units.  Every other kernel is bound by HBM traffic.
 // Arena data is touched once per kernel, so it is moved with non-temporal 128-bit accesses.
 // fp32 arithmetic is compiled without contraction (-ffp-contract=off); the fp64 accumulation
 // uses fma(v, v, acc), which equals mul+add because the square of an fp32 value is exact in fp64.
@@ -2385,7 +2390,7 @@ const char* hsadmm_kernel_name(int kernel_id)
 
 // ------------------------------------------------------------------ a language model's ends
 
-// The layer as a table of V rows of D elements, and where it starts in an arena; false: no such layer, or one with positions.
+// The layer as a table of V rows of D elements, and where it starts in an arena.
 static int table_layer(const hsadmm_plan_t* p, int32_t layer, int32_t* V, int32_t* D, int64_t* off)
 {
     if (!p || layer < 0 || layer >= (int32_t)p->layers.size()) return HSADMM_ERR_INVALID_ARGUMENT;
@@ -2582,6 +2587,7 @@ int hsadmm_dropout(const hsadmm_plan_t* p, const void* X, int64_t x_stride, cons
         y_stride > INT32_MAX || (residual && residual_stride > INT32_MAX) || !is_aligned(X, size) || !is_aligned(Y, size) ||
         (residual && !is_aligned(residual, size)) || (call_device && !is_aligned(call_device, 8)))
         return HSADMM_ERR_INVALID_ARGUMENT;
+    if (rows > (1ll << 60) / std::max({x_stride, y_stride, residual ? residual_stride : 0})) return HSADMM_ERR_UNSUPPORTED;
     DropoutArgs a{};
     // (65536 p to the nearest whole number, 65535 at most)
     a.least = (uint32_t)std::min(65535.0, std::floor(prob * 65536.0 + 0.5));
@@ -2619,8 +2625,12 @@ struct ProductPlan {
     bool fills;          // tiles enough for the chip without parts
 };
 
-// The largest tile that has a workgroup for each of the chip's 256 compute units (tiles of 256: 16-bit types only); with parts
-// allowed, parts of `least` of k count too, and their number is the one that leaves the fewest compute units idle in the last round.
+// The largest tile that has a workgroup for each of the chip's 256 compute units (tiles of 256: 16-bit types only); where parts are
+// allowed, parts of four tiles' lengths of k count too, and their number is the one that leaves the fewest places on the chip idle in
+// the last round (a hundredth off for each: their sums are written and read).  Up to 32 rows the tile is 128 x 32.  us:
+//   tiles of 128 / 256: inputs' gradients of 3690 x 2048 x 32768, bf16 799 / 652 (256 in two parts)
+//   tiles of 64 / 128, fp32 256 x 2048 x 1000: logits 14.5 (8 parts; 4: 15.8, 1: 49) / 16.6 (16 parts; 8: 23), weights' gradients 14.3 / 23.8
+//   tiles of 128 x 32 / 128 x 128, bf16 x 2048 x 131072: one row 92 / 102, 32 rows 99 / 115, 33 rows 147 / 116
 static ProductPlan plan_product(int64_t out_p, int64_t out_q, int64_t k, bool sixteen, bool narrow, bool parts)
 {
     constexpr int64_t kUnits = 256;
@@ -2684,8 +2694,9 @@ static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int6
     s.pieces = (int)((V + s.Vc - 1) / s.Vc);
     s.logits = plan_product(V, n, s.Dp, sixteen, narrow, false);
     // Rounding the gradients of the logits to 16 bits is lost among the terms of a long sum.  In a short one (a vocabulary of a few
-    // classes for the inputs' gradient, a few rows for the weights') it would add half as much again to the rounding of the output:
-    // there what is left of the rounding is multiplied too, twice the time of a product that is short.
+    // classes for the inputs' gradient, a few rows for the weights') it would add half as much again to the rounding of the output
+    // (fp16, relative to 64 bits: 0.00031 for 0.00021): there what is left of the rounding is multiplied too, twice the time of a
+    // product that is short (0.00022).
     const bool fits = s.pieces == 1 && 4 * s.Np * s.Vc <= p->loss_held;
     s.rest_inputs = gradients && sixteen && fits && V <= kFewTerms;
     s.rest_weights = gradients && sixteen && fits && n <= kFewTerms;
@@ -2842,7 +2853,7 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
         if (e == hipSuccess) e = launch(p, kLossSoftmax, loss_softmax<T>, (unsigned)n, threads, s, m);
     }
     if (e == hipSuccess && x->total)
-        e = launch(p, kLossTotal, loss_total, 1u, kBlock, s, (const LossHead*)r.head, (const float*)held_loss, (int)(x->mean != 0), x->total);
+        e = launch(p, kLossTotal, loss_total, 1u, kScanBlock, s, (const LossHead*)r.head, (const float*)held_loss, (int)(x->mean != 0), x->total);
     if (!gradients) return e;
     for (int i = ws.pieces - 1; i >= 0 && e == hipSuccess; --i) {
         const int32_t v0 = (int32_t)(i * ws.Vc);

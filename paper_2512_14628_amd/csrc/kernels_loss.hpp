@@ -74,33 +74,46 @@ struct LossRows {
     int32_t* place;      // [N] the held row of an original one, or -1
 };
 
-// Lists the rows whose label lies in [0, V), in order (one workgroup), and settles the rows that have none.
+// Lists the rows whose label lies in [0, V), in order (one workgroup, four labels a thread at a time), and settles the rows that have
+// none.  Bound by the loads' latency: 8192 labels in 7.6 us (10.5 with one label a thread at a time).
 __global__ __launch_bounds__(kScanBlock) void loss_targets(const void* __restrict__ labels, int wide, int64_t n, int32_t V, double scale,
                                                            int mean, LossRows r, float* __restrict__ loss, float* __restrict__ lse)
 {
-    __shared__ int32_t sums[2][kScanWaves];
+    constexpr int kAtOnce = 4;
+    __shared__ int32_t sums[2][kAtOnce][kScanWaves];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     int32_t before = 0;
     int turn = 0;
-    for (int64_t i0 = 0; i0 < n; i0 += kScanBlock, turn ^= 1) {
-        const int64_t i = i0 + threadIdx.x;
-        const int64_t y = i < n ? index_at(labels, wide != 0, i) : -1;
-        const bool has = y >= 0 && y < V;
-        const unsigned long long all = __ballot(has);
-        if (lane == 0) sums[turn][wave] = __popcll(all);
-        __syncthreads();
-        int32_t at = before;
-        for (int w = 0; w < kScanWaves; ++w) {
-            const int32_t s = sums[turn][w];
-            before += s;
-            if (w < wave) at += s;
+    for (int64_t i0 = 0; i0 < n; i0 += kAtOnce * kScanBlock, turn ^= 1) {
+        int64_t y[kAtOnce];
+        unsigned long long all[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            const int64_t i = i0 + u * kScanBlock + threadIdx.x;
+            y[u] = i < n ? index_at(labels, wide != 0, i) : -1;
         }
-        at += __popcll(all & ((1ull << lane) - 1));
-        if (i < n) {
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            all[u] = __ballot(y[u] >= 0 && y[u] < V);
+            if (lane == 0) sums[turn][u][wave] = __popcll(all[u]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) {
+            int32_t at = before;
+            for (int w = 0; w < kScanWaves; ++w) {
+                const int32_t s = sums[turn][u][w];
+                before += s;
+                if (w < wave) at += s;
+            }
+            at += __popcll(all[u] & ((1ull << lane) - 1));
+            const int64_t i = i0 + u * kScanBlock + threadIdx.x;
+            if (i >= n) continue;
+            const bool has = (all[u] >> lane) & 1;
             r.place[i] = has ? at : -1;
             if (has) {
                 r.row[at] = (int32_t)i;
-                r.label[at] = (int32_t)y;
+                r.label[at] = (int32_t)y[u];
             } else {
                 if (loss) loss[i] = 0.f;
                 if (lse) lse[i] = 0.f;
@@ -299,7 +312,13 @@ __device__ __forceinline__ v16f multiply(typename Wide<T>::vec a, typename Wide<
 // q = l % 32 and 16 of the p.  A turn is a tile of k, four steps of the matrix units; while a step is multiplied the next one's operands
 // are read from LDS.  LDS has five places for operands' tiles, taken in the order p, q, p, q, ...: two are read, three are on
 // their way.  One barrier a turn, before its last step: the next turn's tiles have arrived, and this turn's are read, so their
-// places take the q of the turn after the next and the p of the one behind that.
+// places take the q of the turn after the next and the p of the one behind that.  Loads and LDS reads stand between the products.
+//
+// Bound by the matrix units at the clock that their power leaves (1.7 GHz, busy 70 % of the cycles): 8192 x 4096 x 32768 in bf16,
+// logits 1205 TFLOP/s, inputs' gradients 1230, weights' 1190 (a library's plain products of these sizes 1353, 1250, 1115).  Two whole
+// turns in LDS, each loaded in one go at its predecessor's beginning: 889, 896, 902; the same without loads 1248, 1596, 1439, without
+// products 1019, 1421, 1407, so the two hardly overlapped.  Four waves of 128 x 128 instead of eight of 128 x 64: 963, 1175, 1132.
+// In fp32, 256 x 2048 x 1000 (tiles of 64, four to eight parts): 14.5 us each, 72 TFLOP/s.
 template <int T, int BP, int BQ, int WP, int WQ, bool PMAJOR, bool QMAJOR, int WHAT>
 __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
 {
@@ -349,12 +368,13 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     const TileSource<T, BQ, QMAJOR, kThreads> from_q(a.q, q0, k_begin);
     constexpr int kLoadsP = from_p.kLoads, kLoadsQ = from_q.kLoads;
     const unsigned char* zeros = a.head->zeros;
-    // Where a call streams its weights past a few rows (BQ = 32), workgroups begin at different turns: rows of a power of two of bytes
-    // that all workgroups read at the same column keep a few of the memory's channels busy (one row x 2048 x 131072, bf16: 121 us, so 91).
-    const int begin = BQ < 64 && once > 0 ? (int)(p0 / BP % once) : 0;
+    // Where one tile of rows sees all weights, which are then read once, workgroups begin at different turns: rows of a power of two of
+    // bytes that all workgroups read at the same column keep a few of the memory's channels busy (one row x 2048 x 131072, bf16:
+    // 121 us, so 92, 5.8 TB/s).
+    const int begin = WHAT != kWeightGrads && a.tiles_q == 1 && once > 0 ? (int)(p0 / BP % once) : 0;
     const auto at_turn = [&](int turn) {
-        const int u = turn >= once && a.rest ? turn - once : turn;
-        return BQ < 64 ? (u + begin < once ? u + begin : u + begin - once) : u;
+        const int u = (turn >= once && a.rest ? turn - once : turn) + begin;
+        return u < once || begin == 0 ? u : u - once;
     };
     const int all_p = (int)(a.p.k - k_begin), all_q = (int)(a.q.k - k_begin);
     const auto left_p = [&](int turn) { return all_p - at_turn(turn) * LP::kK; };
@@ -696,18 +716,25 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
 }
 
 // The sum (mean) of the losses, in fp64 and in an order that depends on their number alone, and how many there are.
-__global__ __launch_bounds__(kBlock) void loss_total(const LossHead* __restrict__ head, const float* __restrict__ held, int mean,
-                                                     float* __restrict__ total)
+__global__ __launch_bounds__(kScanBlock) void loss_total(const LossHead* __restrict__ head, const float* __restrict__ held, int mean,
+                                                         float* __restrict__ total)
 {
-    __shared__ double red[kWaves];
+    __shared__ double red[kScanWaves];
+    constexpr int kAtOnce = 4;
     const int count = head->count;
     double s = 0.0;
-    for (int i = threadIdx.x; i < count; i += kBlock) s += (double)held[i];
+    for (int i0 = threadIdx.x; i0 < count; i0 += kAtOnce * kScanBlock) {
+        float x[kAtOnce];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) x[u] = held[min(i0 + u * kScanBlock, count - 1)];
+#pragma unroll
+        for (int u = 0; u < kAtOnce; ++u) s += i0 + u * kScanBlock < count ? (double)x[u] : 0.0;
+    }
     s = wave_xor_sum(s, kWave);
     if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kWaves; ++w) s += red[w];
+        for (int w = 1; w < kScanWaves; ++w) s += red[w];
         total[0] = (float)(mean ? s / (double)max(count, 1) : s);
         total[1] = (float)count;
     }

@@ -10,7 +10,8 @@ namespace {
 
 // ------------------------------------------------------------------ embedding
 
-// out[i] = scale W[id_i], zeros for an id outside [0, V).  `lanes` threads (a power of two) share a row.
+// out[i] = scale W[id_i], zeros for an id outside [0, V).  `lanes` threads (a power of two) share a row.  Bound by HBM: 32768 tokens x
+// 2048, bf16, 262 MB in 50 us (5.3 TB/s; tokens that are named often come from the caches).
 template <int T>
 __global__ __launch_bounds__(kBlock) void embedding_rows(const typename ElemOf<T>::type* __restrict__ W, int32_t V, int cols,
                                                          const void* __restrict__ ids, int wide, int64_t n, float scale,
@@ -398,9 +399,11 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
     }
 }
 
-// The rows of dW that have tokens.  A wave takes kPlaces places of the sorted list and the tokens whose positions begin there; it has the
-// keys and positions of the 64 places from its first on in its lanes, so most tokens' rows are loaded as soon as those are there.
-// kAcross pieces of 16 bytes a lane of up to four rows are in flight at once.
+// The rows of dW that have tokens.  A wave takes kPlacesOfWave places of the sorted list and the tokens whose positions begin there; it
+// has the keys and positions of the 64 places from its first on in its lanes, so most tokens' rows are loaded as soon as those are
+// there.  kAcross pieces of 16 bytes a lane of up to four rows are in flight at once.  Bound by latency (keys, first rows, and the
+// stretches' sums of a token of many positions, one after the other): 32768 positions x 2048 in bf16, 134 MB read and 45 written, in
+// 54 us, behind 26 for the stretches.  Eight places a wave 63; rows of four pieces at once take registers that cost a wave, 70.
 constexpr int kPlacesOfWave = 4;
 constexpr int kAcross = 2;
 
@@ -526,6 +529,8 @@ __device__ __forceinline__ void philox(uint64_t group, uint64_t call, uint64_t s
     w[0] = c0; w[1] = c1; w[2] = c2; w[3] = c3;
 }
 
+// A thread has a group of eight elements, one counter's numbers.  Bound by HBM: 16384 x 4096 in bf16 with a residual, 403 MB in 68 us
+// (5.9 TB/s).
 struct DropoutArgs {
     const void* X;
     const void* R;              // residual, or null
