@@ -2625,23 +2625,28 @@ struct ProductPlan {
     bool fills;          // tiles enough for the chip without parts
 };
 
-// The largest tile that has a workgroup for each of the chip's 256 compute units (tiles of 256: 16-bit types only); where parts are
-// allowed, parts of four tiles' lengths of k count too, and their number is the one that leaves the fewest places on the chip idle in
-// the last round (a hundredth off for each: their sums are written and read).  Up to 32 rows the tile is 128 x 32.  us:
-//   tiles of 128 / 256: inputs' gradients of 3690 x 2048 x 32768, bf16 799 / 652 (256 in two parts)
-//   tiles of 64 / 128, fp32 256 x 2048 x 1000: logits 14.5 (8 parts; 4: 15.8, 1: 49) / 16.6 (16 parts; 8: 23), weights' gradients 14.3 / 23.8
-//   tiles of 128 x 32 / 128 x 128, bf16 x 2048 x 131072: one row 92 / 102, 32 rows 99 / 115, 33 rows 147 / 116
+// The largest tile that has a workgroup for each of the chip's 256 compute units: 256 (16-bit types only; where parts of the k axis are
+// allowed they count too), 128, 64.  Fewer tiles of 64 than that: parts, of tiles of 128 in 16 bits if those then fill the chip.  The
+// number of parts is the one that leaves the fewest places on the chip idle in the last round (a hundredth off for each: their sums
+// are written and read); parts of tiles of 64 that fill the chip are none.  Up to 32 rows the tile is 128 x 32.  us (parts):
+//   tiles of 128 / 256   inputs' gradients of 3690 x 2048 x 32768, bf16 799 / 652 (2)
+//   tiles of 64 / 128    rows x 1568 x 3479, 560 rows: bf16 18.9 (1), 20.7 (2) / 23.6 (1), 22.4 (2); fp32 67 (1) / 108 (1), 81 (3)
+//                        256 x 16384 x 2048, bf16 97.8 (1), 32.4 (8) / 30.3 (8), 28.0 (16); 256 x 2048 x 1000, fp32 14.5 (8), 49 (1) / 16.6 (16)
+//   128 x 32 / 128 x 128 x 2048 x 131072, bf16: one row 92 / 102, 32 rows 99 / 115, 33 rows 147 / 116
 static ProductPlan plan_product(int64_t out_p, int64_t out_q, int64_t k, bool sixteen, bool narrow, bool parts)
 {
     constexpr int64_t kUnits = 256;
     const auto tiles = [&](int64_t b) { return narrow ? (out_p + kNarrowTile - 1) / kNarrowTile : ((out_p + b - 1) / b) * ((out_q + b - 1) / b); };
     const auto most_parts = [&](int64_t b) { return parts ? std::max<int64_t>(1, k / (4 * b)) : 1; };
     ProductPlan r{};
-    r.b = narrow ? kNarrow : sixteen && tiles(256) * most_parts(256) >= kUnits ? 256 : tiles(128) * most_parts(128) >= kUnits ? 128 : 64;
+    r.b = narrow ? kNarrow
+        : sixteen && tiles(256) * most_parts(256) >= kUnits ? 256
+        : tiles(128) >= kUnits ? 128
+        : sixteen && tiles(64) < kUnits && tiles(128) * most_parts(128) >= kUnits ? 128 : 64;
     const int64_t n = tiles(r.b);
     r.fills = n >= kUnits;
     r.splits = 1;
-    if (parts && k > 0) {
+    if (parts && k > 0 && !(r.b == 64 && r.fills)) {
         const int64_t at_once = kUnits * (r.b == 256 ? 1 : r.b == 128 || !sixteen ? 2 : 4);        // workgroups that share the chip
         const int64_t most = std::min<int64_t>({r.b >= 128 ? most_parts(r.b) : std::max<int64_t>(1, k / 128), std::max<int64_t>(1, 2 * at_once / n), 64});
         double best = 0.0;
@@ -2700,7 +2705,8 @@ static LossScratch loss_scratch(const hsadmm_plan* p, int32_t V, int32_t D, int6
     const bool fits = s.pieces == 1 && 4 * s.Np * s.Vc <= p->loss_held;
     s.rest_inputs = gradients && sixteen && fits && V <= kFewTerms;
     s.rest_weights = gradients && sixteen && fits && n <= kFewTerms;
-    s.small = (!s.logits.fills && s.pieces == 1) || s.rest_inputs || s.rest_weights;
+    // (tiles of 64 are for so few logits that they are joined by rows as well)
+    s.small = (s.pieces == 1 && (!s.logits.fills || s.logits.b == 64)) || s.rest_inputs || s.rest_weights;
     if (s.small) s.logits = plan_product(V, n, s.Dp, sixteen, narrow, true);
     else if (!narrow && s.logits.b == 64) s.logits.b = 128;
     s.inputs = plan_product(D, n, s.Vc, sixteen, narrow, true);
@@ -2907,7 +2913,8 @@ int hsadmm_softmax_loss(const hsadmm_plan_t* p, const hsadmm_softmax_loss_args_t
     int64_t off;
     if (const int rc = table_layer(p, x->layer, &V, &D, &off); rc != HSADMM_OK) return rc;
     if (!on_plan_device(p)) return HSADMM_ERR_INVALID_ARGUMENT;
-    if (!known_type(x->type) || x->reserved != 0 || (x->index_bits != 32 && x->index_bits != 64) || x->n > kMostLossRows || V > kMostClasses) return HSADMM_ERR_UNSUPPORTED;
+    if (!known_type(x->type) || x->reserved != 0 || (x->index_bits != 32 && x->index_bits != 64) || x->n > kMostLossRows || V > kMostClasses)
+        return HSADMM_ERR_UNSUPPORTED;
     const size_t size = type_size(x->type);
     if (x->n < 0 || !x->W || !is_aligned(x->W, 16) || !x->workspace || !is_aligned(x->workspace, 256) || !(std::fabs(x->scale) <= 3e38))
         return HSADMM_ERR_INVALID_ARGUMENT;
