@@ -2564,10 +2564,21 @@ int hsadmm_embedding_gradient(const hsadmm_plan_t* p, int32_t layer, const void*
     g.scale = scale; g.add = accumulate != 0;
     e = for_type(type, [&](auto t) {
         constexpr int T = decltype(t)::value;
+        // a workgroup for each span of columns that its waves read at once, as long as a grid holds them
+        const auto shared = [&](int64_t workgroups, int64_t span) {
+            g.shares = (int)std::max<int64_t>(1, std::min<int64_t>((D + span - 1) / span, kGridMost / workgroups));
+            return (unsigned)(workgroups * g.shares);
+        };
+        constexpr int64_t kPiece = Wide<T>::n;
         hipError_t r = hipSuccess;
-        if (n > ws.part) r = launch(p, kEmbedParts, embedding_parts<T>, (unsigned)ws.stretches, kBlock, s, g);
-        if (r == hipSuccess) r = launch(p, kEmbedGrad, embedding_gradient<T>, (unsigned)((n + kWaves * kPlacesOfWave - 1) / (kWaves * kPlacesOfWave)), kBlock, s,
-                                        g);
+        if (n > ws.part) {
+            const unsigned grid = shared(ws.stretches, kBlock * kPiece);
+            r = launch(p, kEmbedParts, embedding_parts<T>, grid, kBlock, s, g);
+        }
+        if (r == hipSuccess) {
+            const unsigned grid = shared((n + kWaves * kPlacesOfWave - 1) / (kWaves * kPlacesOfWave), kAcross * kWave * kPiece);
+            r = launch(p, kEmbedGrad, embedding_gradient<T>, grid, kBlock, s, g);
+        }
         return r;
     });
     return e == hipSuccess ? HSADMM_OK : HSADMM_ERR_HIP;

@@ -297,6 +297,7 @@ struct EmbedGradArgs {
     void* G;
     float scale;
     int add;
+    int shares;         // workgroups that share a stretch's, or some places', columns
 };
 
 // First place in the sorted list whose token is at least v, by a whole wave: it looks at 64 places at a time.
@@ -365,7 +366,8 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
 {
     constexpr int m = Wide<T>::n;
     __shared__ int bound[4];
-    const int64_t b = blockIdx.x;
+    const int64_t b = blockIdx.x / a.shares;
+    const int share = blockIdx.x % a.shares;
     const int from = (int)(b * a.part), to = (int)min((int64_t)a.n, (b + 1) * a.part), wave = threadIdx.x / kWave, lane = threadIdx.x & (kWave - 1);
     // the extent of the tokens of the first and the last position
     {
@@ -381,12 +383,12 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
         const int f = which ? bound[2] : from, t = which ? to : min(to, bound[1]);
         float* sums = a.sums + (2 * b + which) * a.pitch;
         if (a.cols < m) {
-            if ((int)threadIdx.x < a.cols) sums[threadIdx.x] = add_column<T>(a, f, t, threadIdx.x);
+            if (share == 0 && (int)threadIdx.x < a.cols) sums[threadIdx.x] = add_column<T>(a, f, t, threadIdx.x);
             continue;
         }
-        for (int c0 = wave * kWave * m; c0 < a.cols; c0 += kBlock * m) {
-            const int at = c0 + lane * m;
-            const int c[1] = {min(at, a.cols - m)};
+        for (int64_t c0 = ((int64_t)share * kWaves + wave) * kWave * m; c0 < a.cols; c0 += (int64_t)a.shares * kBlock * m) {
+            const int64_t at = c0 + lane * m;
+            const int c[1] = {(int)min(at, (int64_t)a.cols - m)};
             float x[1][m] = {};
             for (int i = f; i < t; i += kWave) {
                 const int n = min(kWave, t - i);
@@ -415,7 +417,8 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
     typedef typename Wide<T>::any A;
     constexpr int m = Wide<T>::n;
     const int lane = threadIdx.x & (kWave - 1);
-    const int64_t first = ((int64_t)blockIdx.x * kWaves + threadIdx.x / kWave) * kPlacesOfWave;
+    const int share = blockIdx.x % a.shares;
+    const int64_t first = ((int64_t)(blockIdx.x / a.shares) * kWaves + threadIdx.x / kWave) * kPlacesOfWave;
     if (first >= a.n) return;
     const int64_t place = min(first + lane, (int64_t)a.n - 1);
     const int32_t key = first + lane < a.n ? a.key[place] : a.V;       // (behind the last place: no token)
@@ -436,7 +439,7 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
         const int64_t inside = b0 * a.part != from ? 1 : 0;
         E* row = static_cast<E*>(a.G) + (int64_t)v * a.cols;
         if (a.cols < m) {
-            if (lane < a.cols) {
+            if (share == 0 && lane < a.cols) {
                 float x = 0.f;
                 if (!many) x = add_column<T>(a, from, from + n, lane);
                 else
@@ -445,16 +448,16 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
             }
             continue;
         }
-        for (int c0 = 0; c0 < a.cols; c0 += kAcross * kWave * m) {
+        for (int64_t c0 = (int64_t)share * kAcross * kWave * m; c0 < a.cols; c0 += (int64_t)a.shares * kAcross * kWave * m) {
             float x[kAcross][m] = {};
             int c[kAcross];
             bool on[kAcross];
             V g[kAcross];
 #pragma unroll
             for (int k = 0; k < kAcross; ++k) {
-                const int at = c0 + (k * kWave + lane) * m;
+                const int64_t at = c0 + (k * kWave + lane) * m;
                 on[k] = at < a.cols;
-                c[k] = min(at, a.cols - m);
+                c[k] = (int)min(at, (int64_t)a.cols - m);
             }
             if (a.add)
 #pragma unroll
@@ -494,7 +497,7 @@ __global__ __launch_bounds__(kBlock) void embedding_gradient(EmbedGradArgs a)
                     V y;
 #pragma unroll
                     for (int e = 0; e < m; ++e) y[e] = (E)(a.add ? x[k][e] * a.scale + (float)g[k][e] : x[k][e] * a.scale);
-                    const int skip = c0 + (k * kWave + lane) * m - c[k];
+                    const int skip = (int)(c0 + (k * kWave + lane) * m - c[k]);
                     if (!a.add || skip == 0) {
                         *reinterpret_cast<A*>(row + c[k]) = y;
                     } else {
