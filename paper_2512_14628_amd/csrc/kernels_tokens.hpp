@@ -40,8 +40,7 @@ __global__ __launch_bounds__(kBlock) void embedding_rows(const typename ElemOf<T
 
 // Positions sorted by their token, tokens that are equal in the order of their positions: radix sort from the lowest digit, of up to
 // kDigitBits bits each.  Ids outside [0, V) become V and so come last.  A workgroup takes a tile of positions, a wave of it adjacent
-// ones, kSortAtOnce for each lane at a time (their loads are in flight together: one after the other, 32768 positions took 146 us);
-// lanes with equal digits find each other by ballots, so places depend on the ids alone.
+// ones, kSortAtOnce for each lane at a time, whose loads are in flight together; lanes with equal digits find each other by ballots, so places depend on the ids alone.
 typedef float v4f_at2 __attribute__((ext_vector_type(4), aligned(2)));
 constexpr int kDigitBits = 9;
 constexpr int kDigits = 1 << kDigitBits;
@@ -209,15 +208,69 @@ __device__ void sort_places(SortShared& s, const uint32_t* start, int stride)
     __syncthreads();
 }
 
-// A single tile: all passes in one workgroup, the first.
+// A single tile: all passes in one workgroup, the first.  Positions and their tokens stay in registers and pass through LDS from digit
+// to digit (through memory: 18.6 us for 777 positions and two digits, so 13.6 with the clearing of 80 MB beside it).
+struct SortedTile {
+    int32_t key[kSortMost];
+    uint16_t pos[kSortMost];
+};
+
 __global__ __launch_bounds__(kScanBlock) void token_sort(SortArgs a)
 {
     __shared__ SortShared s;
+    __shared__ SortedTile moved;
     if (blockIdx.x > 0) return clear_rows(a.clear, 0, blockIdx.x - 1, gridDim.x - 1);
+    constexpr int kOwn = kSortMost / kScanBlock;
+    static_assert(kSortMost <= 1 << 16, "positions of 16 bits");
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, mask = (1 << a.bits) - 1;
+    const SortPart part(a, 0);
+    int32_t key[kOwn];
+    uint32_t pos[kOwn];
+    bool active[kOwn];
+#pragma unroll
+    for (int u = 0; u < kOwn; ++u) {
+        const int64_t i = part.from + u * kWave + lane;
+        active[u] = i < part.to;
+        key[u] = active[u] ? sort_key(a, 0, i) : 0;
+        pos[u] = (uint32_t)i;
+    }
     for (int pass = 0; pass < a.passes; ++pass) {
-        sort_count(a, pass, 0, s);
+        const int shift = pass * a.bits;
+        for (int d = lane; d < kDigits; d += kWave) s.count[wave][d] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kOwn; ++u)
+            if (active[u]) atomicAdd(&s.count[wave][(key[u] >> shift) & mask], 1u);
+        __syncthreads();
         sort_places(s, nullptr, 0);
-        sort_move(a, pass, 0, s);
+        const bool last = pass == a.passes - 1;
+#pragma unroll
+        for (int u = 0; u < kOwn; ++u) {
+            const int d = (key[u] >> shift) & mask;
+            const unsigned long long same = same_digit(d, a.bits, active[u]);
+            const int first = active[u] ? __ffsll((long long)same) - 1 : lane;
+            uint32_t at = 0;
+            if (active[u] && first == lane) at = atomicAdd(&s.count[wave][d], (uint32_t)__popcll(same));
+            at = __shfl(at, first, kWave) + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+            if (!active[u]) continue;
+            if (last) {
+                a.key[pass & 1][at] = key[u];
+                a.pos[pass & 1][at] = (int32_t)pos[u];
+            } else {
+                moved.key[at] = key[u];
+                moved.pos[at] = (uint16_t)pos[u];
+            }
+        }
+        if (last) break;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kOwn; ++u) {
+            if (!active[u]) continue;
+            const int i = (int)part.from + u * kWave + lane;
+            key[u] = moved.key[i];
+            pos[u] = moved.pos[i];
+        }
+        // (the next digit's counts are cleared behind a barrier that all of this has passed)
     }
 }
 
@@ -280,8 +333,7 @@ __global__ __launch_bounds__(kScanBlock) void token_move(SortArgs a, int pass)
 // ------------------------------------------------------------------ gradient of the embedding
 
 // dW[v] = scale times the sum of dY over v's tokens, in the order of their positions; in fp32, rounded once.  (Rows without a token
-// are cleared beside the sort.)  A token with more than
-// `part` positions is summed in parts first, those of the sorted list's stretches of `part`: a stretch holds the end of at most one
+// are cleared beside the sort.)  A token with more than `part` positions is summed in parts first, those of the sorted list's stretches of `part`: a stretch holds the end of at most one
 // such token and the beginning of at most one (or the whole stretch is one's), so it has two rows of sums: [2 b] for the token of its
 // first position, [2 b + 1] for another that begins in it.
 struct EmbedGradArgs {
@@ -405,7 +457,7 @@ __global__ __launch_bounds__(kBlock) void embedding_parts(EmbedGradArgs a)
 // has the keys and positions of the 64 places from its first on in its lanes, so most tokens' rows are loaded as soon as those are
 // there.  kAcross pieces of 16 bytes a lane of up to four rows are in flight at once.  Bound by latency (keys, first rows, and the
 // stretches' sums of a token of many positions, one after the other): 32768 positions x 2048 in bf16, 134 MB read and 45 written, in
-// 54 us, behind 26 for the stretches.  Eight places a wave 63; rows of four pieces at once take registers that cost a wave, 70.
+// 47 us, behind 27 for the stretches.  Columns not shared among workgroups 54, for 11961 positions x 3854 over 87 rows, fp32, 89 for 15.
 constexpr int kPlacesOfWave = 4;
 constexpr int kAcross = 2;
 
