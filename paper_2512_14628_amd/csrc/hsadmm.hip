@@ -48,8 +48,8 @@
 //
 //   embedding_rows, token_sort / token_count / token_scan / token_move, embedding_parts / embedding_gradient, dropout_kernel   the
 //                   tokens' way into a language model, and back (hsadmm_embedding, hsadmm_embedding_gradient, hsadmm_dropout)
-//   loss_targets / loss_rows / loss_product / loss_softmax / loss_total / loss_inputs   softmax cross entropy of a layer's products and
-//                   its gradients (hsadmm_softmax_loss)
+//   loss_few / loss_targets / loss_rows / loss_product / loss_softmax / loss_total / loss_inputs   softmax cross entropy of a layer's
+//                   products and its gradients (hsadmm_softmax_loss)
 //
 // loss_product is the one dense contraction: tiles on the matrix units.  Every other kernel is bound by HBM traffic.
 // Arena data is touched once per kernel, so it is moved with non-temporal 128-bit accesses.
@@ -2799,11 +2799,20 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
     E* rows = reinterpret_cast<E*>(w + ws.rows);
     E* packed = reinterpret_cast<E*>(w + ws.packed);
     const E* W = static_cast<const E*>(at_elem(x->W, off, size));
-    hipError_t e = launch(p, kLossTargets, loss_targets, 1u, kScanBlock, s, x->labels, (int)(x->index_bits == 64), n, V, x->scale,
-                          (int)(x->mean != 0), r, x->loss, x->lse);
-    if (e == hipSuccess && n > 0)
-        e = launch(p, kLossRows, loss_rows<T, true>, row_grid(n, ws.Dp * size), kBlock, s, static_cast<const E*>(x->X), x->x_stride, n, (int)D, r,
-                   rows, (int)ws.Dp, row_lanes(ws.Dp * size));
+    const unsigned grid = row_grid(n, ws.Dp * size);
+    const int lanes = row_lanes(ws.Dp * size), wide = x->index_bits == 64, mean = x->mean != 0;
+    const E* X = static_cast<const E*>(x->X);
+    hipError_t e;
+    // (few rows: 256 of 2048 fp32 inputs listed and copied by one launch in 4.9 us, by two in 2.2 and 3.6 and the gap; with more rows
+    // every workgroup would read too many labels)
+    if (n > 0 && n <= kFewLabels) {
+        e = launch(p, kLossRows, loss_few<T>, grid, kBlock, s, x->labels, wide, (int)n, V, x->scale, mean, r, x->loss, x->lse, X, x->x_stride,
+                   (int)D, rows, (int)ws.Dp, lanes);
+    } else {
+        e = launch(p, kLossTargets, loss_targets, 1u, kScanBlock, s, x->labels, wide, n, V, x->scale, mean, r, x->loss, x->lse);
+        if (e == hipSuccess && n > 0)
+            e = launch(p, kLossRows, loss_rows<T, true>, grid, kBlock, s, X, x->x_stride, n, (int)D, r, rows, (int)ws.Dp, lanes);
+    }
     ProductArgs a{};
     a.head = r.head;
     a.V = V;
@@ -2869,8 +2878,9 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
         const unsigned threads = work <= 256 ? 64 : work <= 2048 && n >= 512 ? kBlock : kScanBlock;
         if (e == hipSuccess) e = launch(p, kLossSoftmax, loss_softmax<T>, (unsigned)n, threads, s, m);
     }
-    if (e == hipSuccess && x->total)
-        e = launch(p, kLossTotal, loss_total, 1u, kScanBlock, s, (const LossHead*)r.head, (const float*)held_loss, (int)(x->mean != 0), x->total);
+    const bool total_behind = x->dX && n > 0;
+    if (e == hipSuccess && x->total && !total_behind)
+        e = launch(p, kLossTotal, loss_total, 1u, kBlock, s, (const LossHead*)r.head, (const float*)held_loss, mean, x->total);
     if (!gradients) return e;
     for (int i = ws.pieces - 1; i >= 0 && e == hipSuccess; --i) {
         const int32_t v0 = (int32_t)(i * ws.Vc);
@@ -2911,9 +2921,10 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
             e = launch_product<T, true, true, kWeightGrads>(p, kLossWeightGrads, how, D, classes, f, s);
         }
     }
-    if (e == hipSuccess && x->dX && n > 0)
-        e = launch(p, kLossInputs, loss_inputs<T>, row_grid(n, D * size), kBlock, s, (const float*)(w + ws.sums), ws.inputs.splits, ws.Np * ws.Dp,
-                   ws.Dp, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D, row_lanes(D * size));
+    if (e == hipSuccess && total_behind)
+        e = launch(p, kLossInputs, loss_inputs<T>, row_grid(n, D * size) + (x->total ? 1 : 0), kBlock, s, (const float*)(w + ws.sums), ws.inputs.splits, ws.Np * ws.Dp,
+                   ws.Dp, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D, row_lanes(D * size),
+                   (const float*)held_loss, mean, x->total);
     return e;
 }
 

@@ -127,6 +127,64 @@ __global__ __launch_bounds__(kScanBlock) void loss_targets(const void* __restric
     if (threadIdx.x < kZeroPage / 4) reinterpret_cast<float*>(r.head->zeros)[threadIdx.x] = 0.f;
 }
 
+// Both for up to kFewLabels rows, in one launch: every workgroup reads all labels, so a row knows its place by itself, and copies it there
+// if it has a target.  `lanes` threads (a wave or four) share a row.  Bound by the loads' latency: 32 rows of 64 in 3.6 us, 256 of 2048
+// fp32 elements in 4.9, 1537 of 1441 in half precision in 7.0; two launches 2.4 + 2.7, 2.2 + 3.6, 5.1 + 5.1 and 1 to 2 between them.
+constexpr int kFewLabels = 2048;
+template <int T>
+__global__ __launch_bounds__(kBlock) void loss_few(const void* __restrict__ labels, int wide, int n, int32_t V, double scale, int mean,
+                                                   LossRows r, float* __restrict__ loss, float* __restrict__ lse,
+                                                   const typename ElemOf<T>::type* __restrict__ src, int64_t ld, int cols,
+                                                   typename ElemOf<T>::type* __restrict__ dst, int pitch, int lanes)
+{
+    constexpr int kEach = kFewLabels / kBlock, kWords = kFewLabels / kWave, m = Wide<T>::n;
+    static_assert(kWords <= kWave, "a lane per word");
+    __shared__ unsigned long long target[kWords];           // bit i % 64 of word i / 64: row i has one
+    const int lane = threadIdx.x % kWave;
+    int64_t y[kEach];
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const int i = u * kBlock + (int)threadIdx.x;
+        y[u] = i < n ? index_at(labels, wide != 0, i) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kEach; ++u) {
+        const unsigned long long all = __ballot(y[u] >= 0 && y[u] < V);
+        if (lane == 0) target[(u * kBlock + (int)threadIdx.x) / kWave] = all;
+    }
+    __syncthreads();
+    const int i = (int)blockIdx.x * (kBlock / lanes) + (int)threadIdx.x / lanes;       // one row a wave
+    const unsigned long long own = lane < kWords ? target[lane] : 0;
+    const int word = i / kWave;
+    int count = __popcll(own), at = lane < word ? count : lane == word ? __popcll(own & ((1ull << (i % kWave)) - 1)) : 0;
+    for (int o = kWave / 2; o > 0; o >>= 1) {
+        count += __shfl_xor(count, o, kWave);
+        at += __shfl_xor(at, o, kWave);
+    }
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0) {
+            r.head->count = count;
+            r.head->factor = (float)(mean ? scale / (double)max(count, 1) : scale);
+        }
+        if (threadIdx.x < kZeroPage / 4) reinterpret_cast<float*>(r.head->zeros)[threadIdx.x] = 0.f;
+    }
+    if (i >= n) return;
+    const bool has = (target[word] >> (i % kWave)) & 1;
+    if (threadIdx.x % lanes == 0) {
+        r.place[i] = has ? at : -1;
+        if (has) {
+            r.row[at] = i;
+            r.label[at] = (int32_t)index_at(labels, wide != 0, i);
+        } else {
+            if (loss) loss[i] = 0.f;
+            if (lse) lse[i] = 0.f;
+        }
+    }
+    if (!has) return;
+    for (int c = (threadIdx.x & (lanes - 1)) * m; c < pitch; c += lanes * m)
+        *reinterpret_cast<typename Wide<T>::vec*>(dst + (int64_t)at * pitch + c) = load_piece<T>(src + i * ld + c, cols - c);
+}
+
 // Copies rows of `cols` elements that lie ld apart to rows of `pitch` (a multiple of kInputCols), zeros behind the last column.  LIST:
 // the rows of the list (those that have a target: what the others hold, NaN included, is not looked at again).  The products then
 // load whole 16-byte pieces and know no strides.  `lanes` threads (a wave or four) share a row.
@@ -715,38 +773,49 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
     }
 }
 
-// The sum (mean) of the losses, in fp64 and in an order that depends on their number alone, and how many there are.
-__global__ __launch_bounds__(kScanBlock) void loss_total(const LossHead* __restrict__ head, const float* __restrict__ held, int mean,
-                                                         float* __restrict__ total)
+// The sum (mean) of the losses, in fp64 and in an order that depends on their number alone, and how many there are.  One workgroup, a
+// launch of its own only where no inputs' gradients are made.
+__device__ void add_losses(const LossHead* __restrict__ head, const float* __restrict__ held, int mean, float* __restrict__ total)
 {
-    __shared__ double red[kScanWaves];
-    constexpr int kAtOnce = 4;
+    __shared__ double red[kWaves];
+    constexpr int kAtOnce = 16;
     const int count = head->count;
     double s = 0.0;
-    for (int i0 = threadIdx.x; i0 < count; i0 += kAtOnce * kScanBlock) {
+    for (int i0 = threadIdx.x; i0 < count; i0 += kAtOnce * kBlock) {
         float x[kAtOnce];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) x[u] = held[min(i0 + u * kScanBlock, count - 1)];
+        for (int u = 0; u < kAtOnce; ++u) x[u] = held[min(i0 + u * kBlock, count - 1)];
 #pragma unroll
-        for (int u = 0; u < kAtOnce; ++u) s += i0 + u * kScanBlock < count ? (double)x[u] : 0.0;
+        for (int u = 0; u < kAtOnce; ++u) s += i0 + u * kBlock < count ? (double)x[u] : 0.0;
     }
     s = wave_xor_sum(s, kWave);
     if (threadIdx.x % kWave == 0) red[threadIdx.x / kWave] = s;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kScanWaves; ++w) s += red[w];
+        for (int w = 1; w < kWaves; ++w) s += red[w];
         total[0] = (float)(mean ? s / (double)max(count, 1) : s);
         total[1] = (float)count;
     }
 }
+__global__ __launch_bounds__(kBlock) void loss_total(const LossHead* __restrict__ head, const float* __restrict__ held, int mean,
+                                                     float* __restrict__ total)
+{
+    add_losses(head, held, mean, total);
+}
 
 // The gradients of the inputs: the parts' sums in order, times the factor, to the rows they belong to; zeros where there is no target.
+// Where `total` is asked for the first workgroup makes that instead (a launch less, 3 to 5 us).
 template <int T>
 __global__ __launch_bounds__(kBlock) void loss_inputs(const float* __restrict__ sums, int splits, int64_t part, int64_t sum_ld, LossRows r,
-                                                      typename ElemOf<T>::type* __restrict__ dX, int64_t ld, int64_t n, int cols, int lanes)
+                                                      typename ElemOf<T>::type* __restrict__ dX, int64_t ld, int64_t n, int cols, int lanes,
+                                                      const float* __restrict__ held_loss, int mean, float* __restrict__ total)
 {
     constexpr int m = Wide<T>::n;
-    const int64_t i = (int64_t)blockIdx.x * (kBlock / lanes) + threadIdx.x / lanes;
+    if (total && blockIdx.x == 0) {
+        add_losses(r.head, held_loss, mean, total);
+        return;
+    }
+    const int64_t i = (int64_t)(blockIdx.x - (total ? 1 : 0)) * (kBlock / lanes) + threadIdx.x / lanes;
     if (i >= n) return;
     const int64_t q = r.place[i];
     const float f = r.head->factor * (1.f / grad_unit<T>());

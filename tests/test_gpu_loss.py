@@ -231,6 +231,33 @@ def test_same_bits_from_run_to_run(kind, n, D, V):
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("bits", [32, 64])
+@pytest.mark.parametrize("n", [63, 64, 65, 255, 257, 2047, 2048, 2049])
+@pytest.mark.parametrize("D", [24, 264])
+def test_listing_rows_around_the_sizes_of_its_pieces(n, D, bits):
+    """Half the rows have no target; the total's bits do not depend on what else is asked for."""
+    say("listing", n, D, bits)
+    case = Case(F32, n, D, 37, seed=n, share=0.5, index_bits=bits).run().check()
+    total = case.total.clone()
+    case.run(outputs=("total",))
+    assert torch.equal(case.total[:2], total[:2])
+
+
+@pytest.mark.parametrize("which", ["first", "last", "all", "none"])
+@pytest.mark.parametrize("n", [1, 65, 2048, 2049])
+def test_listing_one_row_or_all(n, which):
+    say("listing", n, which)
+    case = Case(BF16, n, 40, 9, seed=n, share=0.0)
+    if which in ("first", "last"):
+        keep = 0 if which == "first" else n - 1
+        y = int(case.labels[keep])
+        case.labels.fill_(-100)
+        case.labels[keep] = y
+    elif which == "none":
+        case.labels.fill_(-100)
+    case.run().check()
+
+
 def test_gradients_against_differences():
     """The kernels' gradients in fp32 against differences of the loss in 64 bits: a step h = 1e-4 of both sides is off by h^2 / 6 times
     the third derivative, which for a softmax is at most |direction . input|^3 of its logits."""
