@@ -9,6 +9,7 @@
 #define KERNELS_LOSS_HPP
 #include "hsadmm_device.hpp"
 #include "kernels_training.hpp"
+#include "loss_plan.hpp"
 
 namespace {
 
@@ -55,8 +56,6 @@ __device__ __forceinline__ int64_t index_at(const void* p, bool wide, int64_t i)
 
 // ------------------------------------------------------------------ rows that have a target
 
-constexpr int kInputRows = 256;          // rows of the held copies are rounded up to this ...
-constexpr int kInputCols = 64;           // ... and their columns to this (128 bytes at least)
 constexpr int kZeroPage = 256;          // bytes of zeros that stand for what lies outside an operand
 
 struct LossHead {
@@ -65,7 +64,7 @@ struct LossHead {
     int32_t pad[62];
     unsigned char zeros[kZeroPage];
 };
-static_assert(sizeof(LossHead) == 512, "LossHead layout");
+static_assert(sizeof(LossHead) == kLossHeadBytes, "LossHead layout");
 
 struct LossRows {
     LossHead* head;
@@ -569,7 +568,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                     if constexpr (T != HSADMM_TYPE_F32) acc[i][j][e] = x * grad_unit<T>();
                 }
             sum += __shfl_xor(sum, 32, kWave);
-            if (half == 0) a.slab[q * a.slabs + (a.v0 + p0 + wp) / (BP / WP)] = make_float2(top, sum);
+            if (half == 0 && q < count) a.slab[q * a.slabs + (a.v0 + p0 + wp) / (BP / WP)] = make_float2(top, sum);
             if (keep)
 #pragma unroll
                 for (int i = 0; i < TP; ++i)
@@ -607,14 +606,15 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     } else if constexpr (WHAT == kSums) {
 #pragma unroll
         for (int j = 0; j < TQ; ++j) {
-            float* row = a.sums + part * a.sum_part + (q0 + wq + 32 * j + (lane & 31)) * a.ld;
+            const int64_t q = q0 + wq + 32 * j + (lane & 31);
+            float* row = a.sums + part * a.sum_part + q * a.ld;
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const int64_t c = p0 + wp + 32 * i + 8 * g + 4 * half;
                     v4f x = four(i, j, g);
-                    if (c < a.ld) {
+                    if (q < count && c < a.ld) {
                         if (a.add) x += *reinterpret_cast<const v4f*>(row + c);
                         *reinterpret_cast<v4f*>(row + c) = x;
                     }
