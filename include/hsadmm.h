@@ -982,9 +982,9 @@ int hsadmm_dropout(const hsadmm_plan_t* plan, const void* X, int64_t x_stride, c
  *     dX = f P W;   the layer's rows of G = f P^T X (with `accumulate` added to what G holds)
  * `scale` multiplies the gradients alone (a loss scale of fp16 training).  Rows without a target cost nothing, and what X holds there
  * is not looked at.  Logits are formed in fp32; P is rounded to `type` (half precision: 2^15 P) for the products that follow, some of it
- * from exponentials that were rounded to `type` before (sums of up to 256 terms, rows or classes, also take what the rounding
- * leaves).  At most 2^31 bytes of either are held, a piece of the vocabulary: where it
- * takes several, the logits of all but the last are formed twice.
+ * from exponentials that were rounded to `type` before.  What rounding the label's own P_i,label_i leaves, most of a row's gradient,
+ * is added to dX and G; up to 256 classes, and in G up to 256 rows, that of the other classes is too.  At most 2^31 bytes of logits
+ * or of P are held, a piece of the vocabulary: where it takes several, the logits of all but the last are formed twice.
  * Fill a zeroed hsadmm_softmax_loss_args_t; a NULL field means "not wanted"; at least one output is.
  *   struct_bytes  sizeof(hsadmm_softmax_loss_args_t) as the caller was compiled (INVALID_ARGUMENT if it differs)
  *   W             in, arena of weights, 16-byte aligned

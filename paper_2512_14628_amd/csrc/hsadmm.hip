@@ -2705,6 +2705,8 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
     a.held = w + ws.grads;
     a.ld = ws.Vc;
     a.stat = reinterpret_cast<float2*>(w + ws.stat);
+    float* own = reinterpret_cast<float*>(w + ws.own);
+    a.own = own;
     const Operand inputs{rows, ws.Dp, ws.Np, ws.Dp};
     // the weights of the classes from v0 on, `classes` of them
     const auto weights = [&](int32_t v0, int64_t classes, Operand* o) -> hipError_t {
@@ -2748,6 +2750,8 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
         m.parts = ws.logits.splits;
         m.sum_part = ws.Np * ws.Vc;
         m.stat = reinterpret_cast<float2*>(w + ws.stat);
+        m.own = own;
+        m.rounded = reinterpret_cast<int32_t*>(w + ws.rounded);
         m.held_loss = held_loss;
         m.loss = x->loss; m.lse = x->lse;
         m.held = w + ws.grads;
@@ -2794,10 +2798,12 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
             ProductArgs f = a;
             f.p = Operand{rows, ws.Dp, ws.Dp, 0};
             f.q = Operand{w + ws.grads, ws.Vc, classes, 0};
+            f.v0 = v0;
             f.out = static_cast<E*>(x->G) + off + (int64_t)v0 * D;
             f.ld = D;
             f.add = x->accumulate != 0;
             f.rest = ws.rest_weights ? size * ws.Np * ws.Vc : 0;
+            if (!ws.rest_weights) f.rounded = reinterpret_cast<const int32_t*>(w + ws.rounded);
             ProductPlan how = ws.weights;
             how.k_part = INT64_MAX / 2;
             e = launch_product<T, true, true, kWeightGrads>(p, kLossWeightGrads, how, D, classes, f, s);
@@ -2806,7 +2812,7 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
     if (e == hipSuccess && total_behind)
         e = launch(p, kLossInputs, loss_inputs<T>, row_grid(n, D * size) + (x->total ? 1 : 0), kBlock, s, (const float*)(w + ws.sums), ws.inputs.splits, ws.Np * ws.Dp,
                    ws.Dp, r, static_cast<E*>(x->dX), x->dx_stride, n, (int)D, row_lanes(D * size),
-                   (const float*)held_loss, mean, x->total);
+                   (const float*)held_loss, mean, x->total, W, (const float*)(x->type == HSADMM_TYPE_F32 || ws.rest_inputs ? nullptr : own));
     return e;
 }
 

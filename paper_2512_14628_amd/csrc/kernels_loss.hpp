@@ -230,6 +230,8 @@ struct ProductArgs {
     int32_t keep0;
     int64_t ld;
     const float2* stat;         // [rows] largest logit, 1 / sum
+    const float* own;           // [rows] gradient of the label's logit
+    const int32_t* rounded;     // [rows] the label of a row whose own gradient's rounding leaves something, else -1; or null: nothing is added
     // kSums: [splits][rows][ld]; kWeightGrads: rows of ld elements, part of an arena
     float* sums;
     int64_t sum_part;
@@ -380,6 +382,7 @@ template <int T, int BP, int BQ, int WP, int WQ, bool PMAJOR, bool QMAJOR, int W
 __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
 {
     typedef typename ElemOf<T>::type E;
+    typedef typename Wide<T>::vec V;
     typedef TilePart<T, BP, PMAJOR> LP;
     typedef TilePart<T, BQ, QMAJOR> LQ;
     constexpr int kThreads = WP * WQ * kWave, TP = BP / WP / 32, TQ = BQ / WQ / 32, kSteps = 4;
@@ -502,11 +505,110 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     }
     tile_barrier<0>();
 
+    // What rounding the labels' gradients has left, over the rows whose label is one of the tile's classes: a product like the one
+    // above, of those rows' inputs and a matrix with one element a row.  A thread looks at kEach adjacent rows at a time; the rows found
+    // are gathered, 64 a turn, two turns ahead.  us a call without / with it, bf16, labels as frequent as tokens are: 4096 x 2048 x 32768
+    // 1495 / 1511, 16384 x 512 x 4096 394 / 447 (half the labels in the first tile), 560 x 1568 x 3479 72 / 79.
+    if constexpr (WHAT == kWeightGrads && T != HSADMM_TYPE_F32) if (a.rounded) {
+        constexpr int kEach = 16, kChunk = kThreads * kEach, kW = kThreads / kWave;
+        constexpr int kRowThreads = kThreads / LQ::kK;          // that make a row of the second operand
+        static_assert(PMAJOR && kChunk <= 1 << 16 && kChunk * 2 <= kPlace, "the list fits its place");
+        uint16_t* list = reinterpret_cast<uint16_t*>(place(2));                     // rows found, numbers in the chunk, ascending
+        int* found = reinterpret_cast<int*>(place(4));                              // [2][waves]
+        const auto ring = [&](int slot) { return place(slot == 2 ? 3 : slot); };    // 0, 1, 3; 4 is the second operand's
+        const int class0 = a.v0 + (int)q0, classes = (int)min((int64_t)BQ, a.q.mn - q0);
+        typedef int v4i __attribute__((ext_vector_type(4)));
+        v4i next[kEach / 4];
+        const auto look = [&](int r0) {
+            const int r = r0 + (int)threadIdx.x * kEach;
+#pragma unroll
+            for (int u = 0; u < kEach / 4; ++u) next[u] = r + 4 * u < count ? *reinterpret_cast<const v4i*>(a.rounded + r + 4 * u) : v4i{-1, -1, -1, -1};
+        };
+        look(0);
+        for (int r0 = 0, side = 0; r0 < count; r0 += kChunk, side ^= 1) {
+            uint32_t hits = 0;
+#pragma unroll
+            for (int u = 0; u < kEach; ++u)
+                if (r0 + (int)threadIdx.x * kEach + u < count && (uint32_t)(next[u / 4][u % 4] - class0) < (uint32_t)classes) hits |= 1u << u;
+            if (r0 + kChunk < count) look(r0 + kChunk);
+            int upto = __popc(hits);
+            for (int o = 1; o < kWave; o <<= 1) {
+                const int x = __shfl_up(upto, o, kWave);
+                if (lane >= o) upto += x;
+            }
+            if (lane == kWave - 1) found[side * kW + wave] = upto;
+            __syncthreads();
+            int n = 0, at = upto - __popc(hits);
+#pragma unroll
+            for (int w = 0; w < kW; ++w) {
+                const int x = found[side * kW + w];
+                n += x;
+                if (w < wave) at += x;
+            }
+            n = __builtin_amdgcn_readfirstlane(n);
+            if (n == 0) continue;
+            for (uint32_t h = hits; h != 0; h &= h - 1) list[at++] = (uint16_t)(threadIdx.x * kEach + __ffs(h) - 1);
+            __syncthreads();
+            const int turns = (n + LP::kK - 1) / LP::kK;
+            const auto load = [&](int turn, char* to) {
+#pragma unroll
+                for (int i = 0; i < kLoadsP; ++i) {
+                    const int slot = i * kThreads + threadIdx.x, k = slot / LP::kRow, piece = (slot % LP::kRow) ^ LP::turn(k), h = turn * LP::kK + k;
+                    const int64_t mn = p0 + piece * LP::kPiece;
+                    const void* from = zeros;
+                    if (h < n) from = static_cast<const E*>(a.p.at) + (r0 + (int64_t)list[h]) * a.p.ld + (mn < a.p.mn ? mn : 0);
+                    load_to_lds(from, to + (i * kThreads + (threadIdx.x & ~(kWave - 1))) * 16);
+                }
+            };
+            // of the thread's row of the second operand, a turn ahead
+            const int k = threadIdx.x / kRowThreads;
+            int of = 0;
+            float own = 0.f;
+            const auto second = [&](int turn) {
+                const int h = turn * LQ::kK + k;
+                of = 0;
+                own = 0.f;
+                if (h < n) {
+                    of = a.label[r0 + (int)list[h]] - class0;
+                    own = a.own[r0 + (int)list[h]];
+                }
+            };
+            second(0);
+            load(0, ring(0));
+            load(1, ring(1));
+            for (int u = 0, slot = 0; u < turns; ++u) {
+                tile_barrier<kLoadsP>();
+                const char* at_p = ring(slot);
+                V one;
+#pragma unroll
+                for (int e = 0; e < LQ::kPiece; ++e) one[e] = (of & (LQ::kPiece - 1)) == e ? (E)(own - (float)(E)own) : (E)0.f;
+#pragma unroll
+                for (int i = 0; i < LQ::kRow / kRowThreads; ++i) {
+                    const int piece = i * kRowThreads + threadIdx.x % kRowThreads;
+                    *reinterpret_cast<V*>(place(4) + (k * LQ::kRow + (piece ^ LQ::turn(k))) * 16) = piece == of / LQ::kPiece ? one : V{};
+                }
+                second(u + 1);
+                load(u + 2, ring(slot == 0 ? 2 : slot - 1));
+                slot = slot == 2 ? 0 : slot + 1;
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s) {
+#pragma unroll
+                    for (int r = 0; r < kReads; ++r) read(r, s, at_p, place(4));
+                    step(s, [](int) {});
+                }
+            }
+            tile_barrier<0>();
+        }
+        __syncthreads();
+    }
+
     // p of element e (0..15) of acc[i][.]: 32 i + 8 (e / 4) + 4 half + e % 4 behind wp.  Outputs of type E pass through LDS, [q][p] with
     // the pieces of a row turned by the row's number, and leave as whole rows: straight from the lanes, 16 bytes in each of 32 rows at
     // a time, a tile of logits took 35 us on top of the 70 of its products (2048 inputs, bf16).
     typedef typename ElemOf<T>::vec V4;
-    typedef typename Wide<T>::vec V;
     constexpr int kPiece = Wide<T>::n, kRowPieces = BP / kPiece;
     static_assert(BP * BQ * (int)sizeof(E) <= kPlaces * kPlace && (kRowPieces & (kRowPieces - 1)) == 0, "the tile fits");
     const auto piece_at = [&](int q, int piece) { return lds + (q * kRowPieces + (piece ^ (q & (kRowPieces - 1)))) * 16; };
@@ -586,6 +688,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
             const int64_t q = q0 + wq + 32 * j + (lane & 31);
             const int label = q < count ? a.label[q] : -1;
             const float2 stat = q < count ? a.stat[q] : make_float2(0.f, 0.f);
+            const float own = q < count ? a.own[q] : 0.f;               // (as loss_softmax has it, to the last bit)
 #pragma unroll
             for (int i = 0; i < TP; ++i)
 #pragma unroll
@@ -594,7 +697,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
                     v4f x = four(i, j, g);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float y = (exp_of(x[e] - stat.x) * stat.y - (v + e == label ? 1.f : 0.f)) * grad_unit<T>();
+                        const float y = v + e == label ? own : exp_of(x[e] - stat.x) * stat.y * grad_unit<T>();
                         x[e] = v + e < a.V ? y : 0.f;
                     }
                     stage(i, j, g, x);
@@ -661,6 +764,8 @@ struct SoftmaxArgs {
     int parts;
     int64_t sum_part;
     float2* stat;
+    float* own;                 // [rows] gradients of the labels' logits ...
+    int32_t* rounded;           // ... and the label where rounding them leaves something that counts, else -1
     float* held_loss;           // [rows], for the total
     float* loss;                // by original rows, may be null
     float* lse;
@@ -696,9 +801,12 @@ __device__ __forceinline__ float2 join(float2 a, float2 b)
 }
 
 // A row per workgroup: largest logit, sum, loss, and the gradients of the logits that are held (softmax minus the label's one).  The order
-// of the additions depends on the sizes alone.  16 bits: what kLogits held is rounded already, so a gradient here carries two
-// roundings; the label's own comes from its logit in fp32, as softmax - 1 of a confident row has far fewer digits than either.
-// Without slabs what the rounding leaves is written as well where the call is one of few terms (a.rest).
+// of the additions here depends on the sizes alone.  16 bits: what kLogits held is rounded already, so a gradient carries two
+// roundings, but the label's own.  That one comes from its logit in fp32, as softmax - 1 of a confident row has far fewer digits than
+// either, and what its rounding leaves is added by those who use it: it is most of the row's gradient, so its rounding would be as large as that of
+// the outputs and the same for the whole row (1024 x 512 x 4096 in bf16, labels' softmax spread over (0, 1), error of dX against 64
+// bits: 0.00215 where it was left out, 0.00166 as the rounding of dX alone).  Without slabs what the rounding of all of them leaves is written as well where the call is
+// one of few terms (a.rest).
 template <int T>
 __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
 {
@@ -718,7 +826,7 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
     } else {
         for (int c = tid * 4; c < a.V; c += threads * 4) {
             const v4f x = add_parts(sum_row + c, a.parts, a.sum_part);
-            if (a.parts > 1) *reinterpret_cast<v4f*>(sum_row + c) = x;      // (read again by this thread, and for the label below)
+            if (a.parts > 1) *reinterpret_cast<v4f*>(sum_row + c) = x;      // (read again below, behind the barrier, by other threads too)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 if (c + e < a.V) s = join(s, make_float2(x[e], x[e] == x[e] ? 1.f : x[e]));
@@ -740,6 +848,12 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
     }
     if (!a.grads) return;
     const float own = (exp_of(picked - s.x) * inv - 1.f) * grad_unit<T>();
+    if (tid == 0) {
+        a.own[q] = own;
+        // (a 64th of half a step of the type is lost in the rounding of what it would be added to)
+        constexpr float kCounts = (T == HSADMM_TYPE_F16 ? 0x1p-11f : 0x1p-8f) / 64.f;
+        a.rounded[q] = __builtin_fabsf(own - (float)(E)own) < __builtin_fabsf(own) * kCounts ? -1 : label;
+    }
     E* to = static_cast<E*>(a.grads) + q * a.ld;
     E* to_rest = reinterpret_cast<E*>(reinterpret_cast<char*>(to) + a.rest);
     const E* held = static_cast<const E*>(a.held) + q * a.ld;
@@ -803,13 +917,16 @@ __global__ __launch_bounds__(kBlock) void loss_total(const LossHead* __restrict_
     add_losses(head, held, mean, total);
 }
 
-// The gradients of the inputs: the parts' sums in order, times the factor, to the rows they belong to; zeros where there is no target.
+// The gradients of the inputs: the parts' sums in order, and (`own`) what rounding the label's gradient has left times its row of W, times
+// the factor, to the rows they belong to; zeros where there is no target.
 // Where `total` is asked for the first workgroup makes that instead (a launch less, 3 to 5 us).
 template <int T>
 __global__ __launch_bounds__(kBlock) void loss_inputs(const float* __restrict__ sums, int splits, int64_t part, int64_t sum_ld, LossRows r,
                                                       typename ElemOf<T>::type* __restrict__ dX, int64_t ld, int64_t n, int cols, int lanes,
-                                                      const float* __restrict__ held_loss, int mean, float* __restrict__ total)
+                                                      const float* __restrict__ held_loss, int mean, float* __restrict__ total,
+                                                      const typename ElemOf<T>::type* __restrict__ W, const float* __restrict__ own)
 {
+    typedef typename ElemOf<T>::type E;
     constexpr int m = Wide<T>::n;
     if (total && blockIdx.x == 0) {
         add_losses(r.head, held_loss, mean, total);
@@ -819,14 +936,25 @@ __global__ __launch_bounds__(kBlock) void loss_inputs(const float* __restrict__ 
     if (i >= n) return;
     const int64_t q = r.place[i];
     const float f = r.head->factor * (1.f / grad_unit<T>());
+    float left = 0.f;
+    if (own && q >= 0) {
+        left = own[q] - (float)(E)own[q];
+        W += (int64_t)r.label[q] * cols;
+    }
     for (int c = (threadIdx.x & (lanes - 1)) * m; c < cols; c += lanes * m) {
         v4f x[m / 4] = {};
-        if (q >= 0)
+        if (q >= 0) {
+            typename Wide<T>::vec w = {};
+            if (own) w = load_piece<T>(W + c, cols - c);
 #pragma unroll
             for (int h = 0; h < m / 4; ++h) x[h] = add_parts(sums + q * sum_ld + c + 4 * h, splits, part);
+            if (own)
+#pragma unroll
+                for (int e = 0; e < m; ++e) x[e / 4][e % 4] += left * (float)w[e];
+        }
         typename Wide<T>::vec y;
 #pragma unroll
-        for (int e = 0; e < m; ++e) y[e] = (typename ElemOf<T>::type)(x[e / 4][e % 4] * f);
+        for (int e = 0; e < m; ++e) y[e] = (E)(x[e / 4][e % 4] * f);
         store_piece<T>(dX + i * ld + c, y, cols - c);
     }
 }

@@ -63,7 +63,7 @@ constexpr int64_t kFewTerms = 256;
 
 // How hsadmm_softmax_loss cuts its products, and where its scratch lies in the workspace.
 struct LossScratch {
-    size_t head, row, label, place, held_loss, picked, stat, slab, rows, packed, parts, grads, sums, total;
+    size_t head, row, label, place, held_loss, picked, own, rounded, stat, slab, rows, packed, parts, grads, sums, total;
     int64_t Np, Dp;             // rows and columns of the held inputs
     int64_t Vc;                 // classes of a piece, a multiple of 256
     int pieces;
@@ -97,13 +97,14 @@ inline LossScratch loss_scratch(int64_t held, int32_t V, int32_t D, int64_t off,
     s.Vc = ((V + s.pieces - 1) / s.pieces + 255) / 256 * 256;
     s.pieces = (int)((V + s.Vc - 1) / s.Vc);
     s.logits = plan_product(V, n, s.Dp, sixteen, narrow, false);
-    // Rounding the gradients of the logits to 16 bits is lost among the terms of a long sum.  In a short one (a vocabulary of a few
-    // classes for the inputs' gradient, a few rows for the weights') it would add half as much again to the rounding of the output
-    // (fp16, relative to 64 bits: 0.00031 for 0.00021): there what is left of the rounding is multiplied too, twice the time of a
-    // product that is short (0.00022).
+    // The gradients of the logits are rounded to 16 bits.  Of the label's what the rounding leaves is always added.  The other classes'
+    // roundings differ in sign: together they are off by sqrt(sum of p^2) of a rounding, little where the softmax is spread over many
+    // classes.  A vocabulary of a few classes is none: there, and in the weights' gradient of a few rows, what is left of all
+    // roundings is multiplied too, twice the time of a product that is short (fp16, error against 64 bits 0.00031 without, 0.00022 with;
+    // the output's own rounding is 0.00021).
     const bool fits = s.pieces == 1 && 4 * s.Np * s.Vc <= held;
     s.rest_inputs = gradients && sixteen && fits && V <= kFewTerms;
-    s.rest_weights = gradients && sixteen && fits && n <= kFewTerms;
+    s.rest_weights = gradients && sixteen && fits && (n <= kFewTerms || V <= kFewTerms);
     // (tiles of 64 are for so few logits that they are joined by rows as well)
     s.small = (s.pieces == 1 && (!s.logits.fills || s.logits.b == 64)) || s.rest_inputs || s.rest_weights;
     if (s.small) s.logits = plan_product(V, n, s.Dp, sixteen, narrow, true);
@@ -121,6 +122,8 @@ inline LossScratch loss_scratch(int64_t held, int32_t V, int32_t D, int64_t off,
     s.place = take(4 * s.Np);
     s.held_loss = take(4 * s.Np);
     s.picked = take(4 * s.Np);
+    s.own = take(gradients ? 4 * s.Np : 0);
+    s.rounded = take(gradients ? 4 * s.Np : 0);
     s.stat = take(8 * s.Np);
     s.slab = take(8 * s.slabs * s.Np);
     s.rows = take(size * s.Np * s.Dp);

@@ -29,8 +29,9 @@ def rounded(kind, value, bound):
     return SAFE * (bound + half_step(kind) * (value.abs() + bound)) + least(kind)
 
 
-def loss_reference(kind, X, W, labels, mean, scale):
-    """{name: (value, bound)}; X, W of the type, labels int64.  Rows without a target are not looked at."""
+def loss_reference(kind, X, W, labels, mean, scale, label=None):
+    """{name: (value, bound)}; X, W of the type, labels int64.  Rows without a target are not looked at.  `label`: what the gradient of
+    the label's own logit is off by, relative to itself, behind its fp32 steps (dX's share, G's); None: as the other classes'."""
     V, D = W.shape
     n = X.shape[0]
     f64 = torch.float64
@@ -71,13 +72,19 @@ def loss_reference(kind, X, W, labels, mean, scale):
     # (in 16 bits up to two roundings: of the exponential that is held, then of the gradient made of it)
     unit = 2.0 ** -15 if kind == pkg.TYPE_F16 else 1.0
     dP = dp + SAFE * (P.abs() + dp) * (2 * half_step(kind) + 4 * U) + 2 * unit * least(kind) + (2.0 ** -125 if kind != pkg.TYPE_F32 else 0)
+    dPx, dPw = dP, dP
+    if label is not None:
+        dPx, dPw = dP.clone(), dP.clone()
+        own = dp[rows, y] + SAFE * (P[rows, y].abs() + dp[rows, y]) * 4 * U
+        for share, into in zip(label, (dPx, dPw)):
+            into[rows, y] = own + SAFE * share * P[rows, y].abs() + (2 * unit * least(kind) if share else 0)
     dx = (P @ w) * g
-    ddx = abs(g) * (dP @ w.abs() + 2 * (V + 64) * U * ((P.abs() + dP) @ w.abs())) + 4 * U * dx.abs()
+    ddx = abs(g) * (dPx @ w.abs() + 2 * (V + 64) * U * ((P.abs() + dPx) @ w.abs())) + 4 * U * dx.abs()
     a, b = X.new_zeros((n, D), dtype=f64), X.new_zeros((n, D), dtype=f64)
     a[at], b[at] = dx, rounded(kind, dx, ddx)
     out["dX"] = (a, b)
     dw = (P.T @ x) * g
-    ddw = abs(g) * (dP.T @ x.abs() + 2 * (count + 2) * U * ((P.abs() + dP).T @ x.abs())) + 4 * U * dw.abs()
+    ddw = abs(g) * (dPw.T @ x.abs() + 2 * (count + 2) * U * ((P.abs() + dPw).T @ x.abs())) + 4 * U * dw.abs()
     out["G"] = (dw, ddw)             # before it is rounded (or added and rounded)
     return out
 

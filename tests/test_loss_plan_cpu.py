@@ -51,7 +51,7 @@ static void check(int64_t size, bool gradients, int64_t n, int32_t D, int32_t V,
     const int64_t each = s.rest_inputs || s.rest_weights ? 2 : 1;
     const struct { const char* what; size_t at; int64_t bytes; } all[] = {
         {"head", s.head, kLossHeadBytes}, {"row", s.row, 4 * n}, {"label", s.label, 4 * n}, {"place", s.place, 4 * n},
-        {"held_loss", s.held_loss, 4 * n}, {"picked", s.picked, 4 * n}, {"stat", s.stat, 8 * n}, {"slab", s.slab, 8 * s.slabs * s.Np},
+        {"held_loss", s.held_loss, 4 * n}, {"picked", s.picked, 4 * n}, {"own", s.own, gradients ? 4 * n : 0}, {"rounded", s.rounded, gradients ? 4 * s.Np : 0}, {"stat", s.stat, 8 * n}, {"slab", s.slab, 8 * s.slabs * s.Np},
         {"rows", s.rows, size * s.Np * s.Dp}, {"packed", s.packed, s.pack ? size * std::min<int64_t>(V, s.Vc) * s.Dp : 0},
         {"parts", s.parts, s.small ? 4 * s.logits.splits * s.Np * s.Vc : 0}, {"grads", s.grads, gradients ? each * size * s.Np * s.Vc : 0},
         {"sums", s.sums, gradients ? 4 * s.inputs.splits * s.Np * s.Dp : 0}, {"total", s.total, 0}};
