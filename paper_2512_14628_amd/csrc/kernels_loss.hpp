@@ -839,7 +839,8 @@ __global__ __launch_bounds__(kScanBlock) void loss_softmax(SoftmaxArgs a)
     for (int w = 1; w < threads / kWave; ++w) s = join(s, red[w]);
     const float picked = a.slab ? a.picked[q] : sum_row[label], inv = 1.f / s.y;
     if (tid == 0) {
-        const float log_sum = s.x + logf(s.y), x = log_sum - picked;
+        // (the largest logit cancels in the loss: in the sum's logarithm a loss of 1e-3 would be rounded to the steps of a logit of 1000)
+        const float log_y = logf(s.y), log_sum = s.x + log_y, x = (s.x - picked) + log_y;
         a.stat[q] = make_float2(s.x, inv);
         a.held_loss[q] = x;
         const int64_t i = a.r.row[q];
