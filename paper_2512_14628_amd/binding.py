@@ -49,7 +49,7 @@ EXPORTS = ("hsadmm_plan_create", "hsadmm_plan_destroy", "hsadmm_plan_sizes", "hs
            "hsadmm_compact_mx", "hsadmm_expand_mx",
            "hsadmm_embedding", "hsadmm_embedding_workspace", "hsadmm_embedding_gradient", "hsadmm_dropout",
            "hsadmm_softmax_loss_workspace", "hsadmm_softmax_loss")
-KERNEL_COUNT = 51
+KERNEL_COUNT = 52
 
 
 class HsadmmError(RuntimeError):

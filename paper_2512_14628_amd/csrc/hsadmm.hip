@@ -121,7 +121,7 @@ struct WsLayout {
     size_t key, colpart, pos, cnt, layer_off, kept_idx, respart, work, rowres, pred, est_cnt, est_keys, est_thr, est_thr_tag, nest, total;
 };
 
-enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kLossTargets, kLossRows, kLossLogits, kLossTotal, kLossSoftmax, kLossLogitGrads, kLossInputGrads, kLossWeightGrads, kLossInputs, kEmbedding, kTokenSort, kTokenCount, kTokenScan, kTokenMove, kEmbedParts, kEmbedGrad, kDropoutRows, kKernelCount };
+enum KernelId { kPass1 = 0, kTopk, kFixup, kScan, kGather, kScatter, kFrozen, kMaskOr, kWKeys, kWFinal, kDualInter, kResPart, kResFinish, kColsums, kChanFinal, kWFixup, kBothFinal, kAverage, kMaskDrift, kFixupGather, kWFixupPack, kRetrainProject, kRetrainExpand, kScaleLayers, kPass1Hinted, kHintedRepair, kSqnormPart, kResPick, kWHintedRepair, kGradSq, kGradFinish, kAdamw, kGatherMx, kScatterMx, kLossTargets, kLossRows, kLossLogits, kLossTotal, kLossSoftmax, kLossLogitGrads, kLossInputGrads, kLossWeightGrads, kLossInputs, kEmbedding, kTokenSort, kTokenCount, kTokenScan, kTokenMove, kEmbedParts, kEmbedGrad, kDropoutRows, kLossFew, kKernelCount };
 static_assert(kKernelCount == HSADMM_KERNEL_COUNT, "kernel id table");
 constexpr size_t kTimingPairs = 8192;
 // Workgroups of one launch: a grid has fewer than 2^32 threads.  The update and the expansion of quantised buffers take several launches for
@@ -2381,6 +2381,7 @@ const char* hsadmm_kernel_name(int kernel_id)
         case kEmbedParts: return "embedding_parts";
         case kEmbedGrad: return "embedding_gradient";
         case kDropoutRows: return "dropout";
+        case kLossFew: return "loss_few";
         default: return "";
     }
 }
@@ -2688,7 +2689,7 @@ static hipError_t launch_loss(const hsadmm_plan* p, const hsadmm_softmax_loss_ar
     // (few rows: 256 of 2048 fp32 inputs listed and copied by one launch in 4.9 us, by two in 2.2 and 3.6 and the gap; with more rows
     // every workgroup would read too many labels)
     if (n > 0 && n <= kFewLabels) {
-        e = launch(p, kLossRows, loss_few<T>, grid, kBlock, s, x->labels, wide, (int)n, V, x->scale, mean, r, x->loss, x->lse, X, x->x_stride,
+        e = launch(p, kLossFew, loss_few<T>, grid, kBlock, s, x->labels, wide, (int)n, V, x->scale, mean, r, x->loss, x->lse, X, x->x_stride,
                    (int)D, rows, (int)ws.Dp, lanes);
     } else {
         e = launch(p, kLossTargets, loss_targets, 1u, kScanBlock, s, x->labels, wide, n, V, x->scale, mean, r, x->loss, x->lse);

@@ -18,7 +18,7 @@ constexpr int kWideRow = 2048;                  // rows at least this long are s
 constexpr int kChanRows = 64;               // CHANNEL tiles: rows per row block
 constexpr int kBothRows = 64;               // composite_colsums tiles: rows per row block
 constexpr int kTopkRegs = 8;                // the selection keeps up to 8 keys per thread in registers
-constexpr int kVersion = 20400;          // 2.4.0 (major * 10000 + minor * 100 + patch)
+constexpr int kVersion = 20401;          // 2.4.1 (major * 10000 + minor * 100 + patch)
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v4f_at4 __attribute__((ext_vector_type(4), aligned(4)));   // four floats at any float's address
