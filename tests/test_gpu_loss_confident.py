@@ -21,7 +21,7 @@ def test_the_largest_logit_cancels(kind, n, V, held, monkeypatch):
     if held:
         monkeypatch.setenv("HSADMM_LOSS_HELD", held)
     say("confident", NAMES[kind], n, V, held)
-    c = Case(kind, n, 8, V, seed=1, share=0.0)
+    c = Case(kind, n, 8, V, seed=1, share=0.0, before=16 if n % 2 else 12)
     gap = torch.tensor([8.0, 10.0, 12.0, 14.0])[torch.arange(n) % 4].double().to(DEV)
     top = V // 3
     w, x = torch.zeros((V, 8)), torch.zeros((n, 8))
