@@ -922,9 +922,10 @@ int hsadmm_expand_mx(const hsadmm_plan_t* plan, const uint8_t* const* codes, con
 
 /*
  * The two ends of a language model's local training (Algorithm 1, Phase 1, for models whose first and last layer have a row per
- * token; the loss is that of any classifier too).  Such a layer is one of the plan's table, V = c_out rows of D = c_in weights with
- * khw = 1, and these calls read it in an arena of weights (the fp32 arena, or W_low of hsadmm_adamw) and write its gradient in a
- * gradient arena, where hsadmm_gradient_norms and hsadmm_adamw read it.  A call serves one replica.
+ * token; the loss is that of any classifier whose last layer has no bias, or has it as a column of W with an input of 1).  Such a
+ * layer is one of the plan's table, V = c_out rows of D = c_in weights with khw = 1, and these calls read it in an arena of weights
+ * (the fp32 arena, or W_low of hsadmm_adamw) and write its gradient in a gradient arena, where hsadmm_gradient_norms and
+ * hsadmm_adamw read it.  A call serves one replica.
  *   layer       index of the layer in the table (INVALID_ARGUMENT: out of range; UNSUPPORTED: khw != 1)
  *   type        HSADMM_TYPE_* of arenas and activations alike; sums are fp32, and every output is rounded once
  *   ids, labels device, n numbers of index_bits 32 or 64, aligned to their size.  One outside [0, V) is no token, no target
@@ -945,8 +946,8 @@ int hsadmm_embedding(const hsadmm_plan_t* plan, int32_t layer, const void* W, in
 /*
  * The gradient of that: G[v] = scale sum of dY[i] over the i with id_i = v, summed in the order of the tokens (those of a token with
  * many positions in parts first), for every row of the layer: rows without a token become 0.  With `accumulate` the sums are added
- * to what G holds (and rows without a token are left alone): several batches, or a layer that is the first and the last at once,
- * whose other gradient hsadmm_softmax_loss has written.  dY of positions that are no token is not read.
+ * to what G holds, and rounded to its type once a call (rows without a token are left alone): several batches, or a layer that is the
+ * first and the last at once, whose other gradient hsadmm_softmax_loss has written.  dY of positions that are no token is not read.
  *   workspace   device, hsadmm_embedding_workspace bytes, 256-byte aligned; nothing is kept in it between calls
  * n <= 2^27 (UNSUPPORTED beyond).  Errors: INVALID_ARGUMENT, WORKSPACE, UNSUPPORTED, HIP.
  */
@@ -979,7 +980,7 @@ int hsadmm_dropout(const hsadmm_plan_t* plan, const void* X, int64_t x_stride, c
  *     lse_i = log(sum_v exp(l_iv));  loss_i = lse_i - l_{i,label_i};  both 0 where label_i is no target
  *     total = { mean ? sum of the losses / max(count, 1) : sum, count }
  *     f = mean ? scale / max(count, 1) : scale;   P_iv = exp(l_iv - lse_i) - [v = label_i], rows without a target 0
- *     dX = f P W;   the layer's rows of G = f P^T X (with `accumulate` added to what G holds)
+ *     dX = f P W;   the layer's rows of G = f P^T X (with `accumulate` added to what G holds, and rounded to its type once a call)
  * `scale` multiplies the gradients alone (a loss scale of fp16 training).  Rows without a target cost nothing, and what X holds there
  * is not looked at.  Logits are formed in fp32; P is rounded to `type` (half precision: 2^15 P) for the products that follow, some of it
  * from exponentials that were rounded to `type` before.  What rounding the label's own P_i,label_i leaves, most of a row's gradient,

@@ -373,7 +373,8 @@ __device__ __forceinline__ v16f multiply(typename Wide<T>::vec a, typename Wide<
 // their way.  One barrier a turn, before its last step: the next turn's tiles have arrived, and this turn's are read, so their
 // places take the q of the turn after the next and the p of the one behind that.  Loads and LDS reads stand between the products.
 //
-// Bound by the matrix units at the clock that their power leaves (1.7 GHz, busy 70 % of the cycles): 8192 x 4096 x 32768 in bf16,
+// Bound by the matrix units at the clock that their power leaves (8192 x 4096 x 65536 in bf16: 1.65 GHz, busy 67 to 71 % of the cycles):
+// 8192 x 4096 x 32768 in bf16,
 // logits 1205 TFLOP/s, inputs' gradients 1230, weights' 1190 (a library's plain products of these sizes 1353, 1250, 1115).  Two whole
 // turns in LDS, each loaded in one go at its predecessor's beginning: 889, 896, 902; the same without loads 1248, 1596, 1439, without
 // products 1019, 1421, 1407, so the two hardly overlapped.  Four waves of 128 x 128 instead of eight of 128 x 64: 963, 1175, 1132.
@@ -430,7 +431,8 @@ __global__ __launch_bounds__(WP * WQ * kWave) void loss_product(ProductArgs a)
     const unsigned char* zeros = a.head->zeros;
     // Where one tile of rows sees all weights, which are then read once, workgroups begin at different turns: rows of a power of two of
     // bytes that all workgroups read at the same column keep a few of the memory's channels busy (one row x 2048 x 131072, bf16:
-    // 121 us, so 92, 5.8 TB/s).
+    // 121 us, so 92, 5.8 TB/s).  (The tiles of rows are those that have a target: their number is the one thing beside the sizes that
+    // the order of a logit's additions, and so its last bits, depend on.)
     const int begin = WHAT != kWeightGrads && a.tiles_q == 1 && once > 0 ? (int)(p0 / BP % once) : 0;
     const auto at_turn = [&](int turn) {
         const int u = (turn >= once && a.rest ? turn - once : turn) + begin;

@@ -8,7 +8,11 @@
 
 namespace {
 
-constexpr int64_t kLossHeld = 1ll << 31;   // bytes of logits, and then their gradients, that hsadmm_softmax_loss holds at once
+// Bytes of logits, and then their gradients, that hsadmm_softmax_loss holds at once.  A piece costs its logits a second time: 8192 x 2048 x
+// 131072 in bf16, a twentieth padding, 11.9 ms in one piece of 2^31 bytes, 13.3 in two, 14.1 in four, 14.6 in eight; 16384 rows, in two,
+// 26.5 for twice 11.9.  So more than this would save a tenth to a fifth of the largest calls only, for a workspace of as many more
+// gigabytes beside the model.
+constexpr int64_t kLossHeld = 1ll << 31;
 constexpr int kInputRows = 256;          // rows of the held copies are rounded up to this ...
 constexpr int kInputCols = 64;           // ... and their columns to this (128 bytes at least)
 constexpr int kLossHeadBytes = 512;
