@@ -63,7 +63,7 @@ static void check(int64_t size, bool gradients, int64_t n, int32_t D, int32_t V,
 
 int main()
 {
-    const int64_t ns[] = {0, 1, 2, 31, 32, 33, 48, 64, 65, 100, 127, 128, 129, 192, 255, 256, 257, 300, 511, 513, 1000, 1024, 1537, 4095, 4096, 8191, 16384, 65536};
+    const int64_t ns[] = {0, 1, 2, 31, 32, 33, 48, 64, 65, 100, 127, 128, 129, 192, 255, 256, 257, 300, 511, 513, 1000, 1024, 1537, 4095, 4096, 8191, 16384, 65536, 1000003, 1 << 21};
     const int32_t Ds[] = {1, 5, 8, 24, 63, 64, 65, 72, 128, 255, 256, 512, 1000, 1024, 1441, 2048, 4096, 4104, 8192, 16384};
     const int32_t Vs[] = {1, 3, 10, 64, 127, 128, 129, 255, 256, 257, 700, 1000, 4096, 4100, 8192, 16383, 16384, 20011, 32000, 32768, 65280, 65281, 65536, 70000,
                           131072, 151936, 262144, 1 << 20};
