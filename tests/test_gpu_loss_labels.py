@@ -9,6 +9,7 @@ may do (ref_tokens.py) is far below half a step of the result."""
 import pytest
 import torch
 
+import paper_2512_14628_amd as pkg
 from tests import ref_tokens as ref
 from tests.test_gpu_loss import BF16, DEV, F16, F32, NAMES, Case, say
 
@@ -113,3 +114,20 @@ def test_either_gradient_alone(outputs):
         assert torch.equal(a.dX, b.dX) and torch.isnan(b.G).all()
     else:
         assert torch.equal(a.layer(a.G), b.layer(b.G)) and torch.isnan(b.all_dx).all()
+
+
+def test_captured_calls_replay_with_other_labels():
+    """Which rows a tile of classes gathers follows from the labels that are there when the graph runs."""
+    c = spread(BF16, 600, 128, 2500, 19, 500)
+    ws = torch.zeros(pkg.hsadmm_softmax_loss_workspace(c.plan, 1, 600, BF16, True), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        pkg.hsadmm_softmax_loss(c.plan, 1, c.W, c.X, c.labels, workspace=ws, loss=c.loss[:600], dX=c.dX, G=c.G, type=BF16, index_bits=64)
+    for seed, named, few in ((20, 500, 1.0), (21, 3, 0.5), (22, 2500, 0.9), (23, 1, 1.0)):
+        other = spread(BF16, 600, 128, 2500, seed, named, few=few)
+        for a, b in ((c.X, other.X), (c.labels, other.labels), (c.W, other.W)):
+            a.copy_(b)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(other.run())
+        assert torch.equal(c.dX, other.dX) and torch.equal(c.layer(c.G), other.layer(other.G)) and torch.equal(c.loss[:600], other.loss[:600])
